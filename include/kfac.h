@@ -260,6 +260,83 @@ size_t kfac_precondition_inverse_workspace_bytes(int n, const kfac_precond_inv_i
 int kfac_precondition_batched_scaled(kfac_ctx *ctx, int n, const kfac_precond_item *items /* host */, float kappa,
                                      float lr, float *nu /* device, out */);
 
+/* ---- layers of experts -------------------------------------------------------------------------------------
+ * A layer of experts (a mixture-of-experts block's Linear) holds `experts` weight matrices W_e of one shape, and every row of
+ * its samples belongs to one of them.  Rows are sorted by expert: expert e owns rows offsets[e] .. offsets[e+1] - 1.  offsets lies in
+ * DEVICE memory, so what a router wrote there need not come to the host; an expert may have no rows, and rows in front of offsets[0]
+ * or behind offsets[experts]-1 belong to nobody.  Offsets are read as if clamped to [0, rows]; where they descend, which
+ * expert's result a row gets is undefined, but nothing outside the matrices is touched.
+ * The calls allocate nothing, need no workspace, copy nothing from the host and may be captured into a graph, which reads the offsets
+ * anew at every replay.  Sample matrices have a row pitch (in elements, at most 2^20) and may start at any element; a bf16 matrix
+ * whose rows all start on 16 bytes is read fastest.
+ *   append_ones : 1: the weights carry the bias as their last column, as the gradients that kfac_precondition() takes do */
+typedef struct {
+    int experts;             /* 1 .. 4096                                                                  */
+    int rows;                /* R, rows of the sample matrices; 0 <= R < 2^30                               */
+    int d_in, d_out;         /* 1 .. 65536                                                                 */
+    int append_ones;
+    int dtype;               /* of X, G, W, Y, dX                                                          */
+    const int *offsets;      /* device, [experts + 1]                                                      */
+} kfac_expert_desc;
+
+/* Y[r] = X[r] W_e^T for every row r of every expert, plus the last column of W_e with append_ones.
+ *   X [R][d_in] with pitch ldx;  W [experts][d_out][d_in + append_ones];  Y [R][d_out] with pitch ldy.  Sums in fp32, rounded once.
+ * Rows of Y that belong to nobody are left as they were, and so is what lies between a row's end and the pitch.  */
+int kfac_experts_forward(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *X, int64_t ldx, const void *W, void *Y, int64_t ldy);
+
+/* dX[r] = G[r] W_e (without the bias column): the gradient of the input from that of the output, G [R][d_out], dX [R][d_in].  */
+int kfac_experts_input_grad(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *G, int64_t ldg, const void *W, void *dX, int64_t ldx);
+
+/* dW_e = sum over the rows of e of G[r]^T [X[r] | 1 if append_ones], the gradient that kfac_precondition() takes for each expert.
+ *   dW [experts][d_out][d_in + append_ones], grad_dtype; zero for an expert without rows.
+ *   accumulate : 1: added to what dW holds (several batches before one step)  */
+int kfac_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *G, int64_t ldg, const void *X, int64_t ldx, int accumulate,
+                             void *dW, int grad_dtype);
+
+/* The running averages of every expert's Kronecker factor (kfac_update_factors() with the rows of one expert as the samples):
+ *   F_e <- decay * F_e + (1 - decay) * s_e * Xt^T Xt,   Xt = [X | 1] if append_ones else X, over the rows of e
+ *   mean  : 1: s_e = scale / rows of e, and an expert without rows keeps F_e as it is;  0: s_e = scale
+ *   F     : [experts][D][D] fp32, D = d + append_ones <= 8192, full symmetric storage, in/out, exactly symmetric; decay = 0 overwrites it
+ * bf16 samples are multiplied on the bf16 matrix instructions (exact products, fp32 sums).  The result is bit-reproducible.  */
+int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets /* device */, const void *X, int dtype, int64_t ldx, int d,
+                                int append_ones, int mean, float scale, float decay, float *F);
+
+/* ---- the optimizer step behind the preconditioner --------------------------------------------------------------
+ * The preconditioned gradient stands in place and any optimizer may follow (Listing 1); this is AdamW over a list of tensors:
+ *   g = grad * grad_scale;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2
+ *   param <- param - lr weight_decay param - lr (m / (1 - beta1^step)) / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * computed in fp32.  State in 32 bits (m_scale = v_scale = NULL): m and v are fp32.  State in 8 bits: m and v point to one byte for
+ * each element, OCP e4m3 codes of m and of sqrt(v), and m_scale / v_scale to one byte for each 128 elements (the last may be fewer), the power of
+ * two (biased by 127) that the codes are multiplied with: the smallest from 2^-127 on for which the block's largest magnitude is at
+ * most 448 times it.  Codes are rounded half to even; a sqrt(v) above zero is held as the smallest code above zero at least; what is not
+ * finite is held as NaN.  All bytes zero stand for a state of zero.  The parameter is updated with the moments before they are rounded.
+ * One launch for each 54 tensors and kind of state.  Nothing is copied from the host, no workspace is used, and the call may be captured; with
+ * step_dev, lr_dev and grad_scale its replays take another step each.  */
+typedef struct {
+    void *param;             /* in/out, [n]                                                                */
+    int param_dtype;         /* bf16 parameters are rounded half to even                                  */
+    const void *grad;        /* [n]                                                                        */
+    int grad_dtype;
+    void *m, *v;             /* in/out, [n]                                                                */
+    unsigned char *m_scale, *v_scale;   /* in/out, [(n + 127) / 128], or both NULL                          */
+    void *copy;              /* out, may be NULL: the updated parameter in bf16, e.g. the weights that the products above read */
+    int64_t n;               /* may be 0                                                                   */
+} kfac_adamw_item;
+typedef struct {
+    double beta1, beta2;     /* 0 <= beta < 1                                                              */
+    float lr, eps, weight_decay;
+    int64_t step;            /* t, counted from 1                                                          */
+    const float *grad_scale; /* DEVICE, may be NULL (1): e.g. the coefficient of a clipping by the global norm over the loss scale */
+    const float *lr_dev;     /* DEVICE, may be NULL: read instead of lr                                    */
+    const int64_t *step_dev; /* DEVICE, may be NULL: read instead of step (below 1 counts as 1)             */
+} kfac_adamw_opts;
+/* Tensors of one call, and the buffers of one tensor, must not overlap.  */
+int kfac_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items /* host */, const kfac_adamw_opts *opts /* host */);
+
+/* What an 8-bit state stands for (for checkpoints, and to go over to fp32 state): out[i] = code[i] * 2^(scale[i / 128] - 127), in fp32 or, as
+ * exactly, in bf16.  */
+int kfac_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype);
+
 /* Update-decoupled schedule (Sec. IV-C, Sec. V-C), host only: at iteration k refresh the factors
  * when k % f_fac == 0 and the eigendecompositions when k % f_eig == 0; precondition always.  */
 int kfac_schedule_due(int64_t k, int f_fac, int f_eig, int *do_factors, int *do_eig);

@@ -308,7 +308,8 @@ int kfac_profile_end(kfac_ctx *ctx, kfac_kernel_stat *out, int max, int *n) {
     static const char *names[KC_COUNT] = {"unfold", "syrk", "syrk_reduce", "precond_gemm", "eig_small",
                                           "eig_pivot_solve", "eig_apply", "eig_misc", "eig_post_gemm", "eig_copy", "eig_outer_cols",
                                           "precond_scale", "syrk_bf16", "precond_gemm_split", "eig_outer_rows", "factor_inverse",
-                                          "eig_reduce_mv", "eig_reduce_vec", "eig_reduce_update", "eig_tridiag_solve", "eig_back"};
+                                          "eig_reduce_mv", "eig_reduce_vec", "eig_reduce_update", "eig_tridiag_solve", "eig_back",
+                                          "experts", "experts_bf16", "adamw"};
     ctx->prof_on = false;
     KFAC_HIP_CHECK(hipStreamSynchronize(ctx->stream));
     kfac_kernel_stat acc[KC_COUNT] = {};
@@ -362,6 +363,80 @@ size_t kfac_precondition_workspace_bytes(int n, const kfac_precond_item *items) 
     for (int i = 0; i < n; ++i)
         if (items[i].dA < 1 || items[i].dG < 1 || items[i].dA > KFAC_MAX_D || items[i].dG > KFAC_MAX_D) return 0;
     return kfac_precond_ws_bytes_impl(n, items);
+}
+
+// The rows that a call touches must lie inside 31 bits each way; offsets are read on the device and clamped there.
+static bool valid_expert_desc(const kfac_expert_desc *d) {
+    if (!d || !d->offsets || ((uintptr_t)d->offsets & 3) || d->experts < 1 || d->experts > KFAC_MAX_EXPERTS) return false;
+    if (d->rows < 0 || d->rows >= 1 << 30 || (d->append_ones != 0 && d->append_ones != 1) || !valid_dtype(d->dtype)) return false;
+    return d->d_in >= 1 && d->d_out >= 1 && d->d_in <= KFAC_MAX_EXPERT_D && d->d_out <= KFAC_MAX_EXPERT_D;
+}
+static bool valid_pitch(int64_t ld, int d) { return ld >= d && ld <= KFAC_MAX_PITCH; }
+
+int kfac_experts_forward(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *X, int64_t ldx, const void *W, void *Y, int64_t ldy) {
+    if (!ctx || !valid_expert_desc(desc) || !W || Y == W) return KFAC_EINVAL;
+    if (!valid_pitch(ldx, desc->d_in) || !valid_pitch(ldy, desc->d_out)) return KFAC_EINVAL;
+    if (desc->rows == 0) return KFAC_OK;
+    if (!X || !Y || X == Y) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_forward(ctx, desc, X, ldx, W, Y, ldy);
+}
+
+int kfac_experts_input_grad(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *G, int64_t ldg, const void *W, void *dX, int64_t ldx) {
+    if (!ctx || !valid_expert_desc(desc) || !W || dX == W) return KFAC_EINVAL;
+    if (!valid_pitch(ldg, desc->d_out) || !valid_pitch(ldx, desc->d_in)) return KFAC_EINVAL;
+    if (desc->rows == 0) return KFAC_OK;
+    if (!G || !dX || G == dX) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_input_grad(ctx, desc, G, ldg, W, dX, ldx);
+}
+
+int kfac_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *desc, const void *G, int64_t ldg, const void *X, int64_t ldx, int accumulate,
+                             void *dW, int grad_dtype) {
+    if (!ctx || !valid_expert_desc(desc) || !dW || dW == G || dW == X || !valid_dtype(grad_dtype) || (accumulate != 0 && accumulate != 1)) return KFAC_EINVAL;
+    if (!valid_pitch(ldg, desc->d_out) || !valid_pitch(ldx, desc->d_in)) return KFAC_EINVAL;
+    if (desc->rows > 0 && (!G || !X)) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_weight_grad(ctx, desc, G, ldg, X, ldx, accumulate, dW, grad_dtype);
+}
+
+int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets, const void *X, int dtype, int64_t ldx, int d, int append_ones,
+                                int mean, float scale, float decay, float *F) {
+    const kfac_expert_desc desc{experts, rows, d, 1, append_ones, dtype, offsets};
+    if (!ctx || !valid_expert_desc(&desc) || !F || (const void *)F == X || (rows > 0 && !X) || (mean != 0 && mean != 1)) return KFAC_EINVAL;
+    if (d + append_ones > KFAC_MAX_D || !valid_pitch(ldx, d)) return KFAC_EINVAL;
+    if (!(decay >= 0.f && decay <= 1.f) || !std::isfinite(scale)) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_update_factors_experts(ctx, experts, rows, offsets, X, dtype, ldx, d, append_ones, mean, scale, decay, F);
+}
+
+int kfac_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items, const kfac_adamw_opts *o) {
+    if (!ctx || n < 0 || (n > 0 && !items) || !o) return KFAC_EINVAL;
+    if (!(o->beta1 >= 0.0 && o->beta1 < 1.0) || !(o->beta2 >= 0.0 && o->beta2 < 1.0) || !(o->eps >= 0.f) || !std::isfinite(o->eps)) return KFAC_EINVAL;
+    if (!(o->weight_decay >= 0.f) || !std::isfinite(o->weight_decay) || (!o->lr_dev && !std::isfinite(o->lr)) || (!o->step_dev && o->step < 1)) return KFAC_EINVAL;
+    for (int i = 0; i < n; ++i) {
+        const kfac_adamw_item &t = items[i];
+        if (t.n < 0 || !valid_dtype(t.param_dtype) || !valid_dtype(t.grad_dtype) || (t.m_scale == nullptr) != (t.v_scale == nullptr)) return KFAC_EINVAL;
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || t.m == t.v || t.param == t.m || t.param == t.v || t.param == t.grad || t.copy == t.param) return KFAC_EINVAL;
+        if ((t.m_scale && t.m_scale == t.v_scale) || t.grad == t.m || t.grad == t.v || (t.copy && (t.copy == t.grad || t.copy == t.m || t.copy == t.v))) return KFAC_EINVAL;
+    }
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_adamw_batched(ctx, n, items, o);
+}
+
+int kfac_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype) {
+    if (!ctx || n < 0 || !valid_dtype(dtype)) return KFAC_EINVAL;
+    if (n == 0) return KFAC_OK;
+    if (!codes || !scale || !out || codes == out || (const void *)scale == out) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_adamw_state_values(ctx, codes, scale, n, out, dtype);
 }
 
 int kfac_schedule_due(int64_t k, int f_fac, int f_eig, int *do_factors, int *do_eig) {

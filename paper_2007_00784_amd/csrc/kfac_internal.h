@@ -19,7 +19,8 @@ template <typename T> __device__ inline global_ptr<T> as_global(T *p) { return (
 enum KfacKernelClass {
     KC_UNFOLD = 0, KC_SYRK, KC_SYRK_REDUCE, KC_PRECOND_GEMM, KC_EIG_SMALL, KC_EIG_SOLVE, KC_EIG_APPLY,
     KC_EIG_MISC, KC_EIG_POST, KC_EIG_COPY, KC_EIG_OUTER, KC_PRECOND_SCALE, KC_SYRK_B16, KC_PRECOND_GEMM_X3, KC_EIG_OUTER_ROWS, KC_INVERSE,
-    KC_EIG_REDUCE_MV, KC_EIG_REDUCE_VEC, KC_EIG_REDUCE_GEMM, KC_EIG_TRI, KC_EIG_BACK, KC_COUNT
+    KC_EIG_REDUCE_MV, KC_EIG_REDUCE_VEC, KC_EIG_REDUCE_GEMM, KC_EIG_TRI, KC_EIG_BACK,
+    KC_EXPERTS, KC_EXPERTS_B16, KC_ADAMW, KC_COUNT
 };
 struct KfacProfRec { int cls; hipEvent_t t0, t1; double flops, bytes, share; };   // share: of the launch's time
 
@@ -76,6 +77,18 @@ struct KfacProfScope {
     }
 };
 
+// Makes the context's device the current one for the length of a call, whatever device the calling thread is on.
+struct KfacDeviceScope {
+    int before = -1;
+    bool ok;
+    explicit KfacDeviceScope(int device) {
+        ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+        if (before == device) before = -1;
+    }
+    ~KfacDeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+    KfacDeviceScope(const KfacDeviceScope &) = delete;
+};
+
 #define KFAC_HIP_CHECK(expr)                      \
     do {                                          \
         hipError_t _e = (expr);                   \
@@ -105,6 +118,9 @@ constexpr int KFAC_EIG_SMALL = 128;  // factors up to this size are solved insid
 constexpr int KFAC_EIG_REG = 256;    // factors up to this size are reduced to tridiagonal form inside one workgroup's registers
 constexpr int KFAC_EIG_B = 32;       // block size of the blocked Jacobi path (sub-problems are 2B x 2B)
 constexpr int KFAC_MAX_D = 8192;
+constexpr int KFAC_MAX_EXPERTS = 4096;
+constexpr int KFAC_MAX_EXPERT_D = 65536;   // sides of an expert's weights
+constexpr int64_t KFAC_MAX_PITCH = 1 << 20; // elements between the rows of samples: 32-bit offsets inside a tile
 constexpr int KFAC_EIG_SPLIT_MIN = 2048;   // factors from here on use split-fp16 products where an option allows them
 // A factor updated alone splits its contraction into at most this many partial tiles (or one per tile, if it has
 // more tiles than that): what kfac_workspace_bytes() sizes the workspace of a single update for.
@@ -148,5 +164,13 @@ size_t kfac_invert_ws_bytes_impl(int batch, const int *d);
 int kfac_launch_invert_factors(kfac_ctx *ctx, int batch, const float *const *F, const int *d, float damping, float *const *Finv);
 size_t kfac_precondition_inverse_ws_bytes_impl(int n, const kfac_precond_inv_item *items);
 int kfac_launch_precondition_inverse_batched(kfac_ctx *ctx, int n, const kfac_precond_inv_item *items);
+int kfac_launch_experts_forward(kfac_ctx *ctx, const kfac_expert_desc *d, const void *X, int64_t ldx, const void *W, void *Y, int64_t ldy);
+int kfac_launch_experts_input_grad(kfac_ctx *ctx, const kfac_expert_desc *d, const void *G, int64_t ldg, const void *W, void *dX, int64_t ldx);
+int kfac_launch_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *d, const void *G, int64_t ldg, const void *X, int64_t ldx, int accumulate,
+                                    void *dW, int grad_dtype);
+int kfac_launch_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets, const void *X, int dtype, int64_t ldx, int d, int append_ones,
+                                       int mean, float scale, float decay, float *F);
+int kfac_launch_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items, const kfac_adamw_opts *opts);
+int kfac_launch_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype);
 int kfac_launch_eig(kfac_ctx *ctx, int batch, const float *const *F, const int *d, float *const *Q,
                     float *const *lam, const kfac_eig_opts *opts, kfac_eig_info *info);

@@ -1,0 +1,229 @@
+// bf16 MFMA tile engine for operands in rows ([rows][d], d contiguous): one workgroup computes C = sum_k R(r, k) Q(c, k) for a
+// tile of ROWS x COLS outputs, K in slabs of 64 through two LDS buffers per operand.  An operand lies in memory in one of two ways:
+//   OpAlong   the contraction index is the contiguous one (rows of X against rows of W)
+//   OpAcross  the output index is the contiguous one (columns of W, of G or of X; the contraction walks over rows)
+// Both are moved by 16-byte loads that land in LDS (no registers, no LDS stores), and both end as the same operand registers of
+// v_mfma_f32_16x16x32_bf16: eight consecutive k of one output index per lane.  OpAlong reads them as one 16-byte LDS read; OpAcross
+// reads four k of sixteen columns at a time with the transposing LDS read (ds_read_b64_tr_b16: of a group of sixteen lanes, lane i
+// names the 8 bytes at row i / 4, columns 4 (i % 4)..; it is given column i of the four rows).
+//
+// The matrix core's first operand is the COLUMN side, so a lane's four accumulator registers are four consecutive columns of one
+// output row, which it stores as one vector.
+//
+// No load leaves its row: a group of eight that runs past the end of a row is taken from the row's last eight elements instead.  Along the
+// contraction the elements that the group before had already are cleared once they have landed; across it, the tile simply has them twice
+// and side() below says which column a place stands for.  So an extent of 8 at least is assumed, and any pitch.  What is outside an
+// operand (rows behind the last, k behind the end) is loaded with an offset that the buffer's range check turns into zeros.
+#pragma once
+#include "mfma_gemm.h"
+
+namespace kfac {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 wide_bf16x8 __attribute__((ext_vector_type(8)));
+typedef short wide_s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int WK = 64;                      // contraction indices of a slab
+constexpr int WIDE_MIN = 8;                 // smallest extent of any side
+
+__device__ inline const void *uniform_ptr(const void *p) {
+    const uint64_t a = (uint64_t)p;
+    return (const void *)(((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)a));
+}
+
+// 64 x 16 bytes from `off` bytes behind the descriptor's base into 1 KB of LDS at `lds` (the same for the whole wave), lane l at 16 l.
+// The compiler would make every later LDS read wait for it, whatever part of LDS it reads; the waits stand in the loop.
+typedef int wide_rsrc __attribute__((ext_vector_type(4)));
+__device__ inline wide_rsrc wide_buffer(const void *base, unsigned extent) {
+    const uint64_t a = (uint64_t)uniform_ptr(base);
+    return wide_rsrc{(int)a, (int)(a >> 32) & 0xffff, __builtin_amdgcn_readfirstlane((int)extent), 0x00020000};
+}
+__device__ inline void load_to_lds(wide_rsrc rs, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(rs), "s"(lds) : "memory", "m0");
+}
+__device__ inline unsigned lds_address(const void *p) {
+    return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+
+// Which output index the place `at` (from the matrix' first on) of an OpAcross operand with `n` of them stands for, or -1: places n8.. n8 + 7 of
+// a row whose length is n8 + r, 0 < r < 8, hold its last eight, of which the first 8 - r are already there.
+__device__ inline int across_side(int at, int n) {
+    const int n8 = n & ~7, r = n & 7;
+    if (at < n8) return at;
+    if (r == 0 || at >= n8 + 8) return -1;
+    return at - n8 >= 8 - r ? at - (8 - r) : -1;
+}
+
+// elem(i, k) = p[i * ld + k], i < rows, k < K; K >= 8.  EXT output indices from `i0` on; NW waves.
+template <int EXT, int NW>
+struct OpAlong {
+    static constexpr int LOADS = EXT / 8 / NW, BYTES = EXT * WK * 2;
+    const unsigned short *p;      // row i0
+    int64_t ld;
+    int K;
+    unsigned extent, off[LOADS];
+    int g;                        // group of eight k of this thread, the same for its loads
+    __device__ void start(const unsigned short *base, int64_t ld_, int i0, int rows, int K_) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        ld = ld_;
+        K = K_;
+        p = (const unsigned short *)uniform_ptr(base + (int64_t)i0 * ld);
+        extent = (unsigned)((int64_t)min(rows - i0, EXT) * ld * 2);
+        g = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) off[u] = (unsigned)((wave * 8 + (lane >> 3) + u * 8 * NW) * ld * 2 + g * 16);
+    }
+    __device__ int over(int k0) const { return min(max(k0 + 8 * g + 8 - K, 0), 8); }    // of the group's eight, how many are behind the end
+    __device__ void issue(unsigned slab, int k0) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (k0 + WK <= K) {
+            const auto rs = wide_buffer(p + k0, extent - 2u * k0);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) load_to_lds(rs, off[u], slab + (wave * 8 + u * 8 * NW) * (WK * 2));
+        } else {
+            const auto rs = wide_buffer(p, extent);
+            const int o = over(k0);
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u)
+                load_to_lds(rs, o < 8 ? off[u] + 2u * k0 - 2u * o : BUF_OUTSIDE, slab + (wave * 8 + u * 8 * NW) * (WK * 2));
+        }
+    }
+    // Once the slab's loads have landed: clear what the last, shifted group holds of the one before.
+    __device__ void patch(char *slab, int k0) const {
+        const int o = over(k0);
+        if (o == 0 || o == 8) return;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        unsigned keep[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) keep[w] = (2 * w >= o ? 0xffffu : 0u) | (2 * w + 1 >= o ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            uint4 *x = reinterpret_cast<uint4 *>(slab + (wave * 8 + (lane >> 3) + u * 8 * NW) * (WK * 2) + (lane & 7) * 16);
+            uint4 v = *x;
+            v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+            *x = v;
+        }
+    }
+    // The registers of output indices i .. i + 15 (i a multiple of 16, in the tile) and k-step ks (32 k each).
+    __device__ static wide_bf16x8 fragment(const char *slab, int i, int ks) {
+        const int lane = threadIdx.x & 63;
+        wide_bf16x8 x;
+        __builtin_memcpy(&x, __builtin_assume_aligned(slab + (i + (lane & 15)) * (WK * 2) + (((4 * ks + (lane >> 4)) ^ (lane & 7)) * 16), 16), 16);
+        return x;
+    }
+    __device__ int side(int at) const { return at; }      // (the caller knows how many there are)
+};
+
+// elem(i, k) = p[k * ld + i], i < n, k < K; n >= 8.  MAPPED: the other operand is an OpAlong with the same K, whose last group is shifted.
+template <int EXT, int NW, bool MAPPED>
+struct OpAcross {
+    static constexpr int PITCH = EXT * 2, PER = 1024 / PITCH, LOADS = WK / PER / NW, BYTES = EXT * WK * 2;
+    const unsigned short *p;      // row 0
+    int64_t ld;
+    int K, n;
+    unsigned off[LOADS];
+    int k_of[MAPPED ? LOADS : 1];
+    // 32-byte units of a row of LDS are permuted by k, so that the four rows of a transposing read (and the four eight rows on, which the
+    // next sixteen lanes read) lie on different banks
+    __device__ static int swizzle(int k) { return (k & 3) | ((k >> 1) & 4); }
+    __device__ void start(const unsigned short *base, int64_t ld_, int i0, int n_, int K_) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        ld = ld_;
+        K = K_;
+        n = n_;
+        p = (const unsigned short *)uniform_ptr(base);
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) {
+            const int k = (wave + u * NW) * PER + lane / (EXT / 8), slot = lane % (EXT / 8);
+            const int at = i0 + 8 * (2 * ((slot >> 1) ^ swizzle(k)) + (slot & 1));
+            off[u] = at >= n ? BUF_OUTSIDE : (unsigned)(((int64_t)k * ld + min(at, n - 8)) * 2);
+            if (MAPPED) k_of[u] = k;
+        }
+    }
+    __device__ void issue(unsigned slab, int k0) const {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (!MAPPED || k0 + WK <= K) {
+            const auto rs = wide_buffer(p + (int64_t)k0 * ld, (unsigned)min((int64_t)(K - k0) * ld * 2, (int64_t)BUF_EXTENT));
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) load_to_lds(rs, off[u], slab + (wave + u * NW) * 1024);
+        } else {
+            const int back = min(k0, 8), r = K & 7, k8 = K & ~7;
+            const auto rs = wide_buffer(p + (int64_t)(k0 - back) * ld, (unsigned)min((int64_t)(K - k0 + back) * ld * 2, (int64_t)BUF_EXTENT));
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const int k = k0 + k_of[u], shift = k < k8 ? 0 : 8 - r;
+                const bool in = off[u] != BUF_OUTSIDE && (k < k8 || (r != 0 && k < k8 + 8 && k - k8 >= 8 - r));
+                load_to_lds(rs, in ? off[u] + (unsigned)((back - shift) * ld * 2) : BUF_OUTSIDE, slab + (wave + u * NW) * 1024);
+            }
+        }
+    }
+    __device__ void patch(char *, int) const {}
+    __device__ static wide_bf16x8 fragment(const char *slab, int i, int ks) {
+        const int lane = threadIdx.x & 63, sixteenth = lane & 15, q = lane >> 4;
+        const int k = 32 * ks + 8 * q + (sixteenth >> 2);
+        const char *a = slab + k * PITCH + (((i >> 4) ^ swizzle(k)) << 5) + (sixteenth & 3) * 8;
+        typedef __attribute__((address_space(3))) wide_s16x4 *lds4;
+        const wide_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(__attribute__((address_space(3))) char *)a);
+        const wide_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(__attribute__((address_space(3))) char *)(a + 4 * PITCH));
+        wide_bf16x8 x;
+        __builtin_memcpy(&x, &lo, 8);
+        __builtin_memcpy((char *)&x + 8, &hi, 8);
+        return x;
+    }
+    __device__ int side(int at) const { return across_side(at, n); }
+};
+
+// Tile of (16 FR WR) rows x (16 FC WC) columns for WR x WC waves.  acc[i][j]: columns 16 i.., rows 16 j.. of the wave's part.  ONES: with
+// `sums`, one[] of the wave whose column is wc takes the sums over k of row fragments wc FR / WC .. (in every register the same).
+template <class R, class Q, int FR, int FC, int WR, int WC, bool ONES>
+__device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
+#pragma unroll
+    for (int i = 0; i < FC; ++i)
+#pragma unroll
+        for (int j = 0; j < FR; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (ONES)
+#pragma unroll
+        for (int j = 0; j < FR / WC; ++j) one[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (K <= 0) return;
+    wide_bf16x8 unit;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) unit[e] = (__bf16)1.0f;
+    constexpr int STAGE = R::BYTES + Q::BYTES;
+    const unsigned base = lds_address(smem);
+    const int nslab = (K + WK - 1) / WK;
+    row.issue(base, 0);
+    col.issue(base + R::BYTES, 0);
+    for (int s = 0; s < nslab; ++s) {
+        char *cur = smem + (s & 1) * STAGE;
+        const unsigned nxt = base + ((s & 1) ^ 1) * STAGE;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wave's part of slab s has landed
+        if (s + 1 == nslab) {
+            row.patch(cur, s * WK);
+            col.patch(cur + R::BYTES, s * WK);
+        }
+        __syncthreads();                                      // everybody's has, and nobody reads the other buffer any more
+        if (s + 1 < nslab) {
+            row.issue(nxt, (s + 1) * WK);
+            col.issue(nxt + R::BYTES, (s + 1) * WK);
+        }
+#pragma unroll
+        for (int ks = 0; ks < WK / 32; ++ks) {
+            wide_bf16x8 a[FC], b[FR];
+#pragma unroll
+            for (int i = 0; i < FC; ++i) a[i] = Q::fragment(cur + R::BYTES, 16 * (wc * FC + i), ks);
+#pragma unroll
+            for (int j = 0; j < FR; ++j) b[j] = R::fragment(cur, 16 * (wr * FR + j), ks);
+#pragma unroll
+            for (int j = 0; j < FR; ++j)
+#pragma unroll
+                for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+            if (ONES && sums)
+#pragma unroll
+                for (int j = 0; j < FR; ++j)
+                    if (j / (FR / WC) == wc) one[j % (FR / WC)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unit, b[j], one[j % (FR / WC)], 0, 0, 0);
+        }
+    }
+}
+
+}  // namespace kfac

@@ -23,6 +23,8 @@ EXPORTS = (
     "kfac_update_factors_static", "kfac_static_scratch_bytes",
     "kfac_invert_factors", "kfac_invert_workspace_bytes", "kfac_precondition_inverse",
     "kfac_precondition_inverse_batched", "kfac_precondition_inverse_workspace_bytes",
+    "kfac_experts_forward", "kfac_experts_input_grad", "kfac_experts_weight_grad", "kfac_update_factors_experts",
+    "kfac_adamw_batched", "kfac_adamw_state_values",
 )
 
 
@@ -61,6 +63,23 @@ class kfac_factor_item(ctypes.Structure):
     _fields_ = [("X", ctypes.c_void_p), ("dtype", ctypes.c_int), ("layout", ctypes.c_int),
                 ("N", ctypes.c_int), ("d", ctypes.c_int), ("T", ctypes.c_int), ("append_ones", ctypes.c_int),
                 ("scale", ctypes.c_float), ("decay", ctypes.c_float), ("F", ctypes.c_void_p)]
+
+
+class kfac_expert_desc(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int), ("rows", ctypes.c_int), ("d_in", ctypes.c_int), ("d_out", ctypes.c_int),
+                ("append_ones", ctypes.c_int), ("dtype", ctypes.c_int), ("offsets", ctypes.c_void_p)]
+
+
+class kfac_adamw_item(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("param_dtype", ctypes.c_int), ("grad", ctypes.c_void_p), ("grad_dtype", ctypes.c_int),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class kfac_adamw_opts(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("lr", ctypes.c_float), ("eps", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("step", ctypes.c_int64), ("grad_scale", ctypes.c_void_p),
+                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p)]
 
 
 class KfacError(RuntimeError):
@@ -115,6 +134,13 @@ def lib():
     L.kfac_precondition_inverse_batched.argtypes = [vp, i, ctypes.POINTER(kfac_precond_inv_item)]
     L.kfac_precondition_inverse_workspace_bytes.argtypes = [i, ctypes.POINTER(kfac_precond_inv_item)]
     L.kfac_precondition_inverse_workspace_bytes.restype = sz
+    dp = ctypes.POINTER(kfac_expert_desc)
+    L.kfac_experts_forward.argtypes = [vp, dp, vp, i64, vp, vp, i64]
+    L.kfac_experts_input_grad.argtypes = [vp, dp, vp, i64, vp, vp, i64]
+    L.kfac_experts_weight_grad.argtypes = [vp, dp, vp, i64, vp, i64, i, vp, i]
+    L.kfac_update_factors_experts.argtypes = [vp, i, i, vp, vp, i, i64, i, i, i, f, f, vp]
+    L.kfac_adamw_batched.argtypes = [vp, i, ctypes.POINTER(kfac_adamw_item), ctypes.POINTER(kfac_adamw_opts)]
+    L.kfac_adamw_state_values.argtypes = [vp, vp, vp, i64, vp, i]
     L.kfac_profile_begin.argtypes = [vp]
     L.kfac_profile_end.argtypes = [vp, ctypes.POINTER(kfac_kernel_stat), i, ip]
     for name in EXPORTS:
@@ -358,6 +384,149 @@ def kfac_precondition_workspace_bytes(dims):
     for j, (dA, dG) in enumerate(dims):
         arr[j].dA, arr[j].dG = int(dA), int(dG)
     return int(lib().kfac_precondition_workspace_bytes(len(dims), arr))
+
+
+# ---- layers of experts ----
+def _rows(t, name, d):
+    """(address, row pitch) of a matrix of samples [R][d]: any pitch, but the elements of a row side by side."""
+    if t.dim() != 2 or t.shape[1] != d:
+        raise ValueError("%s must be [R, %d]" % (name, d))
+    if t.shape[0] == 0:
+        return None, d
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    ld = t.stride(0) if t.shape[0] > 1 else max(d, t.stride(0))
+    if ld < d:
+        raise ValueError("the rows of %s overlap" % name)
+    return t.data_ptr(), ld
+
+
+def _offsets(t, experts):
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != experts + 1:
+        raise ValueError("offsets must be int32 [experts + 1]")
+    return _ptr(t)
+
+
+def _expert_desc(weight, offsets, rows, append_ones, dtype):
+    """weight: [experts, d_out, d_in + append_ones] (the weights or their gradient), rows: the number of sample rows."""
+    experts, d_out, wide = weight.shape
+    ones = int(bool(append_ones))
+    if wide - ones < 1:
+        raise ValueError("weights without inputs")
+    return kfac_expert_desc(experts, rows, wide - ones, d_out, ones, dtype, _offsets(offsets, experts))
+
+
+def _same(a, b, names):
+    if a.dtype != b.dtype:
+        raise ValueError("%s must have one dtype" % names)
+
+
+def kfac_experts_forward(ctx, X, W, offsets, Y, append_ones=False):
+    """Y[r] = X[r] W_e^T (+ the last column of W_e).  X [R, d_in], W [experts, d_out, d_in + append_ones], Y [R, d_out] (both with any row
+    pitch), offsets int32 [experts + 1] on the GPU."""
+    desc = _expert_desc(W, offsets, X.shape[0], append_ones, _dtype_code(X))
+    _same(X, W, "X and W")
+    _same(X, Y, "X and Y")
+    if Y.shape[0] != X.shape[0]:
+        raise ValueError("X and Y must have as many rows")
+    xp, ldx = _rows(X, "X", desc.d_in)
+    yp, ldy = _rows(Y, "Y", desc.d_out)
+    _check(lib().kfac_experts_forward(ctx, ctypes.byref(desc), xp, ldx, _ptr(W), yp, ldy), "kfac_experts_forward")
+
+
+def kfac_experts_input_grad(ctx, G, W, offsets, dX, append_ones=False):
+    """dX[r] = G[r] W_e, without the bias column.  G [R, d_out], dX [R, d_in]."""
+    desc = _expert_desc(W, offsets, G.shape[0], append_ones, _dtype_code(G))
+    _same(G, W, "G and W")
+    _same(G, dX, "G and dX")
+    if dX.shape[0] != G.shape[0]:
+        raise ValueError("G and dX must have as many rows")
+    gp, ldg = _rows(G, "G", desc.d_out)
+    xp, ldx = _rows(dX, "dX", desc.d_in)
+    _check(lib().kfac_experts_input_grad(ctx, ctypes.byref(desc), gp, ldg, _ptr(W), xp, ldx), "kfac_experts_input_grad")
+
+
+def kfac_experts_weight_grad(ctx, G, X, offsets, dW, append_ones=False, accumulate=False):
+    """dW_e = sum over the rows of e of G[r]^T [X[r] | 1 if append_ones] (added to dW with accumulate).  dW [experts, d_out, d_in + append_ones]
+    in fp32 or bf16; dW[e] is the gradient that the preconditioner takes."""
+    desc = _expert_desc(dW, offsets, G.shape[0], append_ones, _dtype_code(G))
+    _same(G, X, "G and X")
+    if X.shape[0] != G.shape[0]:
+        raise ValueError("G and X must have as many rows")
+    gp, ldg = _rows(G, "G", desc.d_out)
+    xp, ldx = _rows(X, "X", desc.d_in)
+    _check(lib().kfac_experts_weight_grad(ctx, ctypes.byref(desc), gp, ldg, xp, ldx, int(bool(accumulate)), _ptr(dW), _dtype_code(dW)),
+           "kfac_experts_weight_grad")
+
+
+def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0, decay=0.0, mean=True):
+    """F_e <- decay F_e + (1 - decay) s_e Xt^T Xt over the rows of e, Xt = [X | 1 if append_ones]; s_e = scale / rows of e (an expert
+    without rows keeps its factor), or scale with mean=False.  X [R, d], F [experts, D, D] fp32."""
+    import torch
+    ones = int(bool(append_ones))
+    if F.dim() != 3 or F.dtype != torch.float32 or F.shape[1] != F.shape[2] or F.shape[1] != X.shape[1] + ones:
+        raise ValueError("F must be float32 [experts, D, D], D = d + append_ones")
+    experts, d = F.shape[0], X.shape[1]
+    xp, ldx = _rows(X, "X", d)
+    _check(lib().kfac_update_factors_experts(ctx, experts, X.shape[0], _offsets(offsets, experts), xp, _dtype_code(X), ldx, d, ones,
+                                             int(bool(mean)), float(scale), float(decay), _ptr(F)), "kfac_update_factors_experts")
+
+
+# ---- the optimizer step ----
+def adamw_items(items):
+    """The marshalled item array of kfac_adamw_batched for a list of dicts(param, grad, m, v[, m_scale, v_scale][, copy]) of device tensors,
+    reusable while the buffers live.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or uint8), m_scale, v_scale uint8, one for
+    each 128 elements.  copy: bfloat16, takes the updated parameter."""
+    import torch
+    arr = (kfac_adamw_item * len(items))()
+    for j, it in enumerate(items):
+        p, g, m, v, ms, vs, copy = (it.get(k) for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy"))
+        n = p.numel()
+        if g.numel() != n or m.numel() != n or v.numel() != n or (copy is not None and copy.numel() != n):
+            raise ValueError("item %d: buffers of different lengths" % j)
+        if (ms is None) != (vs is None):
+            raise ValueError("item %d: both scales or none" % j)
+        if ms is None:
+            if m.dtype != torch.float32 or v.dtype != torch.float32:
+                raise ValueError("item %d: m and v must be float32 (or come with scales)" % j)
+        else:
+            blocks = (n + 127) // 128
+            if m.element_size() != 1 or v.element_size() != 1 or any(s.dtype != torch.uint8 or s.numel() != blocks for s in (ms, vs)):
+                raise ValueError("item %d: m and v must have a byte for each element, the scales (uint8) one for each 128" % j)
+        if copy is not None and copy.dtype != torch.bfloat16:
+            raise ValueError("item %d: copy must be bfloat16" % j)
+        arr[j] = kfac_adamw_item(_ptr(p), _dtype_code(p), _ptr(g), _dtype_code(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), _ptr(copy), n)
+    return arr
+
+
+def _scalar(t, dtype, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != 1:
+        raise ValueError("%s must be one %s" % (name, dtype))
+    return _ptr(t)
+
+
+def kfac_adamw_batched(ctx, items, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, grad_scale=None):
+    """One AdamW step over a list of tensors (see adamw_items()).  lr and step: numbers, or device tensors of one float32 / int64 that the call
+    reads on the GPU; grad_scale: None or a device tensor of one float32 that every gradient is multiplied with."""
+    import torch
+    arr = adamw_items(items) if isinstance(items, list) else items
+    lr_dev = _scalar(lr, torch.float32, "lr") if torch.is_tensor(lr) else None
+    step_dev = _scalar(step, torch.int64, "step") if torch.is_tensor(step) else None
+    o = kfac_adamw_opts(float(beta1), float(beta2), 0.0 if lr_dev else float(lr), float(eps), float(weight_decay), 1 if step_dev else int(step),
+                        _scalar(grad_scale, torch.float32, "grad_scale"), lr_dev, step_dev)
+    _check(lib().kfac_adamw_batched(ctx, len(arr), arr, ctypes.byref(o)), "kfac_adamw_batched")
+
+
+def kfac_adamw_state_values(ctx, codes, scale, out):
+    """out[i] = codes[i] * 2^(scale[i // 128] - 127): what an 8-bit state stands for (m, and sqrt(v)), float32 or bfloat16."""
+    import torch
+    n = codes.numel()
+    if codes.element_size() != 1 or out.numel() != n or scale.dtype != torch.uint8 or scale.numel() != (n + 127) // 128:
+        raise ValueError("codes: a byte for each element of out, scale: uint8, one for each 128")
+    _check(lib().kfac_adamw_state_values(ctx, _ptr(codes), _ptr(scale), n, _ptr(out), _dtype_code(out)), "kfac_adamw_state_values")
 
 
 def kfac_schedule_due(k, f_fac, f_eig):

@@ -1,0 +1,128 @@
+"""What the calls for layers of experts and the optimizer step refuse, on the CPU: every refusal comes before the context is looked at, let
+alone a launch, so a block of bytes stands for the context and any address for a buffer."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2007_00784_amd import kfac as K
+
+CTX = ctypes.create_string_buffer(4096)
+A, B, C, D = 4096, 8192, 12288, 16384        # addresses that nothing reads
+
+
+def desc(**kw):
+    d = dict(experts=4, rows=100, d_in=64, d_out=32, append_ones=0, dtype=K.KFAC_BF16, offsets=D)
+    d.update(kw)
+    return ctypes.byref(K.kfac_expert_desc(**d))
+
+
+BAD_DESCS = [dict(experts=0), dict(experts=4097), dict(rows=-1), dict(rows=1 << 30), dict(d_in=0), dict(d_out=0), dict(d_in=65537), dict(d_out=65537),
+             dict(append_ones=2), dict(append_ones=-1), dict(dtype=2), dict(offsets=None), dict(offsets=D + 2)]
+
+
+@pytest.mark.parametrize("bad", BAD_DESCS, ids=str)
+def test_descriptions_of_a_layer(bad):
+    L = K.lib()
+    wide = 1 << 17
+    assert L.kfac_experts_forward(CTX, desc(**bad), A, wide, B, C, wide) == K.KFAC_EINVAL
+    assert L.kfac_experts_input_grad(CTX, desc(**bad), A, wide, B, C, wide) == K.KFAC_EINVAL
+    assert L.kfac_experts_weight_grad(CTX, desc(**bad), A, wide, B, wide, 0, C, K.KFAC_F32) == K.KFAC_EINVAL
+    if "d_out" not in bad:
+        d = dict(experts=4, rows=100, offsets=D, dtype=K.KFAC_BF16, d_in=64, append_ones=0)
+        d.update(bad)
+        assert L.kfac_update_factors_experts(CTX, d["experts"], d["rows"], d["offsets"], A, d["dtype"], wide, d["d_in"], d["append_ones"], 1, 1.0, 0.5, C) == K.KFAC_EINVAL
+
+
+def test_matrices_of_products():
+    L = K.lib()
+    bad = K.KFAC_EINVAL
+    for f in (L.kfac_experts_forward, L.kfac_experts_input_grad):
+        assert f(None, desc(), A, 64, B, C, 64) == bad
+        assert f(CTX, None, A, 64, B, C, 64) == bad
+        assert f(CTX, desc(), None, 64, B, C, 64) == bad
+        assert f(CTX, desc(), A, 64, None, C, 64) == bad
+        assert f(CTX, desc(), A, 64, B, None, 64) == bad
+        assert f(CTX, desc(), A, 64, B, A, 64) == bad          # output on an input
+        assert f(CTX, desc(), A, 64, B, B, 64) == bad
+        assert f(CTX, desc(), A, 31, B, C, 64) == bad          # pitch below the row
+        assert f(CTX, desc(), A, 64, B, C, 31) == bad
+        assert f(CTX, desc(), A, (1 << 20) + 1, B, C, 64) == bad
+        assert f(CTX, desc(), A, 64, B, C, (1 << 20) + 1) == bad
+        assert f(CTX, desc(rows=0), None, 64, B, None, 64) == K.KFAC_OK
+    f = L.kfac_experts_weight_grad
+    for args in ((None, 64, B, 64, 0, C, 0), (A, 64, None, 64, 0, C, 0), (A, 64, B, 64, 0, None, 0), (A, 64, B, 64, 2, C, 0), (A, 64, B, 64, 0, C, 2),
+                 (A, 64, B, 64, 0, A, 0), (A, 64, B, 64, 0, B, 0), (A, 31, B, 64, 0, C, 0), (A, 64, B, 63, 0, C, 0), (A, 64, B, (1 << 20) + 1, 0, C, 0)):
+        assert f(CTX, desc(), *args) == bad, args
+    f = L.kfac_update_factors_experts
+    nan, inf = float("nan"), float("inf")
+    #           X  dt ldx d   1s mean scale decay F
+    for args in ((None, 1, 64, 64, 0, 1, 1.0, 0.5, C), (A, 1, 64, 64, 0, 1, 1.0, 0.5, None), (A, 1, 64, 64, 0, 1, 1.0, 0.5, A), (A, 1, 63, 64, 0, 1, 1.0, 0.5, C),
+                 (A, 1, 9000, 8193, 0, 1, 1.0, 0.5, C), (A, 1, 9000, 8192, 1, 1, 1.0, 0.5, C), (A, 1, 64, 64, 0, 2, 1.0, 0.5, C), (A, 1, 64, 64, 0, 1, nan, 0.5, C),
+                 (A, 1, 64, 64, 0, 1, inf, 0.5, C), (A, 1, 64, 64, 0, 1, 1.0, -0.1, C), (A, 1, 64, 64, 0, 1, 1.0, 1.1, C), (A, 1, 64, 64, 0, 1, 1.0, nan, C)):
+        assert f(CTX, 4, 100, D, *args) == bad, args
+    assert f(None, 4, 100, D, A, 1, 64, 64, 0, 1, 1.0, 0.5, C) == bad
+
+
+def adamw(item=None, opts=None, n=1, ctx=CTX):
+    it = dict(param=A, param_dtype=0, grad=B, grad_dtype=0, m=C, v=D, m_scale=None, v_scale=None, copy=None, n=10)
+    it.update(item or {})
+    o = dict(beta1=0.9, beta2=0.999, lr=1e-3, eps=1e-8, weight_decay=0.0, step=1)
+    o.update(opts or {})
+    return K.lib().kfac_adamw_batched(ctx, n, (K.kfac_adamw_item * 1)(K.kfac_adamw_item(**it)), ctypes.byref(K.kfac_adamw_opts(**o)))
+
+
+def test_optimizer_step():
+    bad = K.KFAC_EINVAL
+    for item in (dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(n=-1), dict(param_dtype=2), dict(grad_dtype=-1), dict(m_scale=A + 1), dict(v_scale=A + 1),
+                 dict(m_scale=A + 1, v_scale=A + 1), dict(v=C), dict(grad=A), dict(m=A), dict(v=A), dict(copy=A), dict(copy=B), dict(copy=C), dict(copy=D), dict(grad=C), dict(grad=D)):
+        assert adamw(item) == bad, item
+    nan, inf = float("nan"), float("inf")
+    for opts in (dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan), dict(beta2=1.0), dict(beta2=nan), dict(eps=-1e-8), dict(eps=nan), dict(eps=inf), dict(weight_decay=-0.1),
+                 dict(weight_decay=nan), dict(weight_decay=inf), dict(lr=nan), dict(lr=inf), dict(step=0), dict(step=-3)):
+        assert adamw(opts=opts) == bad, opts
+    assert adamw(n=-1) == bad and adamw(ctx=None) == bad
+    L = K.lib()
+    assert L.kfac_adamw_batched(CTX, 1, None, ctypes.byref(K.kfac_adamw_opts(beta1=0.9, beta2=0.9, step=1))) == bad
+    assert L.kfac_adamw_batched(CTX, 0, None, None) == bad
+    f = L.kfac_adamw_state_values
+    assert f(CTX, A, B, 10, C, 2) == bad and f(CTX, A, B, -1, C, 0) == bad and f(None, A, B, 10, C, 0) == bad
+    assert f(CTX, None, B, 10, C, 0) == bad and f(CTX, A, None, 10, C, 0) == bad and f(CTX, A, B, 10, None, 0) == bad
+    assert f(CTX, A, B, 10, A, 0) == bad and f(CTX, A, B, 10, B, 0) == bad
+    assert f(CTX, None, None, 0, None, 0) == K.KFAC_OK
+
+
+def test_tensors_that_do_not_fit():
+    off = torch.zeros(5, dtype=torch.int32)
+    X, W, Y = torch.zeros(10, 16), torch.zeros(4, 24, 16), torch.zeros(10, 24)
+    bf = torch.bfloat16
+    for args in ((X, W, off[:4], Y), (X, W, off.long(), Y), (X, W, off, Y[:9]), (X, W, off, Y[:, :23]), (X[:, :15], W, off, Y), (X, W.to(bf), off, Y),
+                 (X, W, off, Y.to(bf)), (X.double(), W.double(), off, Y.double()), (torch.zeros(16, 10).t(), W, off, Y), (X[:1].expand(10, 16), W, off, Y),
+                 (X, W.transpose(1, 2).contiguous().transpose(1, 2), off, Y)):
+        with pytest.raises(ValueError):
+            K.kfac_experts_forward(CTX, *args)
+    for args in ((Y, W, off, X[:, :15]), (Y[:9], W, off, X), (Y[:, :20], W, off, X), (Y.to(bf), W, off, X)):
+        with pytest.raises(ValueError):
+            K.kfac_experts_input_grad(CTX, *args)
+    for args in ((Y, X, off, W[:, :, :15]), (Y[:9], X, off, W), (Y, X.to(bf), off, W), (Y, X, off, W.half())):
+        with pytest.raises(ValueError):
+            K.kfac_experts_weight_grad(CTX, *args)
+    F = torch.zeros(4, 16, 16)
+    for args, kw in (((X, off, F), dict(append_ones=True)), ((X, off, F.to(bf)), {}), ((X, off[:3], F), {}), ((X, off, F[:, :15, :15]), {})):
+        with pytest.raises(ValueError):
+            K.kfac_update_factors_experts(CTX, *args, **kw)
+    p, u = torch.zeros(300), torch.zeros(300, dtype=torch.uint8)
+    s = torch.zeros(3, dtype=torch.uint8)
+    good = dict(param=p, grad=p, m=p, v=p)
+    eight = dict(param=p, grad=p, m=u, v=u, m_scale=s, v_scale=s)
+    K.adamw_items([good, eight])
+    for it in (dict(good, grad=p[:299]), dict(good, m=u), dict(good, m_scale=s), dict(eight, m=p), dict(eight, m_scale=s[:2]), dict(eight, v_scale=p[:3]), dict(good, copy=p),
+               dict(good, copy=torch.zeros(299, dtype=bf)), dict(good, param=p.half()), dict(good, grad=torch.zeros(600)[::2])):
+        with pytest.raises(ValueError):
+            K.adamw_items([it])
+    for kw in (dict(lr=torch.zeros(2)), dict(lr=1e-3, step=torch.zeros(1)), dict(lr=1e-3, grad_scale=torch.zeros(1, dtype=bf))):
+        with pytest.raises(ValueError):
+            K.kfac_adamw_batched(CTX, K.adamw_items([good]), **kw)
+    for args in ((u, s[:2], p), (u, s, p[:299]), (p, s, p), (u, s, p.half())):
+        with pytest.raises(ValueError):
+            K.kfac_adamw_state_values(CTX, *args)
