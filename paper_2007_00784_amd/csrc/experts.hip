@@ -130,10 +130,11 @@ __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p
 }
 
 // ---- what becomes of a finished sum ----
-__device__ inline unsigned short to_bf16(float x) {   // half to even; NaN stays NaN
-    const unsigned u = __float_as_uint(x);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (unsigned short)((u >> 16) | 0x40u);
-    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+__device__ inline unsigned short to_bf16(float x) {   // half to even
+    const __bf16 b = (__bf16)x;
+    unsigned short u;
+    __builtin_memcpy(&u, &b, 2);
+    return u;
 }
 // Factor weights of an expert: F <- keep F + alpha sum.  With `mean`, an expert without rows keeps its factor as it is.
 struct Average { float alpha, keep; };
@@ -141,6 +142,8 @@ __device__ inline Average average_of(const ExpertArgs &g, int count) {
     if (!g.mean) return Average{(1.f - g.decay) * g.scale, g.decay};
     return Average{(1.f - g.decay) * g.scale / (float)max(count, 1), g.decay};
 }
+
+typedef __bf16 wide_bf16x4 __attribute__((ext_vector_type(4)));
 
 // out(r, c) for one element; r counts the rows of Y / dX (from the matrix' first on) or of an expert's dW / F.
 template <int MODE>
@@ -168,7 +171,7 @@ __device__ inline void finish(const ExpertArgs &g, int e, int r, int c, float v,
 }
 
 // ---- bf16: the wide engine ----
-template <int MODE, int FR, int FC, int WR, int WC>
+template <int MODE, int FR, int FC, int WR, int WC, int RING>
 __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertArgs g) {
     extern __shared__ __align__(16) char smem[];
     constexpr int ROWS = 16 * FR * WR, COLS = 16 * FC * WC, NW = WR * WC;
@@ -193,40 +196,96 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
     else if constexpr (MODE == INPUT_GRAD) col.start((const unsigned short *)g.b + p.e * g.estride, g.ldb, p.n * COLS, g.cols, K);
     else if constexpr (MODE == WEIGHT_GRAD) col.start((const unsigned short *)g.b + p.r.beg * g.ldb, g.ldb, p.n * COLS, g.cols, K);
     else col.start(a, g.lda, p.n * COLS, g.cols, K);
-    wide_tile<Row, Col, FR, FC, WR, WC, ONES>(row, col, K, smem, acc, one, sums);
+    wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES>(row, col, K, smem, acc, one, sums);
 
+    // Each wave turns its 64 columns round in LDS, 32 rows at a time, so that a store covers whole rows of them (128 or 256 bytes side
+    // by side; the accumulators' own layout has 32 or 64).
+    static_assert(FC == 4 && FR % 2 == 0, "64 columns of a wave");
+    constexpr int PITCH = 64 + 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
+    float *const turn = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
     const Average w = MODE == FACTORS ? average_of(g, count) : Average{};
+    const int c0 = p.n * COLS + 64 * wc + 4 * (lane & 15);                      // four places side by side
+    const bool whole = c0 + 4 <= (MODE == FORWARD ? g.cols : g.cols & ~7) && (MODE != FACTORS || p.m * ROWS >= (p.n + 1) * COLS);
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (MODE == FORWARD && g.ones) {
+        const unsigned short *W = (const unsigned short *)g.b + p.e * g.estride + g.K;
 #pragma unroll
-    for (int i = 0; i < FC; ++i) {
-        const int c0 = p.n * COLS + 16 * (wc * FC + i) + 4 * (lane >> 4);       // four places side by side
-        const bool whole = c0 + 4 <= (MODE == FORWARD ? g.cols : g.cols & ~7);
-        float bias[4] = {0.f, 0.f, 0.f, 0.f};
-        if (MODE == FORWARD && g.ones) {
-            const unsigned short *W = (const unsigned short *)g.b + p.e * g.estride + g.K;
+        for (int x = 0; x < 4; ++x) bias[x] = to_float(W[(int64_t)min(c0 + x, g.cols - 1) * g.ldb]);
+    }
+    __syncthreads();
 #pragma unroll
-            for (int x = 0; x < 4; ++x) bias[x] = to_float(W[(int64_t)min(c0 + x, g.cols - 1) * g.ldb]);
-        }
+    for (int part = 0; part < FR / 2; ++part) {
 #pragma unroll
-        for (int j = 0; j < FR; ++j) {
-            const int at = p.m * ROWS + 16 * (wr * FR + j) + (lane & 15);
-            const int r = row.side(at);
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < FC; ++i)
+                *reinterpret_cast<floatx4 *>(turn + (16 * j + (lane & 15)) * PITCH + 16 * i + 4 * (lane >> 4)) = acc[i][2 * part + j];
+        const int r0 = p.m * ROWS + 16 * (wr * FR + 2 * part);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const int at = 4 * t + (lane >> 4), r = row.side(r0 + at);
             if (r < 0 || r >= (RAGGED ? count : g.rows)) continue;
-            if (RAGGED && whole) {
-                const int64_t o = (int64_t)(p.r.beg + r) * g.ldo + c0;
-                unsigned short b4[4];
+            floatx4 v = *reinterpret_cast<const floatx4 *>(turn + at * PITCH + 4 * (lane & 15));
+            if (MODE == FORWARD)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) b4[x] = to_bf16(acc[i][j][x] + bias[x]);
-                __builtin_memcpy((unsigned short *)g.out + o, b4, 8);
-            } else if (MODE == WEIGHT_GRAD && whole && !g.out_bf16 && !g.accumulate) {
-                __builtin_memcpy((float *)g.out + p.e * g.ostride + (int64_t)r * g.ldo + c0, &acc[i][j], 16);
-            } else {
+                for (int x = 0; x < 4; ++x) v[x] += bias[x];
+            if (!whole) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int c = col.side(c0 + x);
                     if (c < 0 || c >= g.cols || (MODE == FACTORS && c > r)) continue;
-                    finish<MODE>(g, p.e, RAGGED ? p.r.beg + r : r, c, acc[i][j][x] + bias[x], w);
+                    finish<MODE>(g, p.e, RAGGED ? p.r.beg + r : r, c, v[x], w);
                 }
+                continue;
+            }
+            const int64_t o = RAGGED ? (int64_t)(p.r.beg + r) * g.ldo + c0 : p.e * g.ostride + (int64_t)r * g.ldo + c0;
+            if (MODE == FACTORS) {
+                float *d = (float *)g.out + o;
+                floatx4 old = {0.f, 0.f, 0.f, 0.f};
+                if (w.keep != 0.f) __builtin_memcpy(&old, d, 16);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = w.keep != 0.f ? fmaf(w.alpha, v[x], w.keep * old[x]) : w.alpha * v[x];
+                __builtin_memcpy(d, &v, 16);
+                *reinterpret_cast<floatx4 *>(turn + at * PITCH + 4 * (lane & 15)) = v;
+            } else if (RAGGED || g.out_bf16) {
+                unsigned short *d = (unsigned short *)g.out + o;
+                if (MODE == WEIGHT_GRAD && g.accumulate) {
+                    unsigned short old[4];
+                    __builtin_memcpy(old, d, 8);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[x] += to_float(old[x]);
+                }
+                const wide_bf16x4 b = __builtin_convertvector(v, wide_bf16x4);   // half to even
+                __builtin_memcpy(d, &b, 8);
+            } else {
+                float *d = (float *)g.out + o;
+                if (MODE == WEIGHT_GRAD && g.accumulate) {
+                    floatx4 old;
+                    __builtin_memcpy(&old, d, 16);
+                    v += old;
+                }
+                __builtin_memcpy(d, &v, 16);
+            }
+        }
+        if (MODE == FACTORS && p.m * ROWS >= (p.n + 1) * COLS) {
+            // the mirrored part: lane l takes rows 4 (l % 8).. of column l / 8, which lie side by side there
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const int place = 8 * t + (lane >> 3), c = col.side(p.n * COLS + 64 * wc + place);
+                if (c < 0 || c >= (g.cols & ~7)) continue;      // (places of a shifted group have stored theirs)
+                floatx4 v;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = turn[(4 * (lane & 7) + x) * PITCH + place];
+                const int first = r0 + 4 * (lane & 7);
+                float *d = (float *)g.out + p.e * g.ostride + (int64_t)c * g.ldo;
+                if (first + 4 <= (g.rows & ~7)) __builtin_memcpy(d + first, &v, 16);
+                else
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int r = row.side(first + x);
+                        if (r >= 0 && r < g.rows) d[r] = v[x];
+                    }
             }
         }
     }
@@ -317,10 +376,10 @@ unsigned grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
     return (unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, (int64_t)1 << 31);
 }
 
-template <int MODE, int FR, int FC, int WR, int WC>
+template <int MODE, int FR, int FC, int WR, int WC, int RING>
 int launch_wide(kfac_ctx *ctx, const ExpertArgs &g) {
-    constexpr int lds = 2 * 16 * (FR * WR + FC * WC) * WK * 2;
-    const auto kernel = expert_wide_kernel<MODE, FR, FC, WR, WC>;
+    constexpr int lds = ((RING + 1) * 16 * FR * WR + RING * 16 * FC * WC) * WK * 2;
+    const auto kernel = expert_wide_kernel<MODE, FR, FC, WR, WC, RING>;
     if (lds > ctx->max_lds) return KFAC_EHIP;
     KFAC_HIP_CHECK(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     hipLaunchKernelGGL(kernel, dim3(grid_of(g, MODE, 16 * FR * WR, 16 * FC * WC)), dim3(64 * WR * WC), lds, ctx->stream, g);
@@ -346,7 +405,7 @@ int launch_mode(kfac_ctx *ctx, const ExpertArgs &g, int dtype) {
     }
     KfacProfScope prof(ctx, dtype == KFAC_BF16 ? KC_EXPERTS_B16 : KC_EXPERTS, flops, bytes);
     const bool wide = dtype == KFAC_BF16 && g.cols >= WIDE_MIN && (ragged ? g.K : g.rows) >= WIDE_MIN;
-    if (wide) return launch_wide<MODE, 8, 4, 2, 4>(ctx, g);
+    if (wide) return launch_wide<MODE, 8, 4, 2, 4, 2>(ctx, g);
     const dim3 grid(grid_of(g, MODE, BM, BM));
     if (dtype == KFAC_BF16) hipLaunchKernelGGL((expert_tile_kernel<MODE, unsigned short>), grid, dim3(NTHREADS), 0, ctx->stream, g);
     else hipLaunchKernelGGL((expert_tile_kernel<MODE, float>), grid, dim3(NTHREADS), 0, ctx->stream, g);

@@ -1,5 +1,5 @@
 // bf16 MFMA tile engine for operands in rows ([rows][d], d contiguous): one workgroup computes C = sum_k R(r, k) Q(c, k) for a
-// tile of ROWS x COLS outputs, K in slabs of 64 through two LDS buffers per operand.  An operand lies in memory in one of two ways:
+// tile of ROWS x COLS outputs, K in slabs of 64 through a ring of LDS buffers for each operand.  An operand lies in memory in one of two ways:
 //   OpAlong   the contraction index is the contiguous one (rows of X against rows of W)
 //   OpAcross  the output index is the contiguous one (columns of W, of G or of X; the contraction walks over rows)
 // Both are moved by 16-byte loads that land in LDS (no registers, no LDS stores), and both end as the same operand registers of
@@ -15,6 +15,7 @@
 // and side() below says which column a place stands for.  So an extent of 8 at least is assumed, and any pitch.  What is outside an
 // operand (rows behind the last, k behind the end) is loaded with an offset that the buffer's range check turns into zeros.
 #pragma once
+#include <type_traits>
 #include "mfma_gemm.h"
 
 namespace kfac {
@@ -23,7 +24,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 wide_bf16x8 __attribute__((ext_vector_type(8)));
 typedef short wide_s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int WK = 64;                      // contraction indices of a slab
+constexpr int WK = 64;                      // contraction indices of a slab: 128 bytes of a row, a whole cache line
 constexpr int WIDE_MIN = 8;                 // smallest extent of any side
 
 __device__ inline const void *uniform_ptr(const void *p) {
@@ -63,29 +64,32 @@ struct OpAlong {
     int K;
     unsigned extent, off[LOADS];
     int g;                        // group of eight k of this thread, the same for its loads
+    unsigned place;               // LDS offset of the wave's first load in a slab
     __device__ void start(const unsigned short *base, int64_t ld_, int i0, int rows, int K_) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         ld = ld_;
         K = K_;
         p = (const unsigned short *)uniform_ptr(base + (int64_t)i0 * ld);
         extent = (unsigned)((int64_t)min(rows - i0, EXT) * ld * 2);
+        place = __builtin_amdgcn_readfirstlane(wave * 1024);
         g = (lane & 7) ^ (lane >> 3);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) off[u] = (unsigned)((wave * 8 + (lane >> 3) + u * 8 * NW) * ld * 2 + g * 16);
     }
     __device__ int over(int k0) const { return min(max(k0 + 8 * g + 8 - K, 0), 8); }    // of the group's eight, how many are behind the end
+    // load u of a slab that ends before K
+    __device__ void issue_inside(unsigned slab, int k0, int u) const { load_to_lds(wide_buffer(p + k0, extent - 2u * k0), off[u], slab + place + u * NW * 1024); }
     __device__ void issue(unsigned slab, int k0) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        slab += place;
         if (k0 + WK <= K) {
-            const auto rs = wide_buffer(p + k0, extent - 2u * k0);
 #pragma unroll
-            for (int u = 0; u < LOADS; ++u) load_to_lds(rs, off[u], slab + (wave * 8 + u * 8 * NW) * (WK * 2));
+            for (int u = 0; u < LOADS; ++u) issue_inside(slab - place, k0, u);
         } else {
             const auto rs = wide_buffer(p, extent);
             const int o = over(k0);
 #pragma unroll
             for (int u = 0; u < LOADS; ++u)
-                load_to_lds(rs, o < 8 ? off[u] + 2u * k0 - 2u * o : BUF_OUTSIDE, slab + (wave * 8 + u * 8 * NW) * (WK * 2));
+                load_to_lds(rs, o < 8 ? off[u] + 2u * k0 - 2u * o : BUF_OUTSIDE, slab + u * NW * 1024);
         }
     }
     // Once the slab's loads have landed: clear what the last, shifted group holds of the one before.
@@ -98,13 +102,13 @@ struct OpAlong {
         for (int w = 0; w < 4; ++w) keep[w] = (2 * w >= o ? 0xffffu : 0u) | (2 * w + 1 >= o ? 0xffff0000u : 0u);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
-            uint4 *x = reinterpret_cast<uint4 *>(slab + (wave * 8 + (lane >> 3) + u * 8 * NW) * (WK * 2) + (lane & 7) * 16);
+            uint4 *x = reinterpret_cast<uint4 *>(slab + (wave + u * NW) * 1024 + lane * 16);
             uint4 v = *x;
             v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
             *x = v;
         }
     }
-    // The registers of output indices i .. i + 15 (i a multiple of 16, in the tile) and k-step ks (32 k each).
+    // The registers of output indices i .. i + 15 (i a multiple of 16, in the tile) and of half `ks` of the slab.
     __device__ static wide_bf16x8 fragment(const char *slab, int i, int ks) {
         const int lane = threadIdx.x & 63;
         wide_bf16x8 x;
@@ -121,7 +125,7 @@ struct OpAcross {
     const unsigned short *p;      // row 0
     int64_t ld;
     int K, n;
-    unsigned off[LOADS];
+    unsigned off[LOADS], place;
     int k_of[MAPPED ? LOADS : 1];
     // 32-byte units of a row of LDS are permuted by k, so that the four rows of a transposing read (and the four eight rows on, which the
     // next sixteen lanes read) lie on different banks
@@ -132,6 +136,7 @@ struct OpAcross {
         K = K_;
         n = n_;
         p = (const unsigned short *)uniform_ptr(base);
+        place = __builtin_amdgcn_readfirstlane(wave * 1024);
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
             const int k = (wave + u * NW) * PER + lane / (EXT / 8), slot = lane % (EXT / 8);
@@ -140,12 +145,14 @@ struct OpAcross {
             if (MAPPED) k_of[u] = k;
         }
     }
+    __device__ void issue_inside(unsigned slab, int k0, int u) const {
+        load_to_lds(wide_buffer(p + (int64_t)k0 * ld, (unsigned)min((int64_t)(K - k0) * ld * 2, (int64_t)BUF_EXTENT)), off[u], slab + place + u * NW * 1024);
+    }
     __device__ void issue(unsigned slab, int k0) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        slab += place;
         if (!MAPPED || k0 + WK <= K) {
-            const auto rs = wide_buffer(p + (int64_t)k0 * ld, (unsigned)min((int64_t)(K - k0) * ld * 2, (int64_t)BUF_EXTENT));
 #pragma unroll
-            for (int u = 0; u < LOADS; ++u) load_to_lds(rs, off[u], slab + (wave + u * NW) * 1024);
+            for (int u = 0; u < LOADS; ++u) issue_inside(slab - place, k0, u);
         } else {
             const int back = min(k0, 8), r = K & 7, k8 = K & ~7;
             const auto rs = wide_buffer(p + (int64_t)(k0 - back) * ld, (unsigned)min((int64_t)(K - k0 + back) * ld * 2, (int64_t)BUF_EXTENT));
@@ -153,7 +160,7 @@ struct OpAcross {
             for (int u = 0; u < LOADS; ++u) {
                 const int k = k0 + k_of[u], shift = k < k8 ? 0 : 8 - r;
                 const bool in = off[u] != BUF_OUTSIDE && (k < k8 || (r != 0 && k < k8 + 8 && k - k8 >= 8 - r));
-                load_to_lds(rs, in ? off[u] + (unsigned)((back - shift) * ld * 2) : BUF_OUTSIDE, slab + (wave + u * NW) * 1024);
+                load_to_lds(rs, in ? off[u] + (unsigned)((back - shift) * ld * 2) : BUF_OUTSIDE, slab + u * NW * 1024);
             }
         }
     }
@@ -175,7 +182,12 @@ struct OpAcross {
 
 // Tile of (16 FR WR) rows x (16 FC WC) columns for WR x WC waves.  acc[i][j]: columns 16 i.., rows 16 j.. of the wave's part.  ONES: with
 // `sums`, one[] of the wave whose column is wc takes the sums over k of row fragments wc FR / WC .. (in every register the same).
-template <class R, class Q, int FR, int FC, int WR, int WC, bool ONES>
+//
+// The row side has RING + 1 buffers, the column side RING: 3 and 2 slabs of 256 places fill the 160 KB of LDS.  A slab is multiplied in two
+// halves.  While one half is multiplied out of registers the next one's registers are read, each as soon as its last use is issued; so all
+// of a slab has been read when its second half begins.  There stands the only barrier of a slab: behind it everybody has the next slab
+// complete, and the loads of the slabs RING and RING + 1 on (columns, rows) go to the buffers that have just been read empty.
+template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES>
 __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
 #pragma unroll
@@ -189,41 +201,80 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, 
     wide_bf16x8 unit;
 #pragma unroll
     for (int e = 0; e < 8; ++e) unit[e] = (__bf16)1.0f;
-    constexpr int STAGE = R::BYTES + Q::BYTES;
-    const unsigned base = lds_address(smem);
+    constexpr int RB = R::BYTES, QB = Q::BYTES;
+    char *const rows = smem, *const cols = smem + (RING + 1) * RB;
+    const unsigned rows_at = lds_address(rows), cols_at = lds_address(cols);
     const int nslab = (K + WK - 1) / WK;
-    row.issue(base, 0);
-    col.issue(base + R::BYTES, 0);
-    for (int s = 0; s < nslab; ++s) {
-        char *cur = smem + (s & 1) * STAGE;
-        const unsigned nxt = base + ((s & 1) ^ 1) * STAGE;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wave's part of slab s has landed
-        if (s + 1 == nslab) {
-            row.patch(cur, s * WK);
-            col.patch(cur + R::BYTES, s * WK);
+    wide_bf16x8 a[2][FC], b[FR];
+    int rb = 0, cb = 0;                                       // buffers of slab s
+    // Multiplies one half (registers `half`) and reads the other one's from (rslab, cslab); at the end of the contraction that is a
+    // buffer nobody has filled, and what is read is not used.
+    auto multiply = [&](auto half_, const char *rslab, const char *cslab, auto between) {
+        constexpr int half = decltype(half_)::value;
+#pragma unroll
+        for (int j = 0; j < FR; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[half][i], b[j], acc[i][j], 0, 0, 0);
+            if (ONES && sums && j / (FR / WC) == wc) one[j % (FR / WC)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unit, b[j], one[j % (FR / WC)], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j < FC) a[half ^ 1][j] = Q::fragment(cslab, 16 * (wc * FC + j), half ^ 1);
+            b[j] = R::fragment(rslab, 16 * (wr * FR + j), half ^ 1);
+            between(j);
         }
-        __syncthreads();                                      // everybody's has, and nobody reads the other buffer any more
-        if (s + 1 < nslab) {
-            row.issue(nxt, (s + 1) * WK);
-            col.issue(nxt + R::BYTES, (s + 1) * WK);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::integral_constant<int, 0> first;
+    constexpr std::integral_constant<int, 1> second;
+    // `inside`: the slabs that are issued exist and end before K
+    auto slab = [&](int s, auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        const int rn = rb == RING ? 0 : rb + 1, cn = cb == RING - 1 ? 0 : cb + 1;
+        multiply(first, rows + rb * RB, cols + cb * QB, [](int) {});
+        if (INSIDE) {                                          // (rows of slab s + RING may still be on their way)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(R::LOADS) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (s + 2 == nslab) {
+                row.patch(rows + rn * RB, (s + 1) * WK);
+                col.patch(cols + cn * QB, (s + 1) * WK);
+            }
+            __syncthreads();
         }
+        // (one load behind each group of matrix instructions: together they would queue up behind one another, and behind those of all the chip)
+        constexpr int TOTAL = Q::LOADS + R::LOADS, EACH = (TOTAL + FR - 1) / FR;
+        const unsigned to_c = cols_at + cb * QB, to_r = rows_at + rb * RB;
+        if (!INSIDE && s + RING < nslab) col.issue(to_c, (s + RING) * WK);
+        if (!INSIDE && s + RING + 1 < nslab) row.issue(to_r, (s + RING + 1) * WK);
+        multiply(second, rows + rn * RB, cols + cn * QB, [&](int j) {
+            if (!INSIDE) return;
 #pragma unroll
-        for (int ks = 0; ks < WK / 32; ++ks) {
-            wide_bf16x8 a[FC], b[FR];
+            for (int x = j * EACH; x < min((j + 1) * EACH, TOTAL); ++x) {
+                if (x < Q::LOADS) col.issue_inside(to_c, (s + RING) * WK, x);
+                else row.issue_inside(to_r, (s + RING + 1) * WK, x - Q::LOADS);
+            }
+        });
+        rb = rn;
+        cb = cn;
+    };
 #pragma unroll
-            for (int i = 0; i < FC; ++i) a[i] = Q::fragment(cur + R::BYTES, 16 * (wc * FC + i), ks);
-#pragma unroll
-            for (int j = 0; j < FR; ++j) b[j] = R::fragment(cur, 16 * (wr * FR + j), ks);
-#pragma unroll
-            for (int j = 0; j < FR; ++j)
-#pragma unroll
-                for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
-            if (ONES && sums)
-#pragma unroll
-                for (int j = 0; j < FR; ++j)
-                    if (j / (FR / WC) == wc) one[j % (FR / WC)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unit, b[j], one[j % (FR / WC)], 0, 0, 0);
-        }
+    for (int s = 0; s <= RING; ++s) {
+        if (s < nslab) row.issue(rows_at + s * RB, s * WK);
+        if (s < RING && s < nslab) col.issue(cols_at + s * QB, s * WK);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (nslab == 1) {
+        row.patch(rows, 0);
+        col.patch(cols, 0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FC; ++i) a[0][i] = Q::fragment(cols, 16 * (wc * FC + i), 0);
+#pragma unroll
+    for (int j = 0; j < FR; ++j) b[j] = R::fragment(rows, 16 * (wr * FR + j), 0);
+    int s = 0;
+    for (; (s + RING + 2) * WK <= K; ++s) slab(s, std::true_type());
+    for (; s < nslab; ++s) slab(s, std::false_type());
 }
 
 }  // namespace kfac
