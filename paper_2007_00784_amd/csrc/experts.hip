@@ -106,14 +106,33 @@ __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
     return false;
 }
 
-// Outputs fixed per expert: mt x nt tiles each (lower triangular ones of mt x mt where `tri`).
+// Outputs fixed per expert: mt x nt tiles each (lower triangular ones of mt x mt where TRI), whose work goes with the expert's rows.  Experts are taken in
+// the order of their rows, the longest first (where one wave can hold them: 64 at most), so that no long one is left for the end; and each RUN
+// consecutive tiles of that order go to the next XCD, so that every XCD has the same share of every expert and the tiles of a run share its L2.
+constexpr int RUN = 8;
 template <bool TRI>
 __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p) {
     const int each = TRI ? mt * (mt + 1) / 2 : mt * nt;
-    const int64_t total = (int64_t)each * g.E, per = (total + 7) / 8, t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int64_t)(blockIdx.x >> 3) >= per || t >= total) return false;
-    p.e = (int)(t / each);
-    const int local = (int)(t - (int64_t)p.e * each);
+    const int64_t i = blockIdx.x >> 3, t = ((i / RUN) * 8 + (blockIdx.x & 7)) * RUN + i % RUN;
+    if (t >= (int64_t)each * g.E) return false;
+    const int place = (int)(t / each);
+    int e = place;
+    if (g.E <= 64) {
+        const int lane = threadIdx.x & 63;
+        int rows = -1;
+        if (lane < g.E) {
+            const Range r = range_of(g, lane);
+            rows = r.end - r.beg;
+        }
+        int rank = 0;       // how many are longer, or as long and in front
+        for (int o = 0; o < g.E; ++o) {
+            const int other = __builtin_amdgcn_readlane(rows, o);
+            rank += other > rows || (other == rows && o < lane) ? 1 : 0;
+        }
+        e = __builtin_ctzll(__ballot(lane < g.E && rank == place));
+    }
+    p.e = e;
+    const int local = (int)(t - (int64_t)place * each);
     if (TRI) {
         int i = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
         while ((i + 1) * (i + 2) / 2 <= local) ++i;
@@ -373,7 +392,8 @@ unsigned grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
         const int64_t mt = (g.rows + ext_r - 1) / ext_r;
         tiles = (mode == FACTORS ? mt * (mt + 1) / 2 : mt * nt) * g.E;
     }
-    return (unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, (int64_t)1 << 31);
+    const int64_t unit = mode == FORWARD || mode == INPUT_GRAD ? 8 : 8 * RUN;
+    return (unsigned)std::min<int64_t>((tiles + unit - 1) / unit * unit, (int64_t)1 << 31);
 }
 
 template <int MODE, int FR, int FC, int WR, int WC, int RING>
