@@ -266,8 +266,9 @@ int kfac_precondition_batched_scaled(kfac_ctx *ctx, int n, const kfac_precond_it
  * DEVICE memory, so what a router wrote there need not come to the host; an expert may have no rows, and rows in front of offsets[0]
  * or behind offsets[experts]-1 belong to nobody.  Offsets are read as if clamped to [0, rows]; where they descend, which
  * expert's result a row gets is undefined, but nothing outside the matrices is touched.
- * The calls allocate nothing, need no workspace, copy nothing from the host and may be captured into a graph, which reads the offsets
- * anew at every replay.  Sample matrices have a row pitch (in elements, at most 2^20) and may start at any element; a bf16 matrix
+ * The calls allocate nothing, copy nothing from the host and may be captured into a graph, which reads the offsets anew at every
+ * replay.  A few large sums over many rows are cut into parts that meet in the context's workspace (kfac_experts_workspace_bytes()); with less of it
+ * there are fewer parts, and with none the sums are whole: slower, never refused.  (So graphs captured from one context must not run at the same time.)  Sample matrices have a row pitch (in elements, at most 2^20) and may start at any element; a bf16 matrix
  * whose rows all start on 16 bytes is read fastest.
  *   append_ones : 1: the weights carry the bias as their last column, as the gradients that kfac_precondition() takes do */
 typedef struct {
@@ -278,6 +279,10 @@ typedef struct {
     int dtype;               /* of X, G, W, Y, dX                                                          */
     const int *offsets;      /* device, [experts + 1]                                                      */
 } kfac_expert_desc;
+
+/* Pure host function: what the four calls below make use of for such a layer, the factors of its inputs and of its output gradients among them
+ * (0: nothing, or an invalid description; offsets is not read).  */
+size_t kfac_experts_workspace_bytes(const kfac_expert_desc *desc /* host */);
 
 /* Y[r] = X[r] W_e^T for every row r of every expert, plus the last column of W_e with append_ones.
  *   X [R][d_in] with pitch ldx;  W [experts][d_out][d_in + append_ones];  Y [R][d_out] with pitch ldy.  Sums in fp32, rounded once.

@@ -170,6 +170,7 @@ int kfac_launch_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *d, co
                                     void *dW, int grad_dtype);
 int kfac_launch_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets, const void *X, int dtype, int64_t ldx, int d, int append_ones,
                                        int mean, float scale, float decay, float *F);
+size_t kfac_experts_ws_bytes_impl(const kfac_expert_desc *d);
 int kfac_launch_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items, const kfac_adamw_opts *opts);
 int kfac_launch_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype);
 int kfac_launch_eig(kfac_ctx *ctx, int batch, const float *const *F, const int *d, float *const *Q,

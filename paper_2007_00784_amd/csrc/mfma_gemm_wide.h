@@ -12,7 +12,7 @@
 //
 // No load leaves its row: a group of eight that runs past the end of a row is taken from the row's last eight elements instead.  Along the
 // contraction the elements that the group before had already are cleared once they have landed; across it, the tile simply has them twice
-// and side() below says which column a place stands for.  So an extent of 8 at least is assumed, and any pitch.  What is outside an
+// and side() says which column a place stands for.  So an extent of 8 at least is assumed, and any pitch.  What is outside an
 // operand (rows behind the last, k behind the end) is loaded with an offset that the buffer's range check turns into zeros.
 #pragma once
 #include <type_traits>
@@ -46,13 +46,14 @@ __device__ inline unsigned lds_address(const void *p) {
     return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
 }
 
-// Which output index the place `at` (from the matrix' first on) of an OpAcross operand with `n` of them stands for, or -1: places n8.. n8 + 7 of
-// a row whose length is n8 + r, 0 < r < 8, hold its last eight, of which the first 8 - r are already there.
+// Which output index the place `at` (from the matrix' first on) of an operand that is read in groups of G along its `n` outputs stands for, or -1: the
+// group of places that begins at n - r, 0 < r < G left over, holds the last G outputs, of which the first G - r are already there.
+template <int G>
 __device__ inline int across_side(int at, int n) {
-    const int n8 = n & ~7, r = n & 7;
-    if (at < n8) return at;
-    if (r == 0 || at >= n8 + 8) return -1;
-    return at - n8 >= 8 - r ? at - (8 - r) : -1;
+    const int r = n % G, last = n - r;
+    if (at < last) return at;
+    if (r == 0 || at >= last + G) return -1;
+    return at - last >= G - r ? at - (G - r) : -1;
 }
 
 // elem(i, k) = p[i * ld + k], i < rows, k < K; K >= 8.  EXT output indices from `i0` on; NW waves.
@@ -177,10 +178,10 @@ struct OpAcross {
         __builtin_memcpy((char *)&x + 8, &hi, 8);
         return x;
     }
-    __device__ int side(int at) const { return across_side(at, n); }
+    __device__ int side(int at) const { return across_side<8>(at, n); }
 };
 
-// Tile of (16 FR WR) rows x (16 FC WC) columns for WR x WC waves.  acc[i][j]: columns 16 i.., rows 16 j.. of the wave's part.  ONES: with
+// Tile of (16 FR WR) rows x (16 FC WC) columns for WR x WC waves, over the slabs s0 .. s1 - 1 of the contraction.  acc[i][j]: columns 16 i.., rows 16 j.. of the wave's part.  ONES: with
 // `sums`, one[] of the wave whose column is wc takes the sums over k of row fragments wc FR / WC .. (in every register the same).
 //
 // The row side has RING + 1 buffers, the column side RING: 3 and 2 slabs of 256 places fill the 160 KB of LDS.  A slab is multiplied in two
@@ -188,7 +189,7 @@ struct OpAcross {
 // of a slab has been read when its second half begins.  There stands the only barrier of a slab: behind it everybody has the next slab
 // complete, and the loads of the slabs RING and RING + 1 on (columns, rows) go to the buffers that have just been read empty.
 template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES>
-__device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums) {
+__device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int s1, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
 #pragma unroll
     for (int i = 0; i < FC; ++i)
@@ -197,14 +198,13 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, 
     if (ONES)
 #pragma unroll
         for (int j = 0; j < FR / WC; ++j) one[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (K <= 0) return;
+    if (s0 >= s1) return;
     wide_bf16x8 unit;
 #pragma unroll
     for (int e = 0; e < 8; ++e) unit[e] = (__bf16)1.0f;
     constexpr int RB = R::BYTES, QB = Q::BYTES;
     char *const rows = smem, *const cols = smem + (RING + 1) * RB;
     const unsigned rows_at = lds_address(rows), cols_at = lds_address(cols);
-    const int nslab = (K + WK - 1) / WK;
     wide_bf16x8 a[2][FC], b[FR];
     int rb = 0, cb = 0;                                       // buffers of slab s
     // Multiplies one half (registers `half`) and reads the other one's from (rslab, cslab); at the end of the contraction that is a
@@ -235,7 +235,7 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, 
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(R::LOADS) : "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            if (s + 2 == nslab) {
+            if (s + 2 == s1) {
                 row.patch(rows + rn * RB, (s + 1) * WK);
                 col.patch(cols + cn * QB, (s + 1) * WK);
             }
@@ -244,8 +244,8 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, 
         // (one load behind each group of matrix instructions: together they would queue up behind one another, and behind those of all the chip)
         constexpr int TOTAL = Q::LOADS + R::LOADS, EACH = (TOTAL + FR - 1) / FR;
         const unsigned to_c = cols_at + cb * QB, to_r = rows_at + rb * RB;
-        if (!INSIDE && s + RING < nslab) col.issue(to_c, (s + RING) * WK);
-        if (!INSIDE && s + RING + 1 < nslab) row.issue(to_r, (s + RING + 1) * WK);
+        if (!INSIDE && s + RING < s1) col.issue(to_c, (s + RING) * WK);
+        if (!INSIDE && s + RING + 1 < s1) row.issue(to_r, (s + RING + 1) * WK);
         multiply(second, rows + rn * RB, cols + cn * QB, [&](int j) {
             if (!INSIDE) return;
 #pragma unroll
@@ -258,23 +258,23 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, char *smem, 
         cb = cn;
     };
 #pragma unroll
-    for (int s = 0; s <= RING; ++s) {
-        if (s < nslab) row.issue(rows_at + s * RB, s * WK);
-        if (s < RING && s < nslab) col.issue(cols_at + s * QB, s * WK);
+    for (int u = 0; u <= RING; ++u) {
+        if (s0 + u < s1) row.issue(rows_at + u * RB, (s0 + u) * WK);
+        if (u < RING && s0 + u < s1) col.issue(cols_at + u * QB, (s0 + u) * WK);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (nslab == 1) {
-        row.patch(rows, 0);
-        col.patch(cols, 0);
+    if (s0 + 1 == s1) {
+        row.patch(rows, s0 * WK);
+        col.patch(cols, s0 * WK);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < FC; ++i) a[0][i] = Q::fragment(cols, 16 * (wc * FC + i), 0);
 #pragma unroll
     for (int j = 0; j < FR; ++j) b[j] = R::fragment(rows, 16 * (wr * FR + j), 0);
-    int s = 0;
-    for (; (s + RING + 2) * WK <= K; ++s) slab(s, std::true_type());
-    for (; s < nslab; ++s) slab(s, std::false_type());
+    int s = s0;
+    for (; s + RING + 2 <= s1 && (s + RING + 2) * WK <= K; ++s) slab(s, std::true_type());
+    for (; s < s1; ++s) slab(s, std::false_type());
 }
 
 }  // namespace kfac

@@ -24,7 +24,7 @@ EXPORTS = (
     "kfac_invert_factors", "kfac_invert_workspace_bytes", "kfac_precondition_inverse",
     "kfac_precondition_inverse_batched", "kfac_precondition_inverse_workspace_bytes",
     "kfac_experts_forward", "kfac_experts_input_grad", "kfac_experts_weight_grad", "kfac_update_factors_experts",
-    "kfac_adamw_batched", "kfac_adamw_state_values",
+    "kfac_experts_workspace_bytes", "kfac_adamw_batched", "kfac_adamw_state_values",
 )
 
 
@@ -135,6 +135,8 @@ def lib():
     L.kfac_precondition_inverse_workspace_bytes.argtypes = [i, ctypes.POINTER(kfac_precond_inv_item)]
     L.kfac_precondition_inverse_workspace_bytes.restype = sz
     dp = ctypes.POINTER(kfac_expert_desc)
+    L.kfac_experts_workspace_bytes.argtypes = [dp]
+    L.kfac_experts_workspace_bytes.restype = sz
     L.kfac_experts_forward.argtypes = [vp, dp, vp, i64, vp, vp, i64]
     L.kfac_experts_input_grad.argtypes = [vp, dp, vp, i64, vp, vp, i64]
     L.kfac_experts_weight_grad.argtypes = [vp, dp, vp, i64, vp, i64, i, vp, i]
@@ -147,7 +149,7 @@ def lib():
         if name not in ("kfac_workspace_bytes", "kfac_eig_workspace_bytes", "kfac_strerror",
                         "kfac_precondition_workspace_bytes", "kfac_update_factors_workspace_bytes",
                         "kfac_unfold_workspace_bytes", "kfac_static_scratch_bytes", "kfac_invert_workspace_bytes",
-                        "kfac_precondition_inverse_workspace_bytes"):
+                        "kfac_precondition_inverse_workspace_bytes", "kfac_experts_workspace_bytes"):
             getattr(L, name).restype = i
     _lib = L
     return L
@@ -420,6 +422,12 @@ def _expert_desc(weight, offsets, rows, append_ones, dtype):
 def _same(a, b, names):
     if a.dtype != b.dtype:
         raise ValueError("%s must have one dtype" % names)
+
+
+def kfac_experts_workspace_bytes(experts, rows, d_in, d_out, append_ones=False, dtype=KFAC_BF16):
+    """Bytes of workspace that the products and factors of such a layer make use of (they work with less)."""
+    d = kfac_expert_desc(int(experts), int(rows), int(d_in), int(d_out), int(bool(append_ones)), int(dtype), None)
+    return int(lib().kfac_experts_workspace_bytes(ctypes.byref(d)))
 
 
 def kfac_experts_forward(ctx, X, W, offsets, Y, append_ones=False):

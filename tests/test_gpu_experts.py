@@ -301,3 +301,104 @@ def test_no_rows(ctx):
     assert bool((F == 1).all())
     K.kfac_update_factors_experts(ctx.h, X, off, F, decay=0.5, mean=False)
     assert bool((F == 0.5).all())
+
+
+# ---- every engine that a call can take, whole and in parts ----
+FORWARD, INPUT_GRAD, WEIGHT_GRAD, FACTORS = range(4)
+FEW, SOME, SMALL, WIDE, WIDE_SMALL, TILES = range(6)
+# mode, counts, d_in, d_out, ones, bf16, engine, parts
+ENGINES = [
+    (FORWARD, [3, 0, 5], 265, 130, 1, True, FEW, False),
+    (FORWARD, [300, 200], 75, 523, 1, True, SOME, False),
+    (FORWARD, [9000, 1, 2999], 18, 1101, 1, True, WIDE, False),
+    (FORWARD, [100] * 39 + [77], 301, 1100, 0, True, WIDE_SMALL, False),
+    (INPUT_GRAD, [150] * 20 + [0] + [163] * 19, 1001, 27, 0, True, WIDE, False),
+    (INPUT_GRAD, [200, 3, 97], 301, 130, 1, True, WIDE_SMALL, False),
+    (INPUT_GRAD, [170, 130], 70, 1607, 1, True, WIDE_SMALL, True),
+    (WEIGHT_GRAD, [100] * 20 + [0] + [101] * 19, 1003, 133, 1, True, WIDE, False),
+    (WEIGHT_GRAD, [50, 40], 300, 140, 1, True, WIDE_SMALL, False),
+    (WEIGHT_GRAD, [4100, 0, 60, 130], 75, 131, 1, True, WIDE_SMALL, True),
+    (FACTORS, [1500] * 8, 1601, 1, 1, True, WIDE, False),
+    (FACTORS, [50, 40], 300, 1, 1, True, WIDE_SMALL, False),
+    (FACTORS, [6100, 160], 203, 1, 1, True, WIDE_SMALL, True),
+    (FORWARD, [40, 21], 75, 133, 1, False, SMALL, False),
+    (FORWARD, [12000], 16, 130, 1, False, TILES, False),
+    (FORWARD, [2205], 1001, 1103, 1, False, TILES, True),
+    (INPUT_GRAD, [40, 21], 75, 133, 1, False, SMALL, False),
+    (INPUT_GRAD, [2200], 1603, 29, 1, False, TILES, False),
+    (INPUT_GRAD, [2205], 1103, 1001, 1, False, TILES, True),
+    (WEIGHT_GRAD, [40, 21], 75, 133, 1, False, SMALL, False),
+    (WEIGHT_GRAD, [4] * 40, 1601, 101, 1, False, TILES, False),
+    (WEIGHT_GRAD, [6600], 75, 133, 1, False, TILES, True),
+    (FACTORS, [40, 21], 135, 1, 1, False, SMALL, False),
+    (FACTORS, [4, 3, 5], 603, 1, 1, False, TILES, False),
+    (FACTORS, [9900, 700], 255, 1, 1, False, TILES, True),
+]
+
+
+def plan_of(mode, L, workspace):
+    import ctypes
+    f = K.lib().kfac_experts_plan
+    f.argtypes = [ctypes.c_int, ctypes.POINTER(K.kfac_expert_desc), ctypes.c_size_t]
+    d = K.kfac_expert_desc(L.E, L.R, L.d_in, L.d_out, L.ones, K.KFAC_BF16 if L.bf16 else K.KFAC_F32, 4096)
+    p = f(mode, ctypes.byref(d), workspace)
+    return p // 100, p % 100
+
+
+def near_gpu(got, want, mags, terms, bf16):
+    bound = (terms + 2) * 2.0 ** -23 * mags + (2.0 ** -8 if bf16 else 2.0 ** -23) * want.abs() + 1e-37
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+@pytest.mark.parametrize("case", range(len(ENGINES)))
+def test_engines(ctx, case):
+    mode, counts, d_in, d_out, ones, bf16, engine, parts = ENGINES[case]
+    L = Layer(counts, d_in, d_out, ones, bf16, behind=3, seed=case)
+    room = K.kfac_experts_workspace_bytes(L.E, L.R, d_in, d_out, ones, K.KFAC_BF16 if bf16 else K.KFAC_F32)
+    assert room <= ctx.ws.numel()
+    got_engine, got_parts = plan_of(mode, L, room)
+    assert (got_engine, got_parts > 1) == (engine, parts) and plan_of(mode, L, ctx.ws.numel()) == (got_engine, got_parts)
+    bare = K.kfac_create(0, ctx.stream.cuda_stream, None)
+    for h in (ctx.h, bare):
+        X, Xh, _ = L.samples(d_in)
+        G, Gh, _ = L.samples(d_out)
+        Xd, Gd, W = X.double(), G.double(), L.Wd.double()
+        if mode in (FORWARD, INPUT_GRAD):
+            out, _, buf = L.samples(d_out if mode == FORWARD else d_in, fill=7.0)
+            if mode == FORWARD:
+                K.kfac_experts_forward(h, X, L.Wd, L.offsets, out, append_ones=ones)
+            else:
+                K.kfac_experts_input_grad(h, G, L.Wd, L.offsets, out, append_ones=ones)
+            for e, a, b in L.parts():
+                w = W[e, :, :d_in].contiguous()
+                if mode == FORWARD:
+                    bias = W[e, :, d_in] if ones else torch.zeros(d_out, dtype=torch.float64, device=L.dev)
+                    wt = w.t().contiguous()
+                    near_gpu(out[a:b], Xd[a:b] @ wt + bias, Xd[a:b].abs() @ wt.abs() + bias.abs(), d_in + 1, bf16)
+                else:
+                    near_gpu(out[a:b], Gd[a:b] @ w, Gd[a:b].abs() @ w.abs(), d_out, bf16)
+            out[:L.off[-1]] = 7.0
+            assert bool((buf == 7.0).all())
+        else:
+            rows = G if mode == WEIGHT_GRAD else X
+            D = d_in + ones
+            out = torch.full((L.E, d_out if mode == WEIGHT_GRAD else D, D), 1.0, device=L.dev)
+            if mode == WEIGHT_GRAD:
+                K.kfac_experts_weight_grad(h, G, X, L.offsets, out, append_ones=ones, accumulate=True)
+            else:
+                K.kfac_update_factors_experts(h, X, L.offsets, out, append_ones=ones, scale=0.5, decay=0.25)
+            for e in range(L.E):
+                a, b = L.off[e], L.off[e + 1]
+                x = torch.cat([Xd[a:b], torch.ones(b - a, 1, dtype=torch.float64, device=L.dev)], 1) if ones else Xd[a:b]
+                r = (Gd[a:b] if mode == WEIGHT_GRAD else x).t().contiguous()
+                if mode == WEIGHT_GRAD:
+                    near_gpu(out[e], 1.0 + r @ x, 1.0 + r.abs() @ x.abs(), b - a + 2, False)
+                elif b > a:
+                    c = 0.75 * 0.5 / (b - a)
+                    near_gpu(out[e], 0.25 + c * (r @ x), 0.25 + c * (r.abs() @ x.abs()), b - a + 4, False)
+                    assert torch.equal(out[e], out[e].t())
+                else:
+                    assert bool((out[e] == 1).all())
+    torch.cuda.synchronize()
+    K.kfac_destroy(bare)

@@ -126,3 +126,20 @@ def test_tensors_that_do_not_fit():
     for args in ((u, s[:2], p), (u, s, p[:299]), (p, s, p), (u, s, p.half())):
         with pytest.raises(ValueError):
             K.kfac_adamw_state_values(CTX, *args)
+
+
+def test_workspace_of_experts():
+    """What is asked for suffices for the plan, less of it means fewer parts, and an invalid description asks for nothing."""
+    f = K.lib().kfac_experts_plan
+    f.argtypes = [ctypes.c_int, ctypes.POINTER(K.kfac_expert_desc), ctypes.c_size_t]
+    for dtype in (K.KFAC_F32, K.KFAC_BF16):
+        for shape in ((1, 32768, 512, 512), (2, 6000, 75, 133), (1, 300, 70, 1607), (64, 4096, 2048, 1000), (3, 1, 8, 8), (1, (1 << 30) - 1, 64, 64), (4096, 0, 65536, 65536)):
+            for ones in (0, 1):
+                need = K.kfac_experts_workspace_bytes(*shape, ones, dtype)
+                assert need % 256 == 0 and need < 1 << 31
+                for mode in range(4):
+                    d = ctypes.byref(K.kfac_expert_desc(*shape, ones, dtype, None))
+                    full, some, none = f(mode, d, 1 << 60), f(mode, d, need // 3), f(mode, d, 0)
+                    assert f(mode, d, need) == full
+                    assert none % 100 == 1 and (some // 100 != full // 100 or some % 100 <= full % 100)
+    assert K.kfac_experts_workspace_bytes(0, 100, 64, 64) == 0 and K.kfac_experts_workspace_bytes(1, -1, 64, 64) == 0
