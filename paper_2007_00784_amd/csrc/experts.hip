@@ -175,6 +175,12 @@ __device__ inline Average average_of(const ExpertArgs &g, int count) {
 
 typedef __bf16 wide_bf16x4 __attribute__((ext_vector_type(4)));
 
+// A vector into memory at any element.  Results are not read again before the L2 has long been through other things; they go past it.
+template <typename V, int ALIGN> __device__ inline void store_past(void *p, const V &v) {
+    typedef V Anywhere __attribute__((aligned(ALIGN)));
+    __builtin_nontemporal_store(v, reinterpret_cast<Anywhere *>(p));
+}
+
 // out(r, c) for one element; r counts the rows of Y / dX (from the matrix' first on) or of an expert's dW / F.
 template <int MODE>
 __device__ inline void finish(const ExpertArgs &g, int e, int r, int c, float v, const Average &w) {
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
                 if (w.keep != 0.f) __builtin_memcpy(&old, d, 16);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) v[x] = w.keep != 0.f ? fmaf(w.alpha, v[x], w.keep * old[x]) : w.alpha * v[x];
-                __builtin_memcpy(d, &v, 16);
+                store_past<floatx4, 4>(d, v);
                 *reinterpret_cast<floatx4 *>(turn + at * PITCH + 4 * (lane & 15)) = v;
             } else if (RAGGED || g.out_bf16) {
                 unsigned short *d = (unsigned short *)g.out + o;
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
                     for (int x = 0; x < 4; ++x) v[x] += to_float(old[x]);
                 }
                 const wide_bf16x4 b = __builtin_convertvector(v, wide_bf16x4);   // half to even
-                __builtin_memcpy(d, &b, 8);
+                store_past<wide_bf16x4, 2>(d, b);
             } else {
                 float *d = (float *)g.out + o;
                 if (MODE == WEIGHT_GRAD && g.accumulate) {
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
                     __builtin_memcpy(&old, d, 16);
                     v += old;
                 }
-                __builtin_memcpy(d, &v, 16);
+                store_past<floatx4, 4>(d, v);
             }
         }
         if (MODE == FACTORS && p.m * ROWS >= (p.n + 1) * COLS) {
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
                 for (int x = 0; x < 4; ++x) v[x] = turn[(4 * (lane & 7) + x) * PITCH + place];
                 const int first = r0 + 4 * (lane & 7);
                 float *d = (float *)g.out + p.e * g.ostride + (int64_t)c * g.ldo;
-                if (first + 4 <= (g.rows & ~7)) __builtin_memcpy(d + first, &v, 16);
+                if (first + 4 <= (g.rows & ~7)) store_past<floatx4, 4>(d + first, v);
                 else
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
