@@ -64,37 +64,32 @@ constexpr int BAND = 4;
 template <int EXT>
 __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
     const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int e0 = 0; e0 < g.E; e0 += 64) {
+    Range r{0, 0};          // of expert e0 + lane
+    int mt = 0, incl = 0;   // its row tiles; those of the experts from e0 on, up to it
+    auto look = [&](int e0) {
         const int e = e0 + lane;
-        int mt = 0;
+        mt = 0;
         if (e < g.E) {
-            const Range r = range_of(g, e);
+            r = range_of(g, e);
             mt = (r.end - r.beg + EXT - 1) / EXT;
         }
+        incl = mt;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) mt += __shfl_xor(mt, d);
-        total += __builtin_amdgcn_readfirstlane(mt);
-    }
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(incl, d);
+            if (lane >= d) incl += o;
+        }
+        return __builtin_amdgcn_readlane(incl, 63);
+    };
+    int64_t total = 0;
+    for (int e0 = 0; e0 < g.E; e0 += 64) total += look(e0);
     total *= nt;
     const int64_t per = (total + 7) / 8, t = (int64_t)((blockIdx.x + blockIdx.y) & 7) * per + (blockIdx.x >> 3);
     if ((int64_t)(blockIdx.x >> 3) >= per || t >= total) return false;
     p.t = t;
     int64_t before = 0;
     for (int e0 = 0; e0 < g.E; e0 += 64) {
-        const int e = e0 + lane;
-        Range r{0, 0};
-        int mt = 0;
-        if (e < g.E) {
-            r = range_of(g, e);
-            mt = (r.end - r.beg + EXT - 1) / EXT;
-        }
-        int incl = mt;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(incl, d);
-            if (lane >= d) incl += o;
-        }
+        if (g.E > 64) look(e0);
         const int64_t last = before + (int64_t)incl * nt;
         const uint64_t past = __ballot(last > t);
         if (past) {
@@ -119,9 +114,10 @@ __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
 // L2.  (Runs of 4, 8, 16 and 32: weight gradient of 32 experts 2048 x 2048 over 32768 rows 357, 355, 359, 379 us, factors of 16 experts 283, 282, 295,
 // 352; with few tiles the runs are shorter, so that all XCDs have some.)
 __host__ __device__ inline int run_of(int64_t tiles) { return tiles >= 512 ? 8 : tiles >= 64 ? (int)(tiles / 64) : 1; }
+__host__ __device__ inline int tiles_each(bool tri, int mt, int nt) { return tri ? mt * (mt + 1) / 2 : mt * nt; }
 template <bool TRI>
 __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p) {
-    const int each = TRI ? mt * (mt + 1) / 2 : mt * nt;
+    const int each = tiles_each(TRI, mt, nt);
     const int run = run_of((int64_t)each * g.E);
     const int64_t i = blockIdx.x >> 3, t = ((i / run) * 8 + ((blockIdx.x + blockIdx.y) & 7)) * run + i % run;
     if (t >= (int64_t)each * g.E) return false;
@@ -131,8 +127,9 @@ __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p
     if (g.E <= 64) {
         const int lane = threadIdx.x & 63;
         int rows = -1;
+        Range r{0, 0};
         if (lane < g.E) {
-            const Range r = range_of(g, lane);
+            r = range_of(g, lane);
             rows = r.end - r.beg;
         }
         int rank = 0;       // how many are longer, or as long and in front
@@ -141,6 +138,9 @@ __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p
             rank += other > rows || (other == rows && o < lane) ? 1 : 0;
         }
         e = __builtin_ctzll(__ballot(lane < g.E && rank == place));
+        p.r = Range{__builtin_amdgcn_readlane(r.beg, e), __builtin_amdgcn_readlane(r.end, e)};
+    } else {
+        p.r = range_of(g, e);
     }
     p.e = e;
     const int local = (int)(t - (int64_t)place * each);
@@ -155,7 +155,6 @@ __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p
         p.n = in / high;
         p.m = band * BAND + (in - p.n * high);
     }
-    p.r = range_of(g, p.e);
     return true;
 }
 
@@ -210,7 +209,7 @@ __device__ inline void finish(const ExpertArgs &g, int e, int r, int c, float v,
 template <int FR, int FC, int WR, int WC> constexpr int wide_part() { return (FC * FR + FR / WC) * 64 * WR * WC * 4; }   // floats of one part
 
 template <int MODE, int FR, int FC, int WR, int WC, int RING, int PHASE>
-__global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertArgs g) {
+__global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const ExpertArgs g) {
     extern __shared__ __align__(16) char smem[];
     constexpr int ROWS = 16 * FR * WR, COLS = 16 * FC * WC, NW = WR * WC;
     constexpr bool RAGGED = MODE == FORWARD || MODE == INPUT_GRAD, ONES = !RAGGED;
@@ -284,7 +283,7 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
     float *const turn = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
     const Average w = MODE == FACTORS ? average_of(g, count) : Average{};
     const int c0 = p.n * COLS + 64 * wc + 4 * (lane & 15);                      // four places side by side
-    const bool whole = c0 + 4 <= (MODE == FORWARD ? g.cols : g.cols & ~7) && (MODE != FACTORS || p.m * ROWS >= (p.n + 1) * COLS);
+    const bool whole = c0 + 4 <= (MODE == FORWARD ? g.cols : g.cols & ~7);
     float bias[4] = {0.f, 0.f, 0.f, 0.f};
     if (MODE == FORWARD && g.ones) {
         const unsigned short *W = (const unsigned short *)g.b + p.e * g.estride + g.K;
@@ -320,11 +319,17 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
             const int64_t o = RAGGED ? (int64_t)(p.r.beg + r) * g.ldo + c0 : p.e * g.ostride + (int64_t)r * g.ldo + c0;
             if (MODE == FACTORS) {
                 float *d = (float *)g.out + o;
-                floatx4 old = {0.f, 0.f, 0.f, 0.f};
-                if (w.keep != 0.f) __builtin_memcpy(&old, d, 16);
+                if (c0 + 3 <= r) {
+                    floatx4 old = {0.f, 0.f, 0.f, 0.f};
+                    if (w.keep != 0.f) __builtin_memcpy(&old, d, 16);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] = w.keep != 0.f ? fmaf(w.alpha, v[x], w.keep * old[x]) : w.alpha * v[x];
-                store_past<floatx4, 4>(d, v);
+                    for (int x = 0; x < 4; ++x) v[x] = w.keep != 0.f ? fmaf(w.alpha, v[x], w.keep * old[x]) : w.alpha * v[x];
+                    store_past<floatx4, 4>(d, v);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (c0 + x <= r) d[x] = v[x] = w.keep != 0.f ? fmaf(w.alpha, v[x], w.keep * d[x]) : w.alpha * v[x];
+                }
                 *reinterpret_cast<floatx4 *>(turn + at * PITCH + 4 * (lane & 15)) = v;
             } else if (RAGGED || g.out_bf16) {
                 unsigned short *d = (unsigned short *)g.out + o;
@@ -346,23 +351,23 @@ __global__ __launch_bounds__(64 * WR * WC) void expert_wide_kernel(const ExpertA
                 store_past<floatx4, 4>(d, v);
             }
         }
-        if (MODE == FACTORS && p.m * ROWS >= (p.n + 1) * COLS) {
+        if (MODE == FACTORS) {
             // the mirrored part: lane l takes rows 4 (l % 8).. of column l / 8, which lie side by side there
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
-                const int place = 8 * t + (lane >> 3), c = col.side(p.n * COLS + 64 * wc + place);
-                if (c < 0 || c >= (g.cols & ~7)) continue;      // (places of a shifted group have stored theirs)
+                const int place = 8 * t + (lane >> 3), c = p.n * COLS + 64 * wc + place;
+                if (c >= (g.cols & ~7)) continue;      // (places of a shifted group have stored theirs)
                 floatx4 v;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) v[x] = turn[(4 * (lane & 7) + x) * PITCH + place];
                 const int first = r0 + 4 * (lane & 7);
                 float *d = (float *)g.out + p.e * g.ostride + (int64_t)c * g.ldo;
-                if (first + 4 <= (g.rows & ~7)) store_past<floatx4, 4>(d + first, v);
+                if (first + 4 <= (g.rows & ~7) && first > c) store_past<floatx4, 4>(d + first, v);
                 else
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int r = row.side(first + x);
-                        if (r >= 0 && r < g.rows) d[r] = v[x];
+                        if (r > c && r < g.rows) d[r] = v[x];
                     }
             }
         }
@@ -709,7 +714,7 @@ unsigned grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
     if (mode == FORWARD || mode == INPUT_GRAD) tiles = ((int64_t)g.R / ext_r + std::min<int64_t>(g.E, g.R)) * nt;
     else {
         const int64_t mt = (g.rows + ext_r - 1) / ext_r;
-        tiles = (mode == FACTORS ? mt * (mt + 1) / 2 : mt * nt) * g.E;
+        tiles = (int64_t)tiles_each(mode == FACTORS, (int)mt, (int)nt) * g.E;
     }
     const int64_t unit = mode == FORWARD || mode == INPUT_GRAD ? 8 : 8 * run_of(tiles);
     return (unsigned)std::min<int64_t>((tiles + unit - 1) / unit * unit, (int64_t)1 << 31);

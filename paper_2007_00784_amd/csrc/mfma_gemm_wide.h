@@ -262,7 +262,8 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
         if (s0 + u < s1) row.issue(rows_at + u * RB, (s0 + u) * WK);
         if (u < RING && s0 + u < s1) col.issue(cols_at + u * QB, (s0 + u) * WK);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (s0 + RING < s1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RING * R::LOADS + (RING - 1) * Q::LOADS) : "memory");   // the first slab
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (s0 + 1 == s1) {
         row.patch(rows, s0 * WK);
         col.patch(cols, s0 * WK);
