@@ -272,7 +272,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
         for (int j = 0; j < FR / WC; ++j) q[(FC * FR + j) * THREADS] = ONES ? one[j] : floatx4{0.f, 0.f, 0.f, 0.f};
         return;
     } else {
-        wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES>(row, col, K, 0, nslab, smem, acc, one, sums);
+        if (RAGGED && count - p.m * ROWS <= ROWS - 16) wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES, RAGGED>(row, col, K, 0, nslab, smem, acc, one, sums, count - p.m * ROWS);
+        else wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES>(row, col, K, 0, nslab, smem, acc, one, sums);
     }
 
     // Each wave turns its 64 columns round in LDS, 32 rows at a time, so that a store covers whole rows of them (128 or 256 bytes side

@@ -188,9 +188,12 @@ struct OpAcross {
 // halves.  While one half is multiplied out of registers the next one's registers are read, each as soon as its last use is issued; so all
 // of a slab has been read when its second half begins.  There stands the only barrier of a slab: behind it everybody has the next slab
 // complete, and the loads of the slabs RING and RING + 1 on (columns, rows) go to the buffers that have just been read empty.
-template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES>
-__device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int s1, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums) {
+// SHORT: of a tile whose rows end inside it, only the fragments with some of its `height` rows are multiplied (the others' accumulators stay zero).
+template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES, bool SHORT = false>
+__device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int s1, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums,
+                                 int height = 0) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
+    const int mine = __builtin_amdgcn_readfirstlane((height + 15) / 16 - wr * FR);      // row fragments of this wave
 #pragma unroll
     for (int i = 0; i < FC; ++i)
 #pragma unroll
@@ -214,8 +217,9 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
 #pragma unroll
         for (int j = 0; j < FR; ++j) {
             __builtin_amdgcn_sched_barrier(0);
+            if (!SHORT || j < mine)
 #pragma unroll
-            for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[half][i], b[j], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[half][i], b[j], acc[i][j], 0, 0, 0);
             if (ONES && sums && j / (FR / WC) == wc) one[j % (FR / WC)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unit, b[j], one[j % (FR / WC)], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             if (j < FC) a[half ^ 1][j] = Q::fragment(cslab, 16 * (wc * FC + j), half ^ 1);
