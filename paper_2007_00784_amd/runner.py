@@ -171,3 +171,79 @@ class KfacRunner:
             w["ema_bytes"] += 8.0 * (l.d_a ** 2 + l.d_g ** 2)
             w["sum_d3"] += float(l.d_a) ** 3 + float(l.d_g) ** 3
         return w
+
+
+class ExpertRunner:
+    """A layer of experts through a training step with the preconditioner: products, both gradients, every expert's factors, their
+    eigendecompositions, the preconditioned gradient and the optimizer step that writes the weights which the next products read.
+
+    The rows of x and g are sorted by expert, offsets (int32 [experts + 1], on the GPU) say where each one's begin.  Parameters are kept in fp32 with their
+    bias as last column; bf16 layers multiply with a bf16 copy of them that the optimizer step writes.
+    """
+
+    def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0"):
+        self.dev = torch.device(device)
+        self.experts, self.rows, self.d_in, self.d_out, self.bias, self.damping = experts, rows, d_in, d_out, bool(bias), damping
+        self.dt = torch.bfloat16 if bf16 else torch.float32
+        dA = d_in + int(self.bias)
+        f32 = dict(dtype=torch.float32, device=self.dev)
+        self.param = torch.zeros((experts, d_out, dA), **f32)
+        self.weight = torch.zeros_like(self.param, dtype=self.dt) if bf16 else self.param
+        self.grad = torch.zeros_like(self.param)
+        self.y = torch.zeros((rows, d_out), dtype=self.dt, device=self.dev)
+        self.dx = torch.zeros((rows, d_in), dtype=self.dt, device=self.dev)
+        self.A, self.G = torch.zeros((experts, dA, dA), **f32), torch.zeros((experts, d_out, d_out), **f32)
+        self.QA, self.QG = torch.zeros_like(self.A), torch.zeros_like(self.G)
+        self.lamA, self.lamG = torch.zeros((experts, dA), **f32), torch.zeros((experts, d_out), **f32)
+        n = self.param.numel()
+        if state_bits == 8:
+            state = {k: torch.zeros(n, dtype=torch.uint8, device=self.dev) for k in ("m", "v")}
+            state.update({k: torch.zeros((n + 127) // 128, dtype=torch.uint8, device=self.dev) for k in ("m_scale", "v_scale")})
+        else:
+            state = {k: torch.zeros(n, **f32) for k in ("m", "v")}
+        self.state = state
+        self.steps = 0
+        dims = [dA] * experts + [d_out] * experts
+        need = max(K.kfac_eig_workspace_bytes(dims), K.kfac_precondition_workspace_bytes([(dA, d_out)] * experts),
+                   K.kfac_experts_workspace_bytes(experts, rows, d_in, d_out, self.bias, K.KFAC_BF16 if bf16 else K.KFAC_F32))
+        self.ws = torch.empty(need + 4096, dtype=torch.uint8, device=self.dev)
+        self.stream = torch.cuda.current_stream(self.dev)
+        self.ctx = K.kfac_create(self.dev.index or 0, self.stream.cuda_stream, self.ws)
+        self._adamw = K.adamw_items([dict(param=self.param, grad=self.grad, **state, **(dict(copy=self.weight) if bf16 else {}))])
+        self._precond = K.precond_items(list(self.QA), list(self.lamA), list(self.QG), list(self.lamG), damping, list(self.grad))
+
+    def close(self):
+        torch.cuda.synchronize()
+        if self.ctx is not None:
+            K.kfac_destroy(self.ctx)
+            self.ctx = None
+
+    def load(self, param):
+        """The parameters [experts, d_out, d_in + bias], and the weights that the products read."""
+        self.param.copy_(param)
+        if self.weight is not self.param:
+            self.weight.copy_(self.param)
+
+    def forward(self, x, offsets):
+        K.kfac_experts_forward(self.ctx, x, self.weight, offsets, self.y, append_ones=self.bias)
+        return self.y
+
+    def backward(self, x, g, offsets, accumulate=False):
+        """The input's gradient (returned) and every expert's (self.grad) from the output's."""
+        K.kfac_experts_input_grad(self.ctx, g, self.weight, offsets, self.dx, append_ones=self.bias)
+        K.kfac_experts_weight_grad(self.ctx, g, x, offsets, self.grad, append_ones=self.bias, accumulate=accumulate)
+        return self.dx
+
+    def update_factors(self, x, g, offsets, decay):
+        K.kfac_update_factors_experts(self.ctx, x, offsets, self.A, append_ones=self.bias, decay=decay)
+        K.kfac_update_factors_experts(self.ctx, g, offsets, self.G, decay=decay)
+
+    def eig(self, **kw):
+        return K.kfac_eig(self.ctx, list(self.A) + list(self.G), list(self.QA) + list(self.QG), list(self.lamA) + list(self.lamG), **kw)
+
+    def precondition(self):
+        K.kfac_precondition_batched(self.ctx, items=self._precond)
+
+    def step(self, lr, grad_scale=None, **hyper):
+        self.steps += 1
+        K.kfac_adamw_batched(self.ctx, self._adamw, lr=lr, step=self.steps, grad_scale=grad_scale, **hyper)
