@@ -487,24 +487,33 @@ def adamw_items(items):
     reusable while the buffers live.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or uint8), m_scale, v_scale uint8, one for
     each 128 elements.  copy: bfloat16, takes the updated parameter."""
     import torch
+    code = {torch.float32: KFAC_F32, torch.bfloat16: KFAC_BF16}
     arr = (kfac_adamw_item * len(items))()
-    for j, it in enumerate(items):
-        p, g, m, v, ms, vs, copy = (it.get(k) for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy"))
+    for d, it in zip(arr, items):
+        p, g, m, v = it["param"], it["grad"], it["m"], it["v"]
+        ms, vs, copy = it.get("m_scale"), it.get("v_scale"), it.get("copy")
         n = p.numel()
         if g.numel() != n or m.numel() != n or v.numel() != n or (copy is not None and copy.numel() != n):
-            raise ValueError("item %d: buffers of different lengths" % j)
+            raise ValueError("buffers of different lengths")
         if (ms is None) != (vs is None):
-            raise ValueError("item %d: both scales or none" % j)
+            raise ValueError("both scales or none")
         if ms is None:
             if m.dtype != torch.float32 or v.dtype != torch.float32:
-                raise ValueError("item %d: m and v must be float32 (or come with scales)" % j)
+                raise ValueError("m and v must be float32 (or come with scales)")
         else:
             blocks = (n + 127) // 128
             if m.element_size() != 1 or v.element_size() != 1 or any(s.dtype != torch.uint8 or s.numel() != blocks for s in (ms, vs)):
-                raise ValueError("item %d: m and v must have a byte for each element, the scales (uint8) one for each 128" % j)
-        if copy is not None and copy.dtype != torch.bfloat16:
-            raise ValueError("item %d: copy must be bfloat16" % j)
-        arr[j] = kfac_adamw_item(_ptr(p), _dtype_code(p), _ptr(g), _dtype_code(g), _ptr(m), _ptr(v), _ptr(ms), _ptr(vs), _ptr(copy), n)
+                raise ValueError("m and v must have a byte for each element, the scales (uint8) one for each 128")
+            d.m_scale, d.v_scale = _ptr(ms), _ptr(vs)
+        if copy is not None:
+            if copy.dtype != torch.bfloat16:
+                raise ValueError("copy must be bfloat16")
+            d.copy = _ptr(copy)
+        try:
+            d.param_dtype, d.grad_dtype = code[p.dtype], code[g.dtype]
+        except KeyError:
+            raise ValueError("parameters and gradients must be float32 or bfloat16") from None
+        d.param, d.grad, d.m, d.v, d.n = _ptr(p), _ptr(g), _ptr(m), _ptr(v), n
     return arr
 
 
