@@ -239,6 +239,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
     else if constexpr (MODE == WEIGHT_GRAD) col.start((const unsigned short *)g.b + p.r.beg * g.ldb, g.ldb, p.n * COLS, g.cols, K);
     else col.start(a, g.lda, p.n * COLS, g.cols, K);
     constexpr int THREADS = 64 * WR * WC;
+    constexpr bool AHEAD = RAGGED && NW == 8;
     const int nslab = (K + WK - 1) / WK;
     floatx4 *const part = reinterpret_cast<floatx4 *>(g.part + p.t * g.splits * wide_part<FR, FC, WR, WC>()) + threadIdx.x;
     constexpr int PART4 = wide_part<FR, FC, WR, WC>() / 4;
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
             for (int j = 0; j < FR / WC; ++j) one[j] = joined(FC * FR + j);
     } else if constexpr (PHASE == PART) {
         const int per = (nslab + g.splits - 1) / g.splits, s0 = min((int)blockIdx.y * per, nslab), s1 = min(s0 + per, nslab);
-        wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES>(row, col, K, s0, s1, smem, acc, one, sums);
+        wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES, AHEAD>(row, col, K, s0, s1, smem, acc, one, sums);
         floatx4 *const q = part + (int64_t)blockIdx.y * PART4;
 #pragma unroll
         for (int i = 0; i < FC; ++i)
@@ -277,8 +278,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
         for (int j = 0; j < FR / WC; ++j) q[(FC * FR + j) * THREADS] = ONES ? one[j] : floatx4{0.f, 0.f, 0.f, 0.f};
         return;
     } else {
-        if (RAGGED && count - p.m * ROWS <= ROWS - 16) wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES, RAGGED>(row, col, K, 0, nslab, smem, acc, one, sums, count - p.m * ROWS);
-        else wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES>(row, col, K, 0, nslab, smem, acc, one, sums);
+        if (RAGGED && count - p.m * ROWS <= ROWS - 16) wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES, AHEAD, RAGGED>(row, col, K, 0, nslab, smem, acc, one, sums, count - p.m * ROWS);
+        else wide_tile<Row, Col, FR, FC, WR, WC, RING, ONES, AHEAD>(row, col, K, 0, nslab, smem, acc, one, sums);
     }
 
     // Each wave turns its 64 columns round in LDS, 32 rows at a time, so that a store covers whole rows of them (128 or 256 bytes side

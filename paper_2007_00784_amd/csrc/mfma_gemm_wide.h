@@ -187,9 +187,12 @@ struct OpAcross {
 // The row side has RING + 1 buffers, the column side RING: 3 and 2 slabs of 256 places fill the 160 KB of LDS.  A slab is multiplied in two
 // halves.  While one half is multiplied out of registers the next one's registers are read, each as soon as its last use is issued; so all
 // of a slab has been read when its second half begins.  There stands the only barrier of a slab: behind it everybody has the next slab
-// complete, and the loads of the slabs RING and RING + 1 on (columns, rows) go to the buffers that have just been read empty.
+// complete.  Columns of slab s + RING are loaded during the second half of slab s, rows of it during the first, a load behind one
+// group of matrix instructions and the next (together they would queue up behind one another, and behind those of all the chip).  AHEAD: rows half a
+// slab earlier, during the second half of the slab before: where experts' rows differ and many tiles have few, 4096 x 4096 forward 892 us instead
+// of 916, input gradients 291 instead of 300; without, weight gradients 320 instead of 324.
 // SHORT: of a tile whose rows end inside it, only the fragments with some of its `height` rows are multiplied (the others' accumulators stay zero).
-template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES, bool SHORT = false>
+template <class R, class Q, int FR, int FC, int WR, int WC, int RING, bool ONES, bool AHEAD, bool SHORT = false>
 __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int s1, char *smem, floatx4 (&acc)[FC][FR], floatx4 (&one)[FR / WC], bool sums,
                                  int height = 0) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / WC, wc = wave % WC;
@@ -234,7 +237,14 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
     auto slab = [&](int s, auto inside) {
         constexpr bool INSIDE = decltype(inside)::value;
         const int rn = rb == RING ? 0 : rb + 1, cn = cb == RING - 1 ? 0 : cb + 1;
-        multiply(first, rows + rb * RB, cols + cb * QB, [](int) {});
+        const int rp = rb == 0 ? RING : rb - 1;                // what slab s - 1 was in
+        const unsigned to_c = cols_at + cb * QB, to_r = rows_at + (AHEAD ? rb : rp) * RB;
+        if (!INSIDE && !AHEAD && s + RING < s1) row.issue(to_r, (s + RING) * WK);
+        multiply(first, rows + rb * RB, cols + cb * QB, [&](int j) {
+            if (INSIDE && !AHEAD)
+#pragma unroll
+                for (int x = j * R::LOADS / FR; x < (j + 1) * R::LOADS / FR; ++x) row.issue_inside(to_r, (s + RING) * WK, x);
+        });
         if (INSIDE) {                                          // (rows of slab s + RING may still be on their way)
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(R::LOADS) : "memory");
         } else {
@@ -245,15 +255,13 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
             }
             __syncthreads();
         }
-        // (one load behind each group of matrix instructions: together they would queue up behind one another, and behind those of all the chip)
-        constexpr int TOTAL = Q::LOADS + R::LOADS, EACH = (TOTAL + FR - 1) / FR;
-        const unsigned to_c = cols_at + cb * QB, to_r = rows_at + rb * RB;
         if (!INSIDE && s + RING < s1) col.issue(to_c, (s + RING) * WK);
-        if (!INSIDE && s + RING + 1 < s1) row.issue(to_r, (s + RING + 1) * WK);
+        if (!INSIDE && AHEAD && s + RING + 1 < s1) row.issue(to_r, (s + RING + 1) * WK);
         multiply(second, rows + rn * RB, cols + cn * QB, [&](int j) {
             if (!INSIDE) return;
+            constexpr int TOTAL = Q::LOADS + (AHEAD ? R::LOADS : 0);
 #pragma unroll
-            for (int x = j * EACH; x < min((j + 1) * EACH, TOTAL); ++x) {
+            for (int x = j * TOTAL / FR; x < (j + 1) * TOTAL / FR; ++x) {
                 if (x < Q::LOADS) col.issue_inside(to_c, (s + RING) * WK, x);
                 else row.issue_inside(to_r, (s + RING + 1) * WK, x - Q::LOADS);
             }
@@ -262,11 +270,13 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
         cb = cn;
     };
 #pragma unroll
-    for (int u = 0; u <= RING; ++u) {
-        if (s0 + u < s1) row.issue(rows_at + u * RB, (s0 + u) * WK);
-        if (u < RING && s0 + u < s1) col.issue(cols_at + u * QB, (s0 + u) * WK);
-    }
-    if (s0 + RING < s1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RING * R::LOADS + (RING - 1) * Q::LOADS) : "memory");   // the first slab
+    for (int u = 0; u < RING; ++u)
+        if (s0 + u < s1) {
+            row.issue(rows_at + u * RB, (s0 + u) * WK);
+            col.issue(cols_at + u * QB, (s0 + u) * WK);
+        }
+    if (AHEAD && s0 + RING < s1) row.issue(rows_at + RING * RB, (s0 + RING) * WK);
+    if (s0 + RING + AHEAD <= s1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * (R::LOADS + Q::LOADS) + AHEAD * R::LOADS) : "memory");   // the first slab
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (s0 + 1 == s1) {
         row.patch(rows, s0 * WK);
@@ -278,7 +288,8 @@ __device__ inline void wide_tile(const R &row, const Q &col, int K, int s0, int 
 #pragma unroll
     for (int j = 0; j < FR; ++j) b[j] = R::fragment(rows, 16 * (wr * FR + j), 0);
     int s = s0;
-    for (; s + RING + 2 <= s1 && (s + RING + 2) * WK <= K; ++s) slab(s, std::true_type());
+    constexpr int TOUCHED = RING + 1 + AHEAD;      // slabs of a step
+    for (; s + TOUCHED <= s1 && (s + TOUCHED) * WK <= K; ++s) slab(s, std::true_type());
     for (; s < s1; ++s) slab(s, std::false_type());
 }
 
