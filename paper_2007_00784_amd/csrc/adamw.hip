@@ -335,7 +335,7 @@ int kfac_launch_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items
     a.step_dev = o->step_dev;
     // a tensor longer than 32-bit offsets and grids reach goes in pieces (a multiple of CHUNK each)
     constexpr int64_t PIECE = (int64_t)1 << 31;
-    constexpr unsigned MOST_WGS = 1u << 30;
+    constexpr unsigned MOST_WGS = 1u << 23;
     int64_t all = 0;
     for (int i = 0; i < n; ++i) all += std::min(items[i].n, SHORT_LIST);
     const bool small = all < SHORT_LIST;

@@ -83,7 +83,7 @@ __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
     };
     int64_t total = 0;
     for (int e0 = 0; e0 < g.E; e0 += 64) total += look(e0);
-    total *= nt;
+    total = min(total * nt, (int64_t)gridDim.x);     // (descending offsets could ask for more tiles than there are workgroups, and places for their parts)
     const int64_t per = (total + 7) / 8, t = (int64_t)((blockIdx.x + blockIdx.y) & 7) * per + (blockIdx.x >> 3);
     if ((int64_t)(blockIdx.x >> 3) >= per || t >= total) return false;
     p.t = t;
@@ -715,7 +715,7 @@ __global__ __launch_bounds__(NTHREADS) __attribute__((amdgpu_waves_per_eu(2))) v
 }
 
 // ---- launches ----
-unsigned grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
+int64_t grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
     const int64_t nt = (g.cols + ext_c - 1) / ext_c;
     int64_t tiles;
     if (mode == FORWARD || mode == INPUT_GRAD) tiles = ((int64_t)g.R / ext_r + std::min<int64_t>(g.E, g.R)) * nt;
@@ -724,10 +724,12 @@ unsigned grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
         tiles = (int64_t)tiles_each(mode == FACTORS, (int)mt, (int)nt) * g.E;
     }
     const int64_t unit = mode == FORWARD || mode == INPUT_GRAD ? 8 : 8 * run_of(tiles);
-    return (unsigned)std::min<int64_t>((tiles + unit - 1) / unit * unit, (int64_t)1 << 31);
+    return (tiles + unit - 1) / unit * unit;
 }
 
-template <typename F> int launch_one(kfac_ctx *ctx, F kernel, dim3 grid, int threads, int lds, const ExpertArgs &g) {
+template <typename F> int launch_one(kfac_ctx *ctx, F kernel, int64_t tiles, int parts, int threads, int lds, const ExpertArgs &g) {
+    if (tiles * threads >= (int64_t)1 << 32) return KFAC_EINVAL;     // more than a launch can have (no such layer fits the memory)
+    const dim3 grid((unsigned)tiles, (unsigned)parts);
     if (lds > ctx->max_lds) return KFAC_EHIP;
     if (lds > 65536) KFAC_HIP_CHECK(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, g);
@@ -738,35 +740,33 @@ template <typename F> int launch_one(kfac_ctx *ctx, F kernel, dim3 grid, int thr
 template <int MODE, int FR, int FC, int WR, int WC, int RING, bool SPLIT>
 int launch_wide(kfac_ctx *ctx, ExpertArgs g, int splits) {
     constexpr int lds = ((RING + 1) * 16 * FR * WR + RING * 16 * FC * WC) * WK * 2, threads = 64 * WR * WC;
-    const unsigned tiles = grid_of(g, MODE, 16 * FR * WR, 16 * FC * WC);
+    const int64_t tiles = grid_of(g, MODE, 16 * FR * WR, 16 * FC * WC);
     if constexpr (SPLIT) {
         if (splits > 1) {
             g.splits = splits;
             g.part = (float *)ctx->ws;
-            KFAC_CHECK(launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, PART>, dim3(tiles, splits), threads, lds, g));
-            return launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, JOIN>, dim3(tiles, FR / 2), threads, threads / 64 * 32 * 68 * 4, g);
+            KFAC_CHECK(launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, PART>, tiles, splits, threads, lds, g));
+            return launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, JOIN>, tiles, FR / 2, threads, threads / 64 * 32 * 68 * 4, g);
         }
     }
-    return launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, WHOLE>, dim3(tiles), threads, lds, g);
+    return launch_one(ctx, expert_wide_kernel<MODE, FR, FC, WR, WC, RING, WHOLE>, tiles, 1, threads, lds, g);
 }
 
 template <int MODE, typename E, int RT, int CT, int WAVES, int DEPTH>
 int launch_direct(kfac_ctx *ctx, const ExpertArgs &g) {
-    return launch_one(ctx, expert_direct_kernel<MODE, E, RT, CT, WAVES, DEPTH>, dim3(grid_of(g, MODE, 16 * RT, 16 * CT)), 64 * WAVES, WAVES * direct_part<RT, CT>() * 4, g);
+    return launch_one(ctx, expert_direct_kernel<MODE, E, RT, CT, WAVES, DEPTH>, grid_of(g, MODE, 16 * RT, 16 * CT), 1, 64 * WAVES, WAVES * direct_part<RT, CT>() * 4, g);
 }
 
-template <int MODE, typename E, bool SPLIT>
+template <int MODE, typename E>
 int launch_tiles(kfac_ctx *ctx, ExpertArgs g, int splits) {
-    const unsigned tiles = grid_of(g, MODE, BM, BM);
-    if constexpr (SPLIT) {
-        if (splits > 1) {
-            g.splits = splits;
-            g.part = (float *)ctx->ws;
-            KFAC_CHECK(launch_one(ctx, expert_tile_kernel<MODE, E, PART>, dim3(tiles, splits), NTHREADS, 0, g));
-            return launch_one(ctx, expert_tile_kernel<MODE, E, JOIN>, dim3(tiles, 4), NTHREADS, 0, g);
-        }
+    const int64_t tiles = grid_of(g, MODE, BM, BM);
+    if (splits > 1) {
+        g.splits = splits;
+        g.part = (float *)ctx->ws;
+        KFAC_CHECK(launch_one(ctx, expert_tile_kernel<MODE, E, PART>, tiles, splits, NTHREADS, 0, g));
+        return launch_one(ctx, expert_tile_kernel<MODE, E, JOIN>, tiles, 4, NTHREADS, 0, g);
     }
-    return launch_one(ctx, expert_tile_kernel<MODE, E, WHOLE>, dim3(tiles), NTHREADS, 0, g);
+    return launch_one(ctx, expert_tile_kernel<MODE, E, WHOLE>, tiles, 1, NTHREADS, 0, g);
 }
 
 // ---- which kernel a call takes ----
@@ -806,8 +806,7 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
             offer(e, s, 3.0 + run + (s > 1 ? 5.0 + 2.0 * (double)part_bytes * t * s / 2.5e6 + 0.3 * s : 0.0));
         }
     };
-    if (dtype == KFAC_BF16) {
-        if (shortest < WIDE_MIN) return best;
+    if (dtype == KFAC_BF16 && shortest >= WIDE_MIN) {
         if (mode == FORWARD) {
             // the weights are streamed past 16 or 32 rows at a time; us: 8 experts of 2048 x 2048 with 8 rows each 14.5, 15.2 and (WIDE_SMALL) 27.5,
             // with 32 25.8, 16.8 and 27.6; 64 of 1024 x 2048 with 16 each 73.8, 66.2 and 70.0, with 64 each 192, 112 and 74.9
@@ -824,7 +823,7 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     }
     // us: input gradient 577 x 512 of 8 experts over 1568 rows 24.4 and (TILES) 53; weight gradient 1001 x 512 of 10 over 1000 37 and 30;
     // 1024 x 1024 forward over 4096 rows 138 and 100
-    if (shortest >= 4) offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(1.0, tiles(32, 32) / 256.0) * K * 0.0085));
+    if (dtype == KFAC_F32 && shortest >= 4) offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(1.0, tiles(32, 32) / 256.0) * K * 0.0085));
     offer_split(TILES, tiles(128, 128), 768, K / BK, 1.36, 3.6, 3.0, 1.0, TILE_PART * 4, grid_of(g, mode, BM, BM));
     return best;
 }
@@ -859,8 +858,7 @@ int launch_mode(kfac_ctx *ctx, const ExpertArgs &g, int dtype) {
         case WIDE_SMALL: return launch_wide<MODE, 4, 4, 2, 2, 2, true>(ctx, g, plan.splits);
         case TILES: break;
     }
-    if (dtype == KFAC_BF16) return launch_tiles<MODE, unsigned short, false>(ctx, g, 1);
-    return launch_tiles<MODE, float, true>(ctx, g, plan.splits);
+    return dtype == KFAC_BF16 ? launch_tiles<MODE, unsigned short>(ctx, g, plan.splits) : launch_tiles<MODE, float>(ctx, g, plan.splits);
 }
 
 }  // namespace

@@ -389,6 +389,13 @@ def kfac_precondition_workspace_bytes(dims):
 
 
 # ---- layers of experts ----
+def _on_gpu(*tensors):
+    """The last thing that is looked at: a host address would be read by a kernel."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+
+
 def _rows(t, name, d):
     """(address, row pitch) of a matrix of samples [R][d]: any pitch, but the elements of a row side by side."""
     if t.dim() != 2 or t.shape[1] != d:
@@ -407,7 +414,9 @@ def _offsets(t, experts):
     import torch
     if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != experts + 1:
         raise ValueError("offsets must be int32 [experts + 1]")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError("offsets must be contiguous")
+    return t
 
 
 def _expert_desc(weight, offsets, rows, append_ones, dtype):
@@ -416,7 +425,9 @@ def _expert_desc(weight, offsets, rows, append_ones, dtype):
     ones = int(bool(append_ones))
     if wide - ones < 1:
         raise ValueError("weights without inputs")
-    return kfac_expert_desc(experts, rows, wide - ones, d_out, ones, dtype, _offsets(offsets, experts))
+    _ptr(weight)                                 # contiguous
+    _offsets(offsets, experts)
+    return kfac_expert_desc(experts, rows, wide - ones, d_out, ones, dtype, offsets.data_ptr())
 
 
 def _same(a, b, names):
@@ -440,6 +451,7 @@ def kfac_experts_forward(ctx, X, W, offsets, Y, append_ones=False):
         raise ValueError("X and Y must have as many rows")
     xp, ldx = _rows(X, "X", desc.d_in)
     yp, ldy = _rows(Y, "Y", desc.d_out)
+    _on_gpu(X, W, offsets, Y)
     _check(lib().kfac_experts_forward(ctx, ctypes.byref(desc), xp, ldx, _ptr(W), yp, ldy), "kfac_experts_forward")
 
 
@@ -452,6 +464,7 @@ def kfac_experts_input_grad(ctx, G, W, offsets, dX, append_ones=False):
         raise ValueError("G and dX must have as many rows")
     gp, ldg = _rows(G, "G", desc.d_out)
     xp, ldx = _rows(dX, "dX", desc.d_in)
+    _on_gpu(G, W, offsets, dX)
     _check(lib().kfac_experts_input_grad(ctx, ctypes.byref(desc), gp, ldg, _ptr(W), xp, ldx), "kfac_experts_input_grad")
 
 
@@ -464,7 +477,9 @@ def kfac_experts_weight_grad(ctx, G, X, offsets, dW, append_ones=False, accumula
         raise ValueError("G and X must have as many rows")
     gp, ldg = _rows(G, "G", desc.d_out)
     xp, ldx = _rows(X, "X", desc.d_in)
-    _check(lib().kfac_experts_weight_grad(ctx, ctypes.byref(desc), gp, ldg, xp, ldx, int(bool(accumulate)), _ptr(dW), _dtype_code(dW)),
+    code = _dtype_code(dW)
+    _on_gpu(G, X, offsets, dW)
+    _check(lib().kfac_experts_weight_grad(ctx, ctypes.byref(desc), gp, ldg, xp, ldx, int(bool(accumulate)), _ptr(dW), code),
            "kfac_experts_weight_grad")
 
 
@@ -477,7 +492,10 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
         raise ValueError("F must be float32 [experts, D, D], D = d + append_ones")
     experts, d = F.shape[0], X.shape[1]
     xp, ldx = _rows(X, "X", d)
-    _check(lib().kfac_update_factors_experts(ctx, experts, X.shape[0], _offsets(offsets, experts), xp, _dtype_code(X), ldx, d, ones,
+    _offsets(offsets, experts)
+    _ptr(F)                                      # contiguous
+    _on_gpu(X, offsets, F)
+    _check(lib().kfac_update_factors_experts(ctx, experts, X.shape[0], offsets.data_ptr(), xp, _dtype_code(X), ldx, d, ones,
                                              int(bool(mean)), float(scale), float(decay), _ptr(F)), "kfac_update_factors_experts")
 
 
@@ -514,6 +532,7 @@ def adamw_items(items):
         except KeyError:
             raise ValueError("parameters and gradients must be float32 or bfloat16") from None
         d.param, d.grad, d.m, d.v, d.n = _ptr(p), _ptr(g), _ptr(m), _ptr(v), n
+        _on_gpu(p, g, m, v, ms, vs, copy)
     return arr
 
 
@@ -522,6 +541,7 @@ def _scalar(t, dtype, name):
         return None
     if t.dtype != dtype or t.numel() != 1:
         raise ValueError("%s must be one %s" % (name, dtype))
+    _on_gpu(t)
     return _ptr(t)
 
 
@@ -543,7 +563,9 @@ def kfac_adamw_state_values(ctx, codes, scale, out):
     n = codes.numel()
     if codes.element_size() != 1 or out.numel() != n or scale.dtype != torch.uint8 or scale.numel() != (n + 127) // 128:
         raise ValueError("codes: a byte for each element of out, scale: uint8, one for each 128")
-    _check(lib().kfac_adamw_state_values(ctx, _ptr(codes), _ptr(scale), n, _ptr(out), _dtype_code(out)), "kfac_adamw_state_values")
+    code = _dtype_code(out)
+    _on_gpu(codes, scale, out)
+    _check(lib().kfac_adamw_state_values(ctx, _ptr(codes), _ptr(scale), n, _ptr(out), code), "kfac_adamw_state_values")
 
 
 def kfac_schedule_due(k, f_fac, f_eig):

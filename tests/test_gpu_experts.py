@@ -402,3 +402,90 @@ def test_engines(ctx, case):
                     assert bool((out[e] == 1).all())
     torch.cuda.synchronize()
     K.kfac_destroy(bare)
+
+
+def test_descending_offsets_with_parts(ctx):
+    """Descending offsets name more rows than there are, and more tiles than the workspace was sized for: nothing outside is touched, and the next
+    call is as it should be."""
+    L = Layer([170, 130], 70, 1607, 1, True)
+    assert plan_of(INPUT_GRAD, L, ctx.ws.numel())[1] > 1
+    G, Gh, _ = L.samples(1607)
+    dX, _, buf = L.samples(70, fill=7.0)
+    room = K.kfac_experts_workspace_bytes(2, 300, 70, 1607, 1, K.KFAC_BF16)
+    ws = torch.full((room + (32 << 20),), 0x5a, dtype=torch.uint8, device=L.dev)
+    h = K.kfac_create(0, ctx.stream.cuda_stream, ws, room)
+    for off in ([0, 300, 0], [300, 0, 300], [0, 2 ** 31 - 1, -5]):
+        K.kfac_experts_input_grad(h, G, L.Wd, torch.tensor(off, dtype=torch.int32, device=L.dev), dX, append_ones=True)
+    torch.cuda.synchronize()
+    assert bool((ws[room:] == 0x5a).all())
+    K.kfac_experts_input_grad(h, G, L.Wd, L.offsets, dX, append_ones=True)
+    for e, a, b in L.parts():
+        w = L.W[e, :, :70].double()
+        near(dX[a:b], Gh[a:b] @ w, Gh[a:b].abs() @ w.abs(), 1607, True)
+    torch.cuda.synchronize()
+    K.kfac_destroy(h)
+
+
+def test_a_short_side_over_many_rows(ctx):
+    """bf16 with a side below the sixteen bytes of a group, over so many rows that the sum goes in parts."""
+    for d_in, d_out in ((5, 40), (40, 3)):
+        L = Layer([9000], d_in, d_out, 1, True)
+        assert plan_of(WEIGHT_GRAD, L, ctx.ws.numel()) [0] == TILES and plan_of(WEIGHT_GRAD, L, ctx.ws.numel())[1] > 1
+        X, Xh, _ = L.samples(d_in)
+        G, Gh, _ = L.samples(d_out)
+        dW = torch.zeros((1, d_out, d_in + 1), device=L.dev)
+        K.kfac_experts_weight_grad(ctx.h, G, X, L.offsets, dW, append_ones=True)
+        x = torch.cat([Xh, torch.ones(9000, 1, dtype=torch.float64)], 1)
+        near(dW[0], Gh.T @ x, Gh.abs().T @ x.abs(), 9000, False)
+
+
+def test_another_stream_than_the_callers(ctx):
+    """A context on a stream of its own, with work on it before and behind the calls; two contexts side by side."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    L = Layer([300, 0, 200], 130, 264, 1, True)
+    X, Xh, _ = L.samples(130)
+    hs = [K.kfac_create(0, s.cuda_stream, torch.empty(8 << 20, dtype=torch.uint8, device=L.dev)) for s in streams]
+    outs = []
+    torch.cuda.synchronize()
+    for s, h in zip(streams, hs):
+        with torch.cuda.stream(s):
+            x = torch.zeros_like(X)
+            big = torch.randn(2000, 2000, device=L.dev)
+            for _ in range(4):
+                big = big @ big / 2000
+            x.copy_(X)
+            y = torch.zeros((L.R, 264), dtype=L.dt, device=L.dev)
+            K.kfac_experts_forward(h, x, L.Wd, L.offsets, y, append_ones=True)
+            outs.append(y.clone())
+    torch.cuda.synchronize()
+    for e, a, b in L.parts():
+        w = L.W[e].double()
+        near(outs[0][a:b], Xh[a:b] @ w[:, :130].T + w[:, 130], Xh[a:b].abs() @ w[:, :130].abs().T + w[:, 130].abs(), 131, True)
+    assert torch.equal(outs[0], outs[1])
+    for h in hs:
+        K.kfac_destroy(h)
+
+
+def test_more_experts_than_a_wave(ctx):
+    """300 experts, most of them without rows: prefix sums over several waves' worth of offsets."""
+    counts = [(i * 7919) % 11 if i % 3 == 0 else 0 for i in range(300)]
+    for bf16 in (True, False):
+        L = Layer(counts, 40, 24, 1, bf16)
+        X, Xh, _ = L.samples(40)
+        G, Gh, _ = L.samples(24)
+        Y, _, _ = L.samples(24, fill=0.0)
+        dW = torch.full((300, 24, 41), float("nan"), device=L.dev)
+        F = torch.ones((300, 41, 41), device=L.dev)
+        K.kfac_experts_forward(ctx.h, X, L.Wd, L.offsets, Y, append_ones=True)
+        K.kfac_experts_weight_grad(ctx.h, G, X, L.offsets, dW, append_ones=True)
+        K.kfac_update_factors_experts(ctx.h, X, L.offsets, F, append_ones=True)
+        for e in range(300):
+            a, b = L.off[e], L.off[e + 1]
+            if a == b:
+                assert bool((dW[e] == 0).all()) and bool((F[e] == 1).all())
+                continue
+            x = torch.cat([Xh[a:b], torch.ones(b - a, 1, dtype=torch.float64)], 1)
+            w = L.W[e].double()
+            near(Y[a:b], x @ w.T, x.abs() @ w.abs().T, 41, bf16)
+            near(dW[e], Gh[a:b].T @ x, Gh[a:b].abs().T @ x.abs(), b - a, False)
+            near(F[e], x.T @ x / (b - a), x.abs().T @ x.abs() / (b - a), b - a + 4, False)
