@@ -58,8 +58,8 @@ __device__ inline Range range_of(const ExpertArgs &g, int e) {
 struct Place { int e, m, n; Range r; int64_t t; };       // t: its number, for its parts in the workspace
 
 // Rows ragged: expert e has ceil(rows / EXT) row tiles times `nt` column tiles.  The tiles of all experts, in order, are dealt to the eight XCDs
-// in equal consecutive parts (workgroup b runs on XCD b % 8; the parts of a split contraction go round them), so that tiles that share operands share an L2; inside an expert the
-// order goes over BAND row tiles before it takes the next column tile.
+// in equal consecutive parts (workgroup b runs on XCD b % 8; the parts of a split contraction go round them), so that tiles that share
+// operands share an L2; inside an expert the order goes over BAND row tiles before it takes the next column tile.
 constexpr int BAND = 4;
 template <int EXT>
 __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
@@ -108,11 +108,11 @@ __device__ inline bool place_ragged(const ExpertArgs &g, int nt, Place &p) {
     return false;
 }
 
-// Outputs fixed per expert: mt x nt tiles each (lower triangular ones of mt x mt where TRI), whose work goes with the expert's rows.  Experts are taken in
-// the order of their rows, the longest first (where one wave can hold them: 64 at most), so that no long one is left for the end; and each run of
-// consecutive tiles of that order goes to the next XCD, so that every XCD has the same share of every expert and the tiles of a run share its
-// L2.  (Runs of 4, 8, 16 and 32: weight gradient of 32 experts 2048 x 2048 over 32768 rows 357, 355, 359, 379 us, factors of 16 experts 283, 282, 295,
-// 352; with few tiles the runs are shorter, so that all XCDs have some.)
+// Outputs fixed per expert: mt x nt tiles each (lower triangular ones of mt x mt where TRI), whose work goes with the expert's rows.
+// Experts are taken in the order of their rows, the longest first (where one wave can hold them: 64 at most), so that no long one is left
+// for the end; and each run of consecutive tiles of that order goes to the next XCD, so that every XCD has the same share of every expert
+// and the tiles of a run share its L2.  (Runs of 4, 8, 16 and 32: weight gradient of 32 experts 2048 x 2048 over 32768 rows 357, 355, 359,
+// 379 us, factors of 16 experts 283, 282, 295, 352; with few tiles the runs are shorter, so that all XCDs have some.)
 __host__ __device__ inline int run_of(int64_t tiles) { return tiles >= 512 ? 8 : tiles >= 64 ? (int)(tiles / 64) : 1; }
 __host__ __device__ inline int tiles_each(bool tri, int mt, int nt) { return tri ? mt * (mt + 1) / 2 : mt * nt; }
 template <bool TRI>
@@ -132,8 +132,8 @@ __device__ inline bool place_fixed(const ExpertArgs &g, int mt, int nt, Place &p
             r = range_of(g, lane);
             rows = r.end - r.beg;
         }
-        // the row count in that place, bit by bit from the top: the largest that more than `place` experts reach; then the expert among its equals
-        // (comparing all with all took 2.7 us a workgroup)
+        // the row count in that place, bit by bit from the top: the largest that more than `place` experts reach; then the expert among its
+        // equals (comparing all with all took 2.7 us a workgroup)
         int rows_at = 0;
         for (int bit = 31 - __builtin_clz(max(g.R, 1)); bit >= 0; --bit) {
             const int tried = rows_at | 1 << bit;
@@ -211,6 +211,10 @@ __device__ inline void finish(const ExpertArgs &g, int e, int r, int c, float v,
 }
 
 // ---- bf16: the wide engine ----
+//
+// Bound by the matrix core and LDS together where the sums are long (see mfma_gemm_wide.h), by what is written where they are short: 32
+// weight gradients 2048 x 2048 over 32768 rows 322 us, of which 111 are the 537 MB of results at 4.8 TB/s; 16 factors 2049 wide over 32768
+// rows 258 us, 137 of them with one slab of rows.
 template <int FR, int FC, int WR, int WC> constexpr int wide_part() { return (FC * FR + FR / WC) * 64 * WR * WC * 4; }   // floats of one part
 
 template <int MODE, int FR, int FC, int WR, int WC, int RING, int PHASE>
@@ -393,13 +397,15 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
 
 // ---- few rows (bf16 forward), small layers (fp32): operands straight from memory to the matrix core's registers ----
 //
-// A workgroup's waves share one tile of (16 RT) x (16 CT) outputs and take turns along the contraction, STEP indices each; their sums are added in
-// a fixed order through LDS.  Nothing is staged: each lane loads 16 bytes that are its own operands of several matrix instructions, DEPTH steps
-// of them in flight, so that a tile with a handful of rows streams its weights at the memory's rate, and many small tiles fill the chip.
+// A workgroup's waves share one tile of (16 RT) x (16 CT) outputs and take turns along the contraction, STEP indices each; their sums are
+// added in a fixed order through LDS.  Nothing is staged: each lane loads what are its own operands of one or several matrix instructions,
+// DEPTH steps of them in flight, so that a tile with a handful of rows streams its weights at the memory's rate, and many small tiles fill
+// the chip.  (8 experts of 2048 x 2048 with a row each: 13.3 us, 59 MB at 4.4 TB/s, a copy runs at 4.9.  fp32 tiles of 32 x 32 have 8
+// operations a byte of L2 traffic, which bounds them.)
 //
-// An operand along the contraction (X, G; W forward): lane l holds index 16 f + l % 16 of fragment f at k = V (l / 16).., V = 16 / sizeof(E) (one
-// v_mfma_f32_16x16x32_bf16, or four v_mfma_f32_16x16x4_f32 of which number t takes element t).  An operand across it (fp32): one row of V = 4
-// consecutive outputs for each t, so that lane l holds index 4 (l % 16) + f of fragment f = 0 .. 3.
+// An operand along the contraction (X, G; W forward): lane l holds index 16 f + l % 16 of fragment f at k = V (l / 16).., V = 16 /
+// sizeof(E) (one v_mfma_f32_16x16x32_bf16, or four v_mfma_f32_16x16x4_f32 of which number t takes element t).  An operand across it (fp32):
+// F consecutive outputs of one row for each t, so that lane l holds index F (l % 16) + f of fragment f.
 template <typename E> struct DirectTraits;
 template <> struct DirectTraits<unsigned short> {
     static constexpr int V = 8, STEP = 32;
@@ -727,8 +733,10 @@ int64_t grid_of(const ExpertArgs &g, int mode, int ext_r, int ext_c) {
     return (tiles + unit - 1) / unit * unit;
 }
 
+bool fits_launch(int64_t tiles, int threads) { return tiles * threads < (int64_t)1 << 32; }     // what a launch can have
+
 template <typename F> int launch_one(kfac_ctx *ctx, F kernel, int64_t tiles, int parts, int threads, int lds, const ExpertArgs &g) {
-    if (tiles * threads >= (int64_t)1 << 32) return KFAC_EINVAL;     // more than a launch can have (no such layer fits the memory)
+    if (!fits_launch(tiles, threads)) return KFAC_EINVAL;     // (not in the largest tiles either: no such layer fits the memory)
     const dim3 grid((unsigned)tiles, (unsigned)parts);
     if (lds > ctx->max_lds) return KFAC_EHIP;
     if (lds > 65536) KFAC_HIP_CHECK(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
@@ -772,10 +780,11 @@ int launch_tiles(kfac_ctx *ctx, ExpertArgs g, int splits) {
 // ---- which kernel a call takes ----
 enum Engine { DIRECT_FEW = 0, DIRECT_SOME, DIRECT_SMALL, WIDE, WIDE_SMALL, TILES };
 struct Plan { Engine engine; int splits; };
+constexpr int TILE_OF[][3] = {{16, 32, 256}, {32, 64, 256}, {32, 32, 256}, {256, 256, 512}, {128, 128, 256}, {BM, BM, NTHREADS}};      // rows, columns, threads
 constexpr int MOST_SPLITS = 32;
 
-// The engines that a call can take are priced in us from its sizes alone (the offsets are on the device: every expert is taken to have rows / experts
-// of them), and the cheapest one runs.
+// The engines that a call can take are priced in us from its sizes alone (the offsets are on the device: every expert is taken to have rows
+// / experts of them), and the cheapest one runs.
 Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     const bool ragged = mode == FORWARD || mode == INPUT_GRAD;
     const int shortest = std::min(g.cols, ragged ? g.K : g.rows);
@@ -792,7 +801,7 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     Plan best{TILES, 1};
     double least = 1e300;
     auto offer = [&](Engine e, int splits, double cost) {
-        if (cost < least) { least = cost; best = Plan{e, splits}; }
+        if (cost < least && fits_launch(grid_of(g, mode, TILE_OF[e][0], TILE_OF[e][1]), TILE_OF[e][2])) { least = cost; best = Plan{e, splits}; }
     };
     // a split engine: `slots` workgroups run at once; a step of the contraction takes `alone` in a workgroup that has its compute unit to itself
     // and `full` where all slots are taken; parts cost the way to memory and back, and a second launch; `stream`: what
@@ -808,21 +817,22 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     };
     if (dtype == KFAC_BF16 && shortest >= WIDE_MIN) {
         if (mode == FORWARD) {
-            // the weights are streamed past 16 or 32 rows at a time; us: 8 experts of 2048 x 2048 with 8 rows each 14.5, 15.2 and (WIDE_SMALL) 27.5,
-            // with 32 25.8, 16.8 and 27.6; 64 of 1024 x 2048 with 16 each 73.8, 66.2 and 70.0, with 64 each 192, 112 and 74.9
+            // the weights are streamed past 16 or 32 rows at a time; us: 8 experts of 2048 x 2048 with 8 rows each 15.1, 15.7 and
+            // (WIDE_SMALL) 21.4, with 32 26.6, 17.5 and 22.2; 64 of 1024 x 2048 with 16 each 74.0, 67.2 and 70.5, with 64 each 194, 111 and
+            // 75.4
             const double few = tiles(16, 32), some = tiles(32, 64);
             offer(DIRECT_FEW, 1, 5.0 + std::max({0.28 * K / 128 * std::max(1.0, few / 1024), hbm, few * 48.0 * 2.0 * K / 9.4e6}));
             offer(DIRECT_SOME, 1, 5.0 + std::max({0.62 * K / 128 * std::max(1.0, some / 512), hbm, some * 96.0 * 2.0 * K / 9.4e6}));
         }
-        // us: one 1024 x 1024 layer forward over 4096 rows 29.5 and 20.8; 8 of 4096 x 4096 over 32768 965 and 1290; weight gradient 512 x 512
-        // over 32768 rows 622 and 418, in 4, 16 parts 138, 106
+        // us: one 1024 x 1024 layer forward over 4096 rows 27.5 and 15.9; 8 of 4096 x 4096 over 32768 872 and 1175; weight gradient 512 x 512
+        // over 32768 rows 654 and 337, in 16 parts 60
         const double slabs = K / WK;
         offer_split(WIDE, tiles(256, 256), 256, slabs, 1.1, 1.55, 4.0, 1.25, ws + 1, 1);
         offer_split(WIDE_SMALL, tiles(128, 128), 512, slabs, 0.72, 1.25, 3.0, 1.15, wide_part<4, 4, 2, 2>() * 4, grid_of(g, mode, 128, 128));
         return best;
     }
-    // us: input gradient 577 x 512 of 8 experts over 1568 rows 24.4 and (TILES) 53; weight gradient 1001 x 512 of 10 over 1000 37 and 30;
-    // 1024 x 1024 forward over 4096 rows 138 and 100
+    // us: input gradient 577 x 512 of 8 experts over 1568 rows 26.6 and (TILES) 52.7; weight gradient 1001 x 512 of 10 over 1000 40.2 and 30.3;
+    // 1024 x 1024 forward over 4096 rows 141 and 102
     if (dtype == KFAC_F32 && shortest >= 4) offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(1.0, tiles(32, 32) / 256.0) * K * 0.0085));
     offer_split(TILES, tiles(128, 128), 768, K / BK, 1.36, 3.6, 3.0, 1.0, TILE_PART * 4, grid_of(g, mode, BM, BM));
     return best;
@@ -891,7 +901,6 @@ size_t part_bytes(Engine e) { return e == WIDE_SMALL ? wide_part<4, 4, 2, 2>() *
 
 }  // namespace
 
-// For tests: the engine that a call takes and its parts, as 100 * engine + parts.
 extern "C" int kfac_experts_plan(int mode, const kfac_expert_desc *d, size_t workspace_bytes) {
     const Plan p = plan_of(args_of(mode, d), mode, d->dtype, workspace_bytes);
     return 100 * p.engine + p.splits;

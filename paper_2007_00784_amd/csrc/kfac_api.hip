@@ -365,10 +365,10 @@ size_t kfac_precondition_workspace_bytes(int n, const kfac_precond_item *items) 
     return kfac_precond_ws_bytes_impl(n, items);
 }
 
-// The rows that a call touches must lie inside 31 bits each way; offsets are read on the device and clamped there.
+// Offsets are read on the device and clamped there; with so many rows the tiles of 64 experts stay below 2^31 whatever the offsets are.
 static bool valid_expert_desc(const kfac_expert_desc *d, bool pointers = true) {
     if (!d || (pointers && (!d->offsets || ((uintptr_t)d->offsets & 3))) || d->experts < 1 || d->experts > KFAC_MAX_EXPERTS) return false;
-    if (d->rows < 0 || d->rows >= 1 << 30 || (d->append_ones != 0 && d->append_ones != 1) || !valid_dtype(d->dtype)) return false;
+    if (d->rows < 0 || d->rows >= KFAC_MAX_EXPERT_ROWS || (d->append_ones != 0 && d->append_ones != 1) || !valid_dtype(d->dtype)) return false;
     return d->d_in >= 1 && d->d_out >= 1 && d->d_in <= KFAC_MAX_EXPERT_D && d->d_out <= KFAC_MAX_EXPERT_D;
 }
 static bool valid_pitch(int64_t ld, int d) { return ld >= d && ld <= KFAC_MAX_PITCH; }

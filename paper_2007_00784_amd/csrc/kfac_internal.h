@@ -119,6 +119,7 @@ constexpr int KFAC_EIG_REG = 256;    // factors up to this size are reduced to t
 constexpr int KFAC_EIG_B = 32;       // block size of the blocked Jacobi path (sub-problems are 2B x 2B)
 constexpr int KFAC_MAX_D = 8192;
 constexpr int KFAC_MAX_EXPERTS = 4096;
+constexpr int KFAC_MAX_EXPERT_ROWS = 1 << 28;
 constexpr int KFAC_MAX_EXPERT_D = 65536;   // sides of an expert's weights
 constexpr int64_t KFAC_MAX_PITCH = 1 << 20; // elements between the rows of samples: 32-bit offsets inside a tile
 constexpr int KFAC_EIG_SPLIT_MIN = 2048;   // factors from here on use split-fp16 products where an option allows them
@@ -160,6 +161,10 @@ constexpr int KFAC_EIG_REFUSED = 2;  // (inside it) a launch that needs all its 
 constexpr int KFAC_CHIP_POLLS = 1 << 18;   // 0.5 to 1 us each
 // For tests: another number of workgroups of a cooperative launch (0: none), and of looks before a wait is given up (0: at once).
 extern "C" void kfac_limit_chip(kfac_ctx *ctx, int workgroups, int polls);
+
+// For tests: the engine that a call on a layer of experts takes and its parts, as 100 * engine + parts.  mode: 0 .. 3, forward, input
+// gradient, weight gradient, factors.
+extern "C" int kfac_experts_plan(int mode, const kfac_expert_desc *d, size_t workspace_bytes);
 size_t kfac_invert_ws_bytes_impl(int batch, const int *d);
 int kfac_launch_invert_factors(kfac_ctx *ctx, int batch, const float *const *F, const int *d, float damping, float *const *Finv);
 size_t kfac_precondition_inverse_ws_bytes_impl(int n, const kfac_precond_inv_item *items);

@@ -18,7 +18,7 @@ def desc(**kw):
     return ctypes.byref(K.kfac_expert_desc(**d))
 
 
-BAD_DESCS = [dict(experts=0), dict(experts=4097), dict(rows=-1), dict(rows=1 << 30), dict(d_in=0), dict(d_out=0), dict(d_in=65537), dict(d_out=65537),
+BAD_DESCS = [dict(experts=0), dict(experts=4097), dict(rows=-1), dict(rows=1 << 28), dict(d_in=0), dict(d_out=0), dict(d_in=65537), dict(d_out=65537),
              dict(append_ones=2), dict(append_ones=-1), dict(dtype=2), dict(offsets=None), dict(offsets=D + 2)]
 
 
@@ -145,7 +145,7 @@ def test_workspace_of_experts():
     f = K.lib().kfac_experts_plan
     f.argtypes = [ctypes.c_int, ctypes.POINTER(K.kfac_expert_desc), ctypes.c_size_t]
     for dtype in (K.KFAC_F32, K.KFAC_BF16):
-        for shape in ((1, 32768, 512, 512), (2, 6000, 75, 133), (1, 300, 70, 1607), (64, 4096, 2048, 1000), (3, 1, 8, 8), (1, (1 << 30) - 1, 64, 64), (4096, 0, 65536, 65536)):
+        for shape in ((1, 32768, 512, 512), (2, 6000, 75, 133), (1, 300, 70, 1607), (64, 4096, 2048, 1000), (3, 1, 8, 8), (1, (1 << 28) - 1, 64, 64), (4096, 0, 65536, 65536)):
             for ones in (0, 1):
                 need = K.kfac_experts_workspace_bytes(*shape, ones, dtype)
                 assert need % 256 == 0 and need < 1 << 31
@@ -155,3 +155,28 @@ def test_workspace_of_experts():
                     assert f(mode, d, need) == full
                     assert none % 100 == 1 and (some // 100 != full // 100 or some % 100 <= full % 100)
     assert K.kfac_experts_workspace_bytes(0, 100, 64, 64) == 0 and K.kfac_experts_workspace_bytes(1, -1, 64, 64) == 0
+
+
+TILE_OF = ((16, 32, 256), (32, 64, 256), (32, 32, 256), (256, 256, 512), (128, 128, 256), (128, 128, 256))      # rows, columns, threads of an engine
+
+
+@pytest.mark.parametrize("dtype", [K.KFAC_F32, K.KFAC_BF16])
+@pytest.mark.parametrize("mode", [0, 1])
+def test_long_layers_fit_a_launch(dtype, mode):
+    """Whatever fits the memory (288 GB) runs: an engine is taken only if its workgroups are fewer than a launch can have (2^32 threads)."""
+    f = K.lib().kfac_experts_plan
+    f.argtypes = [ctypes.c_int, ctypes.POINTER(K.kfac_expert_desc), ctypes.c_size_t]
+    taken = set()
+    for rows in (1 << 20, 1 << 24, (1 << 28) - 1):
+        for side in (4, 8, 16, 64, 128, 256, 1000, 4096):
+            for other in (4, 8, 64, 1000, 4096):
+                for experts in (1, 64, 4096):
+                    if (2 if dtype else 4) * (rows * (side + other) + experts * side * other) > 288e9:
+                        continue
+                    engine = f(mode, ctypes.byref(K.kfac_expert_desc(experts, rows, side, other, 0, dtype, None)), 0) // 100
+                    r, c, threads = TILE_OF[engine]
+                    cols = other if mode == 0 else side
+                    tiles = (rows // r + min(experts, rows)) * -(-cols // c)
+                    assert -(-tiles // 8) * 8 * threads < 1 << 32, (rows, side, other, experts, engine)
+                    taken.add(engine)
+    assert len(taken) > 1
