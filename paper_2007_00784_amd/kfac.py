@@ -404,7 +404,7 @@ def _rows(t, name, d):
         return None, d
     if d > 1 and t.stride(1) != 1:
         raise ValueError("the rows of %s must be contiguous" % name)
-    ld = t.stride(0) if t.shape[0] > 1 else max(d, t.stride(0))
+    ld = t.stride(0) if t.shape[0] > 1 else d
     if ld < d:
         raise ValueError("the rows of %s overlap" % name)
     return t.data_ptr(), ld
@@ -502,11 +502,13 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
 # ---- the optimizer step ----
 def adamw_items(items):
     """The marshalled item array of kfac_adamw_batched for a list of dicts(param, grad, m, v[, m_scale, v_scale][, copy]) of device tensors,
-    reusable while the buffers live.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or uint8), m_scale, v_scale uint8, one for
-    each 128 elements.  copy: bfloat16, takes the updated parameter."""
+    reusable while the buffers live; none that is written may occur twice.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or
+    uint8), m_scale, v_scale uint8, one for each 128 elements.  copy: bfloat16, takes the updated parameter."""
     import torch
     code = {torch.float32: KFAC_F32, torch.bfloat16: KFAC_BF16}
+    codes = (torch.uint8, torch.float8_e4m3fn)
     arr = (kfac_adamw_item * len(items))()
+    written = set()
     for d, it in zip(arr, items):
         p, g, m, v = it["param"], it["grad"], it["m"], it["v"]
         ms, vs, copy = it.get("m_scale"), it.get("v_scale"), it.get("copy")
@@ -520,8 +522,8 @@ def adamw_items(items):
                 raise ValueError("m and v must be float32 (or come with scales)")
         else:
             blocks = (n + 127) // 128
-            if m.element_size() != 1 or v.element_size() != 1 or any(s.dtype != torch.uint8 or s.numel() != blocks for s in (ms, vs)):
-                raise ValueError("m and v must have a byte for each element, the scales (uint8) one for each 128")
+            if m.dtype not in codes or v.dtype not in codes or any(s.dtype != torch.uint8 or s.numel() != blocks for s in (ms, vs)):
+                raise ValueError("m and v must be float8_e4m3fn or uint8, the scales uint8, one for each 128")
             d.m_scale, d.v_scale = _ptr(ms), _ptr(vs)
         if copy is not None:
             if copy.dtype != torch.bfloat16:
@@ -533,6 +535,10 @@ def adamw_items(items):
             raise ValueError("parameters and gradients must be float32 or bfloat16") from None
         d.param, d.grad, d.m, d.v, d.n = _ptr(p), _ptr(g), _ptr(m), _ptr(v), n
         _on_gpu(p, g, m, v, ms, vs, copy)
+        mine = [t for t in (d.param, d.m, d.v, d.m_scale, d.v_scale, d.copy) if t] if n > 0 else []
+        if len(set(mine)) < len(mine) or not written.isdisjoint(mine):      # (it would be updated from two sides at once)
+            raise ValueError("a buffer occurs twice")
+        written.update(mine)
     return arr
 
 
@@ -561,8 +567,8 @@ def kfac_adamw_state_values(ctx, codes, scale, out):
     """out[i] = codes[i] * 2^(scale[i // 128] - 127): what an 8-bit state stands for (m, and sqrt(v)), float32 or bfloat16."""
     import torch
     n = codes.numel()
-    if codes.element_size() != 1 or out.numel() != n or scale.dtype != torch.uint8 or scale.numel() != (n + 127) // 128:
-        raise ValueError("codes: a byte for each element of out, scale: uint8, one for each 128")
+    if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or out.numel() != n or scale.dtype != torch.uint8 or scale.numel() != (n + 127) // 128:
+        raise ValueError("codes: float8_e4m3fn or uint8, as many as out, scale: uint8, one for each 128")
     code = _dtype_code(out)
     _on_gpu(codes, scale, out)
     _check(lib().kfac_adamw_state_values(ctx, _ptr(codes), _ptr(scale), n, _ptr(out), code), "kfac_adamw_state_values")

@@ -140,6 +140,45 @@ def test_tensors_that_do_not_fit():
             call()
 
 
+def test_codes_of_another_format():
+    """One byte an element is not enough: only e4m3 codes are what the state holds."""
+    p, s = torch.zeros(300), torch.zeros(3, dtype=torch.uint8)
+    for dt in (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.int8, torch.bool):
+        u = torch.zeros(300).to(dt)
+        for pair in ((u, torch.zeros(300, dtype=torch.uint8)), (torch.zeros(300, dtype=torch.uint8), u)):
+            with refused():
+                K.adamw_items([dict(param=p, grad=p, m=pair[0], v=pair[1], m_scale=s, v_scale=s)])
+        with refused():
+            K.kfac_adamw_state_values(CTX, u, s, p)
+
+
+def test_buffers_that_occur_twice(monkeypatch):
+    monkeypatch.setattr(K, "_on_gpu", lambda *tensors: None)
+
+    def item(eight=False, n=300):
+        new = (lambda: torch.zeros(n, dtype=torch.uint8)) if eight else (lambda: torch.zeros(n))
+        it = dict(param=torch.zeros(n), grad=torch.zeros(n), m=new(), v=new(), copy=torch.zeros(n, dtype=torch.bfloat16))
+        return dict(it, m_scale=torch.zeros(-(-n // 128), dtype=torch.uint8), v_scale=torch.zeros(-(-n // 128), dtype=torch.uint8)) if eight else it
+
+    for eight in (False, True):
+        a, b = item(eight), item(eight)
+        assert len(K.adamw_items([a, b, item(eight, 0), item(eight, 0)])) == 4
+        assert len(K.adamw_items([a, dict(b, grad=a["grad"])])) == 2       # (a gradient is only read)
+        for key in a:
+            if key != "grad":
+                with pytest.raises(ValueError, match="twice"):
+                    K.adamw_items([a, dict(b, **{key: a[key]})])
+        with pytest.raises(ValueError, match="twice"):
+            K.adamw_items([dict(a, m=a["v"])])
+
+
+def test_the_pitch_of_a_single_row():
+    """One row has no pitch, whatever the matrix was that it is taken from."""
+    assert K._rows(torch.empty(1 << 21).as_strided((1, 8), (1 << 21, 1)), "X", 8)[1] == 8
+    assert K._rows(torch.empty(16).as_strided((1, 8), (0, 1)), "X", 8)[1] == 8
+    assert K._rows(torch.empty(32).as_strided((2, 8), (16, 1)), "X", 8)[1] == 16
+
+
 def test_workspace_of_experts():
     """What is asked for suffices for the plan, less of it means fewer parts, and an invalid description asks for nothing."""
     f = K.lib().kfac_experts_plan
