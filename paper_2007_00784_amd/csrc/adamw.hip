@@ -202,7 +202,6 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamLaunch a) {
     const int id = item_of(a, blockIdx.x);
     const AdamItem it = a.item[id];
     const bool pbf = a.pbf[id], gbf = a.gbf[id];
-    const Hyper h = hyper_of(a);
     const int64_t i = ((int64_t)(blockIdx.x - it.first) * THREADS + threadIdx.x) * N32;
     const int in = (int)min((int64_t)N32, max((int64_t)it.n - i, (int64_t)0));
     float g[N32], p[N32], m[N32], v[N32];
@@ -210,6 +209,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamLaunch a) {
     fetch(it.p, pbf, i, in, p);
     fetch(it.m, false, i, in, m);
     fetch(it.v, false, i, in, v);
+    const Hyper h = hyper_of(a);       // (under the loads: with the step in device memory its powers take 64-bit operations)
 #pragma unroll
     for (int k = 0; k < N32; ++k) (void)adam(h, g[k], m[k], v[k], p[k]);
     put(it.p, pbf, i, in, p);
@@ -240,7 +240,6 @@ __global__ __launch_bounds__(THREADS) void adamw8_kernel(const AdamLaunch a) {
     const int id = item_of(a, blockIdx.x);
     const AdamItem it = a.item[id];
     const bool pbf = a.pbf[id], gbf = a.gbf[id];
-    const Hyper h = hyper_of(a);
     const int64_t i = ((int64_t)(blockIdx.x - it.first) * THREADS + threadIdx.x) * N8;
     const int in = (int)min((int64_t)N8, max((int64_t)it.n - i, (int64_t)0));
     float g[N8], p[N8], m[N8], r[N8];
@@ -248,6 +247,7 @@ __global__ __launch_bounds__(THREADS) void adamw8_kernel(const AdamLaunch a) {
     const int ms = in > 0 ? it.ms[i / BLOCK] : 0, vs = in > 0 ? it.vs[i / BLOCK] : 0;
     fetch(it.g, gbf, i, in, g);
     fetch(it.p, pbf, i, in, p);
+    const Hyper h = hyper_of(a);       // (25.6M parameters, the step in device memory: in front of the loads 83 us, here 79)
     decode8(mc, ms - 127, m);
     decode8(vc, vs - 127, r);
 #pragma unroll
