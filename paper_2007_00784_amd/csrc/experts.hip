@@ -778,9 +778,21 @@ int launch_tiles(kfac_ctx *ctx, ExpertArgs g, int splits) {
 }
 
 // ---- which kernel a call takes ----
-enum Engine { DIRECT_FEW = 0, DIRECT_SOME, DIRECT_SMALL, WIDE, WIDE_SMALL, TILES };
+enum Engine { DIRECT_FEW = 0, DIRECT_SOME, DIRECT_SMALL, WIDE, WIDE_SMALL, TILES, DIRECT_MEDIUM };
 struct Plan { Engine engine; int splits; };
-constexpr int TILE_OF[][3] = {{16, 32, 256}, {32, 64, 256}, {32, 32, 256}, {256, 256, 512}, {128, 128, 256}, {BM, BM, NTHREADS}};      // rows, columns, threads
+struct Shape { int rows, cols, threads; };      // of an engine's tile, and its workgroup
+Shape shape_of(Engine e) {
+    switch (e) {
+        case DIRECT_FEW: return {16, 32, 256};
+        case DIRECT_SOME: return {32, 64, 256};
+        case DIRECT_SMALL: return {32, 32, 256};
+        case DIRECT_MEDIUM: return {32, 64, 256};
+        case WIDE: return {256, 256, 512};
+        case WIDE_SMALL: return {128, 128, 256};
+        case TILES: break;
+    }
+    return {BM, BM, NTHREADS};
+}
 constexpr int MOST_SPLITS = 32;
 
 // The engines that a call can take are priced in us from its sizes alone (the offsets are on the device: every expert is taken to have rows
@@ -794,14 +806,21 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     const double hbm = (weights + es * g.R * (double)(ragged ? g.K + g.cols : g.rows + (mode == FACTORS ? 0 : g.cols))) / 4.5e6;
     auto tiles = [&](double ext_r, double ext_c) {
         const double nt = std::ceil(g.cols / ext_c);
+        if (ragged && g.E == 1) return std::ceil(each / ext_r) * nt;
         if (ragged) return busy * std::max(1.0, each / ext_r + 0.6) * nt;     // (half a tile is lost behind each expert's rows, and they differ)
         const double mt = std::ceil(g.rows / ext_r);
         return (mode == FACTORS ? mt * (mt + 1) / 2 : mt * nt) * busy;
     };
+    // of sums over rows, the longest expert's takes the most, and where there is a compute unit for every tile it is what the call takes
+    const double longest = !ragged && g.E > 1 ? 1.5 : 1.0;
     Plan best{TILES, 1};
     double least = 1e300;
     auto offer = [&](Engine e, int splits, double cost) {
-        if (cost < least && fits_launch(grid_of(g, mode, TILE_OF[e][0], TILE_OF[e][1]), TILE_OF[e][2])) { least = cost; best = Plan{e, splits}; }
+        const Shape t = shape_of(e);
+        if (cost < least && fits_launch(grid_of(g, mode, t.rows, t.cols), t.threads)) {
+            least = cost;
+            best = Plan{e, splits};
+        }
     };
     // a split engine: `slots` workgroups run at once; a step of the contraction takes `alone` in a workgroup that has its compute unit to itself
     // and `full` where all slots are taken; parts cost the way to memory and back, and a second launch; `stream`: what
@@ -809,9 +828,9 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
     auto offer_split = [&](Engine e, double t, double slots, double steps, double alone, double full, double fixed, double stream, size_t part_bytes, size_t grid) {
         for (int s = 1; s <= MOST_SPLITS && (s == 1 || steps / s >= 4.0); s *= 2) {
             if (s > 1 && (size_t)s * part_bytes * grid > ws) break;
-            const double wgs = t * s, share = std::min(1.0, std::max(0.0, (wgs - 256.0) / std::max(slots - 256.0, 1.0)));
-            const double step = slots > 256.0 ? alone + (full - alone) * share : alone + (full - alone) * std::min(1.0, wgs / 256.0);
-            const double run = std::max(std::ceil(wgs / slots) * (fixed + std::ceil(steps / s) * step), stream * hbm);
+            const double wgs = t * s, units = slots / 256.0, there = std::min(units, std::ceil(wgs / 256.0));     // on the fullest compute unit
+            const double step = units > 1.0 ? alone + (full - alone) * (there - 1.0) / (units - 1.0) : alone + (full - alone) * std::min(1.0, wgs / 256.0);
+            const double n = std::ceil(steps / s), run = std::max({std::ceil(wgs / slots) * (fixed + n * step), longest * (fixed + n * alone), stream * hbm});
             offer(e, s, 3.0 + run + (s > 1 ? 5.0 + 2.0 * (double)part_bytes * t * s / 2.5e6 + 0.3 * s : 0.0));
         }
     };
@@ -831,9 +850,13 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
         offer_split(WIDE_SMALL, tiles(128, 128), 512, slabs, 0.72, 1.25, 3.0, 1.15, wide_part<4, 4, 2, 2>() * 4, grid_of(g, mode, 128, 128));
         return best;
     }
-    // us: input gradient 577 x 512 of 8 experts over 1568 rows 26.6 and (TILES) 52.7; weight gradient 1001 x 512 of 10 over 1000 40.2 and 30.3;
-    // 1024 x 1024 forward over 4096 rows 141 and 102
-    if (dtype == KFAC_F32 && shortest >= 4) offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(1.0, tiles(32, 32) / 256.0) * K * 0.0085));
+    // us, in tiles of 32 x 32, of 32 x 64 and (TILES) of 128 x 128: forward 512 x 512 of 8 experts over 64 rows 8.8, 10.0, 26; input
+    // gradient 577 x 512 of 8 over 1568 23.3, 19.7, 52.5; weight gradient 1001 x 512 of 10 over 1000 40, 31.4, 44; 512 x 512 of 16 over
+    // 16384 (32 x 64, TILES) 107 and 174; one 1024 x 1024 forward over 4096 138, 125, 97
+    if (dtype == KFAC_F32 && shortest >= 4) {
+        offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(longest, tiles(32, 32) / 256.0) * K * 0.0085));
+        if (mode != FACTORS) offer(DIRECT_MEDIUM, 1, 6.0 + std::max(hbm, std::max(longest, tiles(32, 64) / 256.0) * K * (mode == FORWARD ? 0.0145 : 0.012)));
+    }
     offer_split(TILES, tiles(128, 128), 768, K / BK, 1.36, 3.6, 3.0, 1.0, TILE_PART * 4, grid_of(g, mode, BM, BM));
     return best;
 }
@@ -864,6 +887,11 @@ int launch_mode(kfac_ctx *ctx, const ExpertArgs &g, int dtype) {
             if constexpr (MODE == FORWARD) return launch_direct<MODE, unsigned short, 2, 4, 4, 2>(ctx, g);
             break;
         case DIRECT_SMALL: return launch_direct<MODE, float, 2, 2, 4, ragged ? 2 : 6>(ctx, g);
+        case DIRECT_MEDIUM:
+            // (steps in flight: 1, 2, 4: forward 577 x 512 of 8 experts over 1568 rows 24.1, 23.4, 23.7 us, input gradient of 1024 x 1024
+            // over 512 18.4, 16.8, 16.1, weight gradient of the table above 31.4, 34.4, 40.1)
+            if constexpr (MODE != FACTORS) return launch_direct<MODE, float, 2, 4, 4, MODE == FORWARD ? 2 : MODE == INPUT_GRAD ? 4 : 1>(ctx, g);
+            break;
         case WIDE: return launch_wide<MODE, 8, 4, 2, 4, 2, false>(ctx, g, 1);
         case WIDE_SMALL: return launch_wide<MODE, 4, 4, 2, 2, 2, true>(ctx, g, plan.splits);
         case TILES: break;

@@ -305,7 +305,7 @@ def test_no_rows(ctx):
 
 # ---- every engine that a call can take, whole and in parts ----
 FORWARD, INPUT_GRAD, WEIGHT_GRAD, FACTORS = range(4)
-FEW, SOME, SMALL, WIDE, WIDE_SMALL, TILES = range(6)
+FEW, SOME, SMALL, WIDE, WIDE_SMALL, TILES, MEDIUM = range(7)
 # mode, counts, d_in, d_out, ones, bf16, engine, parts
 ENGINES = [
     (FORWARD, [3, 0, 5], 265, 130, 1, True, FEW, False),
@@ -323,15 +323,23 @@ ENGINES = [
     (FACTORS, [6100, 160], 203, 1, 1, True, WIDE_SMALL, True),
     (FORWARD, [40, 21], 75, 133, 1, False, SMALL, False),
     (FORWARD, [12000], 16, 130, 1, False, TILES, False),
-    (FORWARD, [2205], 1001, 1103, 1, False, TILES, True),
+    (FORWARD, [2205], 1001, 1103, 1, False, MEDIUM, False),
+    (FORWARD, [30, 0, 7], 70, 1103, 1, False, SMALL, False),
+    (FORWARD, [3] * 12 + [1], 70, 1607, 1, False, MEDIUM, False),
+    (FORWARD, [200, 103], 300, 3, 1, False, TILES, True),
+    (FORWARD, [8000], 1601, 603, 1, False, TILES, True),
     (INPUT_GRAD, [40, 21], 75, 133, 1, False, SMALL, False),
     (INPUT_GRAD, [2200], 1603, 29, 1, False, TILES, False),
-    (INPUT_GRAD, [2205], 1103, 1001, 1, False, TILES, True),
+    (INPUT_GRAD, [2205], 1103, 1001, 1, False, MEDIUM, False),
+    (INPUT_GRAD, [3] * 12 + [1], 1001, 75, 1, False, MEDIUM, False),
+    (INPUT_GRAD, [300], 3, 1607, 1, False, TILES, True),
     (WEIGHT_GRAD, [40, 21], 75, 133, 1, False, SMALL, False),
     (WEIGHT_GRAD, [4] * 40, 1601, 101, 1, False, TILES, False),
+    (WEIGHT_GRAD, [190, 0, 103] * 8, 1601, 75, 1, False, MEDIUM, False),
     (WEIGHT_GRAD, [6600], 75, 133, 1, False, TILES, True),
     (FACTORS, [40, 21], 135, 1, 1, False, SMALL, False),
-    (FACTORS, [4, 3, 5], 603, 1, 1, False, TILES, False),
+    (FACTORS, [4, 3, 5], 603, 1, 1, False, SMALL, False),
+    (FACTORS, [4, 9, 3, 5, 0, 6, 5, 5], 513, 1, 1, False, TILES, False),
     (FACTORS, [9900, 700], 255, 1, 1, False, TILES, True),
 ]
 

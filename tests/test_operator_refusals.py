@@ -196,7 +196,7 @@ def test_workspace_of_experts():
     assert K.kfac_experts_workspace_bytes(0, 100, 64, 64) == 0 and K.kfac_experts_workspace_bytes(1, -1, 64, 64) == 0
 
 
-TILE_OF = ((16, 32, 256), (32, 64, 256), (32, 32, 256), (256, 256, 512), (128, 128, 256), (128, 128, 256))      # rows, columns, threads of an engine
+TILE_OF = ((16, 32, 256), (32, 64, 256), (32, 32, 256), (256, 256, 512), (128, 128, 256), (128, 128, 256), (32, 64, 256))      # rows, columns, threads of an engine
 
 
 @pytest.mark.parametrize("dtype", [K.KFAC_F32, K.KFAC_BF16])
