@@ -314,8 +314,12 @@ int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int 
  * computed in fp32.  State in 32 bits (m_scale = v_scale = NULL): m and v are fp32.  State in 8 bits: m and v point to one byte for
  * each element, OCP e4m3 codes of m and of sqrt(v), and m_scale / v_scale to one byte for each 128 elements (the last may be fewer), the power of
  * two (biased by 127) that the codes are multiplied with: the smallest from 2^-127 on for which the block's largest magnitude is at
- * most 448 times it.  Codes are rounded half to even; a sqrt(v) above zero is held as the smallest code above zero at least; what is not
+ * most 448 times it.  A sqrt(v) above zero is held as the smallest code above zero at least; what is not
  * finite is held as NaN.  All bytes zero stand for a state of zero.  The parameter is updated with the moments before they are rounded.
+ * TRAINING WITH 8-BIT STATE NEEDS A SEED.  With one, a value between two codes becomes the upper one with the probability of its distance from
+ * the lower, so that the state follows its moments over a run (m in expectation, sqrt(v) within some percent).  Without one (seed 0) codes
+ * are rounded half to even: the nearest code after each call, but steps below half the distance of two codes (3 to 6 %) are lost, and over a
+ * run that is nearly all of them: with beta2 = 0.999 sqrt(v) stays at 0.4 of what it should be, and does not fall when gradients do.
  * One launch for each 54 tensors and kind of state.  Nothing is copied from the host, no workspace is used, and the call may be captured; with
  * step_dev, lr_dev and grad_scale its replays take another step each.  */
 typedef struct {
@@ -335,6 +339,8 @@ typedef struct {
     const float *grad_scale; /* DEVICE, may be NULL (1): e.g. the coefficient of a clipping by the global norm over the loss scale */
     const float *lr_dev;     /* DEVICE, may be NULL: read instead of lr                                    */
     const int64_t *step_dev; /* DEVICE, may be NULL: read instead of step (below 1 counts as 1)             */
+    uint64_t seed;           /* of the rounding of 8-bit state, see above; 0: half to even.  What is drawn follows from the seed, the step (which
+                                has to count on from call to call) and a tensor's place in the list       */
 } kfac_adamw_opts;
 /* Tensors of one call, and the buffers of one tensor, must not overlap.  */
 int kfac_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items /* host */, const kfac_adamw_opts *opts /* host */);

@@ -79,7 +79,7 @@ class kfac_adamw_item(ctypes.Structure):
 class kfac_adamw_opts(ctypes.Structure):
     _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("lr", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("step", ctypes.c_int64), ("grad_scale", ctypes.c_void_p),
-                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p)]
+                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("seed", ctypes.c_uint64)]
 
 
 class KfacError(RuntimeError):
@@ -551,15 +551,19 @@ def _scalar(t, dtype, name):
     return _ptr(t)
 
 
-def kfac_adamw_batched(ctx, items, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, grad_scale=None):
+def kfac_adamw_batched(ctx, items, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, grad_scale=None, seed=0):
     """One AdamW step over a list of tensors (see adamw_items()).  lr and step: numbers, or device tensors of one float32 / int64 that the call
-    reads on the GPU; grad_scale: None or a device tensor of one float32 that every gradient is multiplied with."""
+    reads on the GPU; grad_scale: None or a device tensor of one float32 that every gradient is multiplied with.
+    seed (1 .. 2^64 - 1): training with 8-bit state needs one, together with a step that counts on.  Codes are then rounded up or down
+    at random, so that the state follows its moments; with 0 they are rounded half to even, which loses most steps of a run."""
     import torch
+    if not 0 <= int(seed) < 1 << 64:
+        raise ValueError("seed must be 0 .. 2^64 - 1")
     arr = adamw_items(items) if isinstance(items, list) else items
     lr_dev = _scalar(lr, torch.float32, "lr") if torch.is_tensor(lr) else None
     step_dev = _scalar(step, torch.int64, "step") if torch.is_tensor(step) else None
     o = kfac_adamw_opts(float(beta1), float(beta2), 0.0 if lr_dev else float(lr), float(eps), float(weight_decay), 1 if step_dev else int(step),
-                        _scalar(grad_scale, torch.float32, "grad_scale"), lr_dev, step_dev)
+                        _scalar(grad_scale, torch.float32, "grad_scale"), lr_dev, step_dev, int(seed))
     _check(lib().kfac_adamw_batched(ctx, len(arr), arr, ctypes.byref(o)), "kfac_adamw_batched")
 
 

@@ -178,10 +178,13 @@ class ExpertRunner:
     eigendecompositions, the preconditioned gradient and the optimizer step that writes the weights which the next products read.
 
     The rows of x and g are sorted by expert, offsets (int32 [experts + 1], on the GPU) say where each one's begin.  Parameters are kept in fp32 with their
-    bias as last column; bf16 layers multiply with a bf16 copy of them that the optimizer step writes.
+    bias as last column; bf16 layers multiply with a bf16 copy of them that the optimizer step writes.  seed: of the rounding of an 8-bit state.
     """
+    # At step t a gradient as large as the average moves sqrt(v) by 1 / (2 t) (beta2 near 1), which up to the eighth is half the distance of two
+    # codes at least: until then an 8-bit state is rounded to nearest, which is off by less; from then on by the seed, or it would stand still.
+    NEAREST_STEPS = 8
 
-    def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0"):
+    def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0", seed=1):
         self.dev = torch.device(device)
         self.experts, self.rows, self.d_in, self.d_out, self.bias, self.damping = experts, rows, d_in, d_out, bool(bias), damping
         self.dt = torch.bfloat16 if bf16 else torch.float32
@@ -202,7 +205,7 @@ class ExpertRunner:
         else:
             state = {k: torch.zeros(n, **f32) for k in ("m", "v")}
         self.state = state
-        self.steps = 0
+        self.steps, self.seed = 0, seed
         dims = [dA] * experts + [d_out] * experts
         need = max(K.kfac_eig_workspace_bytes(dims), K.kfac_precondition_workspace_bytes([(dA, d_out)] * experts),
                    K.kfac_experts_workspace_bytes(experts, rows, d_in, d_out, self.bias, K.KFAC_BF16 if bf16 else K.KFAC_F32))
@@ -245,5 +248,6 @@ class ExpertRunner:
         K.kfac_precondition_batched(self.ctx, items=self._precond)
 
     def step(self, lr, grad_scale=None, **hyper):
-        self.steps += 1
-        K.kfac_adamw_batched(self.ctx, self._adamw, lr=lr, step=self.steps, grad_scale=grad_scale, **hyper)
+        t = self.steps + 1
+        K.kfac_adamw_batched(self.ctx, self._adamw, lr=lr, step=t, grad_scale=grad_scale, seed=self.seed if t > self.NEAREST_STEPS else 0, **hyper)
+        self.steps = t
