@@ -29,7 +29,7 @@
 // expectation of m then follows the formula exactly.  That of sqrt(v) does too but for second order: a step's variance, at most |step| times the
 // distance of the codes, goes into v, which with normal gradients is 4 % of v, and its spread takes from the mean root: together 1 % of sqrt(v).
 // The words come from a hash of element, tensor, step and seed, so a call is the same from run to run and a graph whose step is in
-// device memory draws anew at every replay.  268M parameters take 797 us with a seed and 790 without.
+// device memory draws anew at every replay.  268M parameters take 808 us with a seed and 790 without.
 #include <algorithm>
 #include <cmath>
 #include "kfac_internal.h"
@@ -90,15 +90,19 @@ __device__ inline Hyper hyper_of(const AdamLaunch &a) {
     return h;
 }
 
-// One element.  m, v (fp32) in and out, the parameter in and out; returns sqrt(v).
-__device__ inline float adam(const Hyper &h, float g, float &m, float &v, float &p) {
-    g *= h.gs;
+// One element: the first moment and the parameter, from the scaled gradient and sqrt(v) of this step.
+__device__ inline void adam(const Hyper &h, float g, float root, float &m, float &p) {
     m = fmaf(h.b1, m, h.c1 * g);
-    v = fmaf(h.b2, v, h.c2 * g * g);
-    const float root = sqrtf(v);
     const float step = (m * h.ibc1) / fmaf(root, h.isbc2, h.eps);
     p = fmaf(-h.lr, step, fmaf(-h.decay, p, p));
-    return root;
+}
+__device__ inline float next_v(const Hyper &h, float g, float v) { return fmaf(h.b2, v, h.c2 * g * g); }
+// sqrt(v) of this step from that of the last, which need not have a square in fp32 (below 2^-75, from 2^64 on): both terms are brought to a size
+// near one by a power of two first, which changes no bit of what can be squared.
+__device__ inline float next_root(const Hyper &h, float g, float root) {
+    const int e = __builtin_amdgcn_frexp_expf(fmaxf(fabsf(g), fabsf(root)));      // (0 for a zero and what is not finite)
+    const float x = ldexpf(root, -e);
+    return ldexpf(sqrtf(next_v(h, ldexpf(g, -e), x * x)), e);
 }
 
 // N consecutive elements from anywhere: tensors may start at any element, and the loads are as wide as N allows all the same (global memory
@@ -247,7 +251,11 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const AdamLaunch a) {
     fetch(it.v, false, i, in, v);
     const Hyper h = hyper_of(a);       // (under the loads: with the step in device memory its powers take 64-bit operations)
 #pragma unroll
-    for (int k = 0; k < N32; ++k) (void)adam(h, g[k], m[k], v[k], p[k]);
+    for (int k = 0; k < N32; ++k) {
+        g[k] *= h.gs;
+        v[k] = next_v(h, g[k], v[k]);
+        adam(h, g[k], sqrtf(v[k]), m[k], p[k]);
+    }
     put(it.p, pbf, i, in, p);
     put(it.m, false, i, in, m);
     put(it.v, false, i, in, v);
@@ -288,8 +296,9 @@ template <bool DITHER> __global__ __launch_bounds__(THREADS) void adamw8_kernel(
     decode8(vc, vs - 127, r);
 #pragma unroll
     for (int k = 0; k < N8; ++k) {
-        float v = r[k] * r[k];
-        r[k] = adam(h, g[k], m[k], v, p[k]);
+        g[k] *= h.gs;
+        r[k] = next_root(h, g[k], r[k]);
+        adam(h, g[k], r[k], m[k], p[k]);
         if (k >= in) m[k] = r[k] = 0.f;       // (a gradient scale that is not finite must not reach the block from behind the tensor's end)
     }
     // one word an element: m takes its upper 20 bits, sqrt(v) its lower 20 (the eight that both have are the last of m's)

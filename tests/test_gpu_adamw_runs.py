@@ -192,3 +192,29 @@ def test_the_runner_of_a_layer_of_experts_follows():
     assert 1 - SAMPLING <= float(out.double().mean() / v.sqrt().mean()) <= STEADY
     assert run.steps == 300
     run.close()
+
+
+@pytest.mark.parametrize("seed", [0, 5])
+def test_roots_that_have_no_square_in_fp32(ctx, seed):
+    """Gradients and roots from 2^-100 to 2^100, block by block: a root is lost neither below 2^-75 nor from 2^64 on, where v is 0 or infinite in fp32."""
+    n = 201 * BLOCK
+    size = 2.0 ** np.repeat(np.arange(-100, 101), BLOCK)
+    t = Tensor(n, 8, seed=11)
+    for k in ("m_scale", "v_scale"):
+        t.t[k].copy_(torch.arange(-100, 101) + 127 - 8)
+    g = np.random.default_rng(12).normal(0, 1, n) * size
+    g[::3] = 0.0                                             # (what is held goes on by itself)
+    t.t["grad"].copy_(torch.from_numpy(g))
+    t.was["grad"] = t.t["grad"].cpu().double().numpy()
+    t.was["m"], t.was["u"] = t.values("m"), t.values("v")
+    t.was["v"] = t.was["u"] ** 2
+    K.kfac_adamw_batched(ctx.h, [t.t], step=3, seed=seed, **HYPER)
+    torch.cuda.synchronize()
+    if seed == 0:
+        t.check()
+    _, m, v, upd = adam64(*(t.was[k] for k in ("param", "grad", "m", "v")), 3, HYPER)
+    assert (np.isfinite(t.values("m")) & np.isfinite(t.values("v"))).all() and (t.values("v")[v > 0] > 0).all()
+    # between neighbouring codes: an eighth of the value, or 2^-9 of the block's unit, whose 448 are at most twice its largest
+    big = np.repeat(np.sqrt(v).reshape(-1, BLOCK).max(1), BLOCK)
+    assert (np.abs(t.values("v") - np.sqrt(v)) <= (1 / 8 + 1e-6) * np.sqrt(v) + 2.0 ** -9 * big / 224).all()
+    assert np.isfinite(t.t["param"].cpu().numpy()).all()
