@@ -313,8 +313,8 @@ int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int 
  *   param <- param - lr weight_decay param - lr (m / (1 - beta1^step)) / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * computed in fp32.  State in 32 bits (m_scale = v_scale = NULL): m and v are fp32.  State in 8 bits: m and v point to one byte for
  * each element, OCP e4m3 codes of m and of sqrt(v), and m_scale / v_scale to one byte for each 128 elements (the last may be fewer), the power of
- * two (biased by 127) that the codes are multiplied with: the smallest from 2^-127 on for which the block's largest magnitude is at
- * most 448 times it.  A sqrt(v) above zero is held as the smallest code above zero at least; what is not
+ * two (biased by 127) that the codes are multiplied with: the smallest from 2^-127 to 2^119 for which the block's largest magnitude is at
+ * most 448 times it (magnitudes above 448 * 2^119 are held as that).  A sqrt(v) above zero is held as the smallest code above zero at least; what is not
  * finite is held as NaN.  All bytes zero stand for a state of zero.  The parameter is updated with the moments before they are rounded.
  * TRAINING WITH 8-BIT STATE NEEDS A SEED.  With one, a value between two codes becomes the upper one with the probability of its distance from
  * the lower, so that the state follows its moments over a run (m in expectation, sqrt(v) within some percent).  Without one (seed 0) codes

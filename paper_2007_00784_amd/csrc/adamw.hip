@@ -14,7 +14,8 @@
 // the first takes 139 and 144 us, with two the last 1079, and 0.47M with 8-bit state 9.2 instead of 6.2.
 //
 // 8-bit state: m and sqrt(v) as e4m3 codes times 2^s, one s (a byte, biased by 127) for each BLOCK consecutive elements of
-// the tensor, the smallest from -127 on for which the block's largest magnitude is at most 448 * 2^s.  With a power of two the scaling
+// the tensor, the smallest from -127 to 119 for which the block's largest magnitude is at most 448 * 2^s (what is above 448 * 2^119, seven eighths
+// of fp32's range, is held as that: twice the scale would have codes that are not finite).  With a power of two the scaling
 // is exact and the code is the only rounding (half to even, at most 2^-4 of the value, or 2^-10 * 2^s below 2^-6 * 2^s); moments are
 // computed in fp32, and the parameter is updated with the moments before they are rounded.  sqrt(v) is kept instead of v because v spans
 // twice as many binades as the 18 that a block's codes do; and a sqrt(v) above zero never becomes a code of zero (it is held as
@@ -209,7 +210,7 @@ template <bool DITHER> __device__ inline Vec<unsigned, 2> encode8(const float (&
         big = fmaxf(big, a < INFINITY ? a : 0.f);
     }
     big = row_max(big);
-    s = big > 0.f ? max(__builtin_amdgcn_frexp_expf(big) - 9 + (__builtin_amdgcn_frexp_mantf(big) > 0.875f ? 1 : 0), -127) : -127;
+    s = big > 0.f ? min(max(__builtin_amdgcn_frexp_expf(big) - 9 + (__builtin_amdgcn_frexp_mantf(big) > 0.875f ? 1 : 0), -127), 119) : -127;
     Vec<unsigned, 2> c;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -217,7 +218,8 @@ template <bool DITHER> __device__ inline Vec<unsigned, 2> encode8(const float (&
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             y[k] = ldexpf(x[4 * w + k], -s);
-            y[k] = fabsf(y[k]) < INFINITY ? (y[k] > 0.f ? fmaxf(y[k], least) : y[k]) : NAN;
+            // (448 is passed only where s is at its limit: what is above 448 * 2^119 would be infinite as the next code)
+            y[k] = fabsf(y[k]) < INFINITY ? (y[k] > 0.f ? __builtin_amdgcn_fmed3f(y[k], least, 448.f) : fmaxf(y[k], -448.f)) : NAN;
         }
         if (DITHER) {
             int r = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], word[4 * w], 0, 0);

@@ -218,3 +218,17 @@ def test_roots_that_have_no_square_in_fp32(ctx, seed):
     big = np.repeat(np.sqrt(v).reshape(-1, BLOCK).max(1), BLOCK)
     assert (np.abs(t.values("v") - np.sqrt(v)) <= (1 / 8 + 1e-6) * np.sqrt(v) + 2.0 ** -9 * big / 224).all()
     assert np.isfinite(t.t["param"].cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("seed", [0, 5])
+def test_moments_at_the_end_of_the_range(ctx, seed):
+    """Gradients of fp32's largest number for many steps: m and sqrt(v) stay finite, and are held as 448 * 2^119 at most."""
+    t = eight(256)
+    t["grad"].fill_(torch.finfo(torch.float32).max)
+    t["grad"][128:] *= -0.9
+    for step in range(1, 6):
+        K.kfac_adamw_batched(ctx.h, [t], lr=1e-3, beta1=0.0, beta2=0.0, step=step, seed=seed)
+        assert bool(torch.isfinite(t["param"]).all())
+        for k in ("m", "v"):
+            assert held(ctx.h, t, k).abs().tolist() == [448 * 2.0 ** 119] * 256 and t[k + "_scale"].tolist() == [246, 246]
+        assert bool((held(ctx.h, t, "m")[128:] < 0).all())
