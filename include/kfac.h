@@ -345,8 +345,9 @@ typedef struct {
 /* Tensors of one call, and the buffers of one tensor, must not overlap.  */
 int kfac_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items /* host */, const kfac_adamw_opts *opts /* host */);
 
-/* What an 8-bit state stands for (for checkpoints, and to go over to fp32 state): out[i] = code[i] * 2^(scale[i / 128] - 127), in fp32 or, as
- * exactly, in bf16.  */
+/* What an 8-bit state stands for (for checkpoints, and to go over to fp32 state): out[i] = code[i] * 2^(scale[i / 128] - 127).  Exact in fp32 for
+ * every scale that a step leaves (up to 246), and in bf16 for those of them from 3 on: below, codes under 2^-133 are rounded half to even, since that is the
+ * smallest number which bf16 has.  */
 int kfac_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype);
 
 /* Update-decoupled schedule (Sec. IV-C, Sec. V-C), host only: at iteration k refresh the factors

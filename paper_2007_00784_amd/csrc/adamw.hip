@@ -30,7 +30,7 @@
 // expectation of m then follows the formula exactly.  That of sqrt(v) does too but for second order: a step's variance, at most |step| times the
 // distance of the codes, goes into v, which with normal gradients is 4 % of v, and its spread takes from the mean root: together 1 % of sqrt(v).
 // The words come from a hash of element, tensor, step and seed, so a call is the same from run to run and a graph whose step is in
-// device memory draws anew at every replay.  268M parameters take 808 us with a seed and 790 without.
+// device memory draws anew at every replay.  268M parameters take 815 us with a seed and 794 without.
 #include <algorithm>
 #include <cmath>
 #include "kfac_internal.h"
@@ -325,7 +325,7 @@ template <bool DITHER> __global__ __launch_bounds__(THREADS) void adamw8_kernel(
     if (it.copy) put(it.copy, true, i, in, p);
 }
 
-// What the 8-bit codes stand for, in fp32 or (exactly: four significant bits) in bf16.
+// What the 8-bit codes stand for, in fp32 or in bf16 (four significant bits, so exactly as long as the last is not below 2^-133: scales from 3 on).
 __global__ __launch_bounds__(THREADS) void adamw_values_kernel(const unsigned char *code, const unsigned char *scale, int64_t n, void *out, int bf) {
     const int64_t i = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * 8;
     const int in = (int)min((int64_t)8, max(n - i, (int64_t)0));

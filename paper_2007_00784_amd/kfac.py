@@ -568,7 +568,8 @@ def kfac_adamw_batched(ctx, items, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_
 
 
 def kfac_adamw_state_values(ctx, codes, scale, out):
-    """out[i] = codes[i] * 2^(scale[i // 128] - 127): what an 8-bit state stands for (m, and sqrt(v)), float32 or bfloat16."""
+    """out[i] = codes[i] * 2^(scale[i // 128] - 127): what an 8-bit state stands for (m, and sqrt(v)), in float32 or
+    bfloat16 (exact there for scales from 3 on; smaller ones have codes below bfloat16's smallest number)."""
     import torch
     n = codes.numel()
     if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or out.numel() != n or scale.dtype != torch.uint8 or scale.numel() != (n + 127) // 128:

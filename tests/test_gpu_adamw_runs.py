@@ -232,3 +232,23 @@ def test_moments_at_the_end_of_the_range(ctx, seed):
         for k in ("m", "v"):
             assert held(ctx.h, t, k).abs().tolist() == [448 * 2.0 ** 119] * 256 and t[k + "_scale"].tolist() == [246, 246]
         assert bool((held(ctx.h, t, "m")[128:] < 0).all())
+
+
+def test_values_of_the_smallest_and_largest_scales(ctx):
+    """Every code with the scales 0 to 4 and 243 to 247: exact in fp32, in bf16 from scale 3 on and the nearest number below.  No step leaves 247: its
+    codes from 256 on are 2^128 and more, above fp32's (and bf16's) largest number."""
+    table = codes_of_e4m3()
+    for scale in (0, 1, 2, 3, 4, 243, 247):
+        codes = torch.arange(256, dtype=torch.uint8, device=DEV)
+        codes[(codes & 127) == 127] = 0
+        scales = torch.full((2,), scale, dtype=torch.uint8, device=DEV)
+        c = codes.cpu().numpy().astype(int)
+        want = torch.from_numpy(np.where(c >= 128, -1.0, 1.0) * table[c & 127] * 2.0 ** (scale - 127))
+        for dt in (torch.float32, torch.bfloat16):
+            out = torch.empty(256, dtype=dt, device=DEV)
+            K.kfac_adamw_state_values(ctx.h, codes, scales, out)
+            # (float64 to float32 is exact here, float32 to bfloat16 rounds half to even)
+            assert torch.equal(out.cpu().double(), want.float().to(dt).double()), (scale, dt)
+            there = want.abs() < 2.0 ** 128
+            assert bool(there.all()) == (scale <= 246)
+            assert scale < 3 or torch.equal(out.cpu().double()[there], want[there])
