@@ -396,6 +396,11 @@ def _on_gpu(*tensors):
             raise ValueError("tensors must be on the GPU")
 
 
+def _c_int(n):
+    """A count as a C int: one that no C int holds (ctypes would cut it to its lower 32 bits) becomes -1, which the library refuses."""
+    return n if -(1 << 31) <= n < 1 << 31 else -1
+
+
 def _rows(t, name, d):
     """(address, row pitch) of a matrix of samples [R][d]: any pitch, but the elements of a row side by side."""
     if t.dim() != 2 or t.shape[1] != d:
@@ -427,7 +432,7 @@ def _expert_desc(weight, offsets, rows, append_ones, dtype):
         raise ValueError("weights without inputs")
     _ptr(weight)                                 # contiguous
     _offsets(offsets, experts)
-    return kfac_expert_desc(experts, rows, wide - ones, d_out, ones, dtype, offsets.data_ptr())
+    return kfac_expert_desc(_c_int(experts), _c_int(rows), _c_int(wide - ones), _c_int(d_out), ones, dtype, offsets.data_ptr())
 
 
 def _same(a, b, names):
@@ -437,7 +442,7 @@ def _same(a, b, names):
 
 def kfac_experts_workspace_bytes(experts, rows, d_in, d_out, append_ones=False, dtype=KFAC_BF16):
     """Bytes of workspace that the products and factors of such a layer make use of (they work with less)."""
-    d = kfac_expert_desc(int(experts), int(rows), int(d_in), int(d_out), int(bool(append_ones)), int(dtype), None)
+    d = kfac_expert_desc(*(_c_int(int(n)) for n in (experts, rows, d_in, d_out)), int(bool(append_ones)), int(dtype), None)
     return int(lib().kfac_experts_workspace_bytes(ctypes.byref(d)))
 
 
@@ -495,7 +500,7 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
     _offsets(offsets, experts)
     _ptr(F)                                      # contiguous
     _on_gpu(X, offsets, F)
-    _check(lib().kfac_update_factors_experts(ctx, experts, X.shape[0], offsets.data_ptr(), xp, _dtype_code(X), ldx, d, ones,
+    _check(lib().kfac_update_factors_experts(ctx, _c_int(experts), _c_int(X.shape[0]), offsets.data_ptr(), xp, _dtype_code(X), ldx, _c_int(d), ones,
                                              int(bool(mean)), float(scale), float(decay), _ptr(F)), "kfac_update_factors_experts")
 
 

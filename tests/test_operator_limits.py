@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2007_00784_amd import kfac as K
 
@@ -13,3 +14,23 @@ def test_seeds():
     for seed in (-1, 1 << 64):
         with pytest.raises(ValueError, match="seed"):
             K.kfac_adamw_batched(CTX, none, lr=1e-3, seed=seed)
+
+
+def test_counts_that_no_c_int_holds(monkeypatch):
+    """2^32 + 5 rows are not five rows: the library gets a number that it refuses (an address that it could read is 64 here, and no launch follows)."""
+    many = (1 << 32) + 5
+    assert K.kfac_experts_workspace_bytes(1, many + 300, 70, 1607) == 0 and K.kfac_experts_workspace_bytes(many, 300, 70, 1607) == 0
+    assert K.kfac_experts_workspace_bytes(1, 300, 70, (1 << 32) + 1607) == 0 and K.kfac_experts_workspace_bytes(1, 300 - (1 << 32), 70, 1607) == 0 and K.kfac_experts_workspace_bytes(1, 300, 70, 1607) > 0
+    monkeypatch.setattr(K, "_on_gpu", lambda *tensors: None)
+    monkeypatch.setattr(K, "_ptr", lambda t: 64)
+    rows = K._rows
+    monkeypatch.setattr(K, "_rows", lambda t, name, d: (128 if name in ("X", "G") else 256, rows(t, name, d)[1]))
+    empty = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device="meta")  # noqa: E731
+    off = torch.zeros(5, dtype=torch.int32)
+    W, X, G = empty(4, 24, 16), empty(many, 16), empty(many, 24)
+    calls = [lambda: K.kfac_experts_forward(CTX, X, W, off, G), lambda: K.kfac_experts_input_grad(CTX, G, W, off, X), lambda: K.kfac_experts_weight_grad(CTX, G, X, off, W),
+             lambda: K.kfac_update_factors_experts(CTX, X, off, torch.empty(4, 16, 16, device="meta"))]
+    for call in calls:
+        with pytest.raises(K.KfacError) as e:
+            call()
+        assert e.value.code == K.KFAC_EINVAL
