@@ -185,6 +185,8 @@ class ExpertRunner:
     NEAREST_STEPS = 8
 
     def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0", seed=1):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
         self.dev = torch.device(device)
         self.experts, self.rows, self.d_in, self.d_out, self.bias, self.damping = experts, rows, d_in, d_out, bool(bias), damping
         self.dt = torch.bfloat16 if bf16 else torch.float32

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2007_00784_amd import kfac as K
+from paper_2007_00784_amd.runner import ExpertRunner
 
 CTX = ctypes.create_string_buffer(4096)
 
@@ -34,3 +35,10 @@ def test_counts_that_no_c_int_holds(monkeypatch):
         with pytest.raises(K.KfacError) as e:
             call()
         assert e.value.code == K.KFAC_EINVAL
+
+
+@pytest.mark.parametrize("bits", [0, 4, 16, 64, "8"])
+def test_bits_of_the_optimizer_state(bits):
+    """Refused before anything is allocated; they used to mean 32."""
+    with pytest.raises(ValueError, match="8 or 32"):
+        ExpertRunner(2, 10, 8, 8, state_bits=bits)
