@@ -173,6 +173,12 @@ class KfacRunner:
         return w
 
 
+def device_of(device):
+    """A device with its number: "cuda" is the current one, for the tensors as for the library's context."""
+    d = torch.device(device)
+    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
 class ExpertRunner:
     """A layer of experts through a training step with the preconditioner: products, both gradients, every expert's factors, their
     eigendecompositions, the preconditioned gradient and the optimizer step that writes the weights which the next products read.
@@ -187,7 +193,7 @@ class ExpertRunner:
     def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0", seed=1):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
-        self.dev = torch.device(device)
+        self.dev = device_of(device)
         self.experts, self.rows, self.d_in, self.d_out, self.bias, self.damping = experts, rows, d_in, d_out, bool(bias), damping
         self.dt = torch.bfloat16 if bf16 else torch.float32
         dA = d_in + int(self.bias)
@@ -213,12 +219,12 @@ class ExpertRunner:
                    K.kfac_experts_workspace_bytes(experts, rows, d_in, d_out, self.bias, K.KFAC_BF16 if bf16 else K.KFAC_F32))
         self.ws = torch.empty(need + 4096, dtype=torch.uint8, device=self.dev)
         self.stream = torch.cuda.current_stream(self.dev)
-        self.ctx = K.kfac_create(self.dev.index or 0, self.stream.cuda_stream, self.ws)
+        self.ctx = K.kfac_create(self.dev.index, self.stream.cuda_stream, self.ws)
         self._adamw = K.adamw_items([dict(param=self.param, grad=self.grad, **state, **(dict(copy=self.weight) if bf16 else {}))])
         self._precond = K.precond_items(list(self.QA), list(self.lamA), list(self.QG), list(self.lamG), damping, list(self.grad))
 
     def close(self):
-        torch.cuda.synchronize()
+        torch.cuda.synchronize(self.dev)
         if self.ctx is not None:
             K.kfac_destroy(self.ctx)
             self.ctx = None

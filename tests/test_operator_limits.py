@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2007_00784_amd import kfac as K
-from paper_2007_00784_amd.runner import ExpertRunner
+from paper_2007_00784_amd.runner import ExpertRunner, device_of
 
 CTX = ctypes.create_string_buffer(4096)
 
@@ -42,3 +42,9 @@ def test_bits_of_the_optimizer_state(bits):
     """Refused before anything is allocated; they used to mean 32."""
     with pytest.raises(ValueError, match="8 or 32"):
         ExpertRunner(2, 10, 8, 8, state_bits=bits)
+
+
+def test_the_device_without_a_number(monkeypatch):
+    """It is the current one, where torch puts the tensors, not the first."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    assert device_of("cuda") == torch.device("cuda", 3) and device_of("cuda:1") == torch.device("cuda", 1) and device_of(torch.device("cuda", 2)).index == 2
