@@ -822,11 +822,11 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
             best = Plan{e, splits};
         }
     };
-    // a split engine: `slots` workgroups run at once; a step of the contraction takes `alone` in a workgroup that has its compute unit to itself
+    // an engine whose sums can go in up to `most` parts: `slots` workgroups run at once; a step of the contraction takes `alone` in a workgroup that has its compute unit to itself
     // and `full` where all slots are taken; parts cost the way to memory and back, and a second launch; `stream`: what
     // reading and writing what the call cannot do without takes, over the rate of a copy
-    auto offer_split = [&](Engine e, double t, double slots, double steps, double alone, double full, double fixed, double stream, size_t part_bytes, size_t grid) {
-        for (int s = 1; s <= MOST_SPLITS && (s == 1 || steps / s >= 4.0); s *= 2) {
+    auto offer_split = [&](Engine e, int most, double t, double slots, double steps, double alone, double full, double fixed, double stream, size_t part_bytes, size_t grid) {
+        for (int s = 1; s <= most && (s == 1 || steps / s >= 4.0); s *= 2) {
             if (s > 1 && (size_t)s * part_bytes * grid > ws) break;
             const double wgs = t * s, units = slots / 256.0, there = std::min(units, std::ceil(wgs / 256.0));     // on the fullest compute unit
             const double step = units > 1.0 ? alone + (full - alone) * (there - 1.0) / (units - 1.0) : alone + (full - alone) * std::min(1.0, wgs / 256.0);
@@ -846,8 +846,8 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
         // us: one 1024 x 1024 layer forward over 4096 rows 27.5 and 15.9; 8 of 4096 x 4096 over 32768 872 and 1175; weight gradient 512 x 512
         // over 32768 rows 654 and 337, in 16 parts 60
         const double slabs = K / WK;
-        offer_split(WIDE, tiles(256, 256), 256, slabs, 1.1, 1.55, 4.0, 1.25, ws + 1, 1);
-        offer_split(WIDE_SMALL, tiles(128, 128), 512, slabs, 0.72, 1.25, 3.0, 1.15, wide_part<4, 4, 2, 2>() * 4, grid_of(g, mode, 128, 128));
+        offer_split(WIDE, 1, tiles(256, 256), 256, slabs, 1.1, 1.55, 4.0, 1.25, 0, 0);
+        offer_split(WIDE_SMALL, MOST_SPLITS, tiles(128, 128), 512, slabs, 0.72, 1.25, 3.0, 1.15, wide_part<4, 4, 2, 2>() * 4, grid_of(g, mode, 128, 128));
         return best;
     }
     // us, in tiles of 32 x 32, of 32 x 64 and (TILES) of 128 x 128: forward 512 x 512 of 8 experts over 64 rows 8.8, 10.0, 26; input
@@ -857,7 +857,7 @@ Plan plan_of(const ExpertArgs &g, int mode, int dtype, size_t ws) {
         offer(DIRECT_SMALL, 1, 6.0 + std::max(hbm, std::max(longest, tiles(32, 32) / 256.0) * K * 0.0085));
         if (mode != FACTORS) offer(DIRECT_MEDIUM, 1, 6.0 + std::max(hbm, std::max(longest, tiles(32, 64) / 256.0) * K * (mode == FORWARD ? 0.0145 : 0.012)));
     }
-    offer_split(TILES, tiles(128, 128), 768, K / BK, 1.36, 3.6, 3.0, 1.0, TILE_PART * 4, grid_of(g, mode, BM, BM));
+    offer_split(TILES, MOST_SPLITS, tiles(128, 128), 768, K / BK, 1.36, 3.6, 3.0, 1.0, TILE_PART * 4, grid_of(g, mode, BM, BM));
     return best;
 }
 

@@ -48,3 +48,16 @@ def test_the_device_without_a_number(monkeypatch):
     """It is the current one, where torch puts the tensors, not the first."""
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
     assert device_of("cuda") == torch.device("cuda", 3) and device_of("cuda:1") == torch.device("cuda", 1) and device_of(torch.device("cuda", 2)).index == 2
+
+
+def test_the_largest_tiles_have_no_parts():
+    """However large the workspace is said to be, the plan is that of the size which the query gives."""
+    f = K.lib().kfac_experts_plan
+    f.argtypes = [ctypes.c_int, ctypes.POINTER(K.kfac_expert_desc), ctypes.c_size_t]
+    for shape in ((8, 39084, 24, 3632), (1, 32768, 512, 512), (2, 6000, 75, 133), (16, 32768, 2048, 2048)):
+        need = K.kfac_experts_workspace_bytes(*shape, True, K.KFAC_BF16)
+        d = ctypes.byref(K.kfac_expert_desc(*shape, 1, K.KFAC_BF16, None))
+        for mode in range(4):
+            for size in ((1 << 63) - 1, (1 << 64) - 1):
+                plan = f(mode, d, size)
+                assert plan == f(mode, d, need) and (plan // 100 != 3 or plan % 100 == 1)
