@@ -210,6 +210,13 @@ __device__ inline void finish(const ExpertArgs &g, int e, int r, int c, float v,
     }
 }
 
+// Between the lanes of a wave LDS goes in program order; this keeps the compiler to that order as well (it may move a lane's load past
+// another address' store).  No instruction comes of it.
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- bf16: the wide engine ----
 //
 // Bound by the matrix core and LDS together where the sums are long (see mfma_gemm_wide.h), by what is written where they are short: 32
@@ -309,6 +316,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
 #pragma unroll
             for (int i = 0; i < FC; ++i)
                 *reinterpret_cast<floatx4 *>(turn + (16 * j + (lane & 15)) * PITCH + 16 * i + 4 * (lane >> 4)) = acc[i][2 * pair + j];
+        wave_order();
         const int r0 = p.m * ROWS + 16 * (wr * FR + 2 * (PHASE == JOIN ? (int)blockIdx.y : pair));
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
@@ -363,6 +371,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
             }
         }
         if (MODE == FACTORS) {
+            wave_order();
             // the mirrored part: lane l takes rows 4 (l % 8).. of column l / 8, which lie side by side there
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
@@ -382,6 +391,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
                     }
             }
         }
+        wave_order();
     }
     if (sums && lane < 16 && (PHASE != JOIN || blockIdx.y == 0)) {
 #pragma unroll
