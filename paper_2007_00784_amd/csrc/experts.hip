@@ -410,8 +410,9 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void expert_wide_kernel(const Expe
 // A workgroup's waves share one tile of (16 RT) x (16 CT) outputs and take turns along the contraction, STEP indices each; their sums are
 // added in a fixed order through LDS.  Nothing is staged: each lane loads what are its own operands of one or several matrix instructions,
 // DEPTH steps of them in flight, so that a tile with a handful of rows streams its weights at the memory's rate, and many small tiles fill
-// the chip.  (8 experts of 2048 x 2048 with a row each: 13.3 us, 59 MB at 4.4 TB/s, a copy runs at 4.9.  fp32 tiles of 32 x 32 have 8
-// operations a byte of L2 traffic, which bounds them.)
+// the chip.  (8 rows on seven of 8 experts 2048 x 2048: 12.7 us, 59 MB at 4.6 TB/s, a copy runs at 4.9.  fp32: what the call waits for
+// are operands and the fullest compute unit: the input gradient of 577 x 512 over 1568 rows, 17.7 us, has its matrix cores busy for 7 and reads 4 to
+// 7 TB/s from the L2, which gives 20 and more.)
 //
 // An operand along the contraction (X, G; W forward): lane l holds index 16 f + l % 16 of fragment f at k = V (l / 16).., V = 16 /
 // sizeof(E) (one v_mfma_f32_16x16x32_bf16, or four v_mfma_f32_16x16x4_f32 of which number t takes element t).  An operand across it (fp32):

@@ -507,7 +507,8 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
 # ---- the optimizer step ----
 def adamw_items(items):
     """The marshalled item array of kfac_adamw_batched for a list of dicts(param, grad, m, v[, m_scale, v_scale][, copy]) of device tensors,
-    reusable while the buffers live; none that is written may occur twice.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or
+    reusable while the buffers live; none that is written may occur twice.  Marshalling takes 4 to 6 us of Python a tensor, for a network's list more
+    than the step itself: a training loop keeps the gradients' buffers, marshals once and hands over the array.  State in 32 bits: m, v float32.  State in 8 bits: m, v float8_e4m3fn (or
     uint8), m_scale, v_scale uint8, one for each 128 elements.  copy: bfloat16, takes the updated parameter."""
     import torch
     code = {torch.float32: KFAC_F32, torch.bfloat16: KFAC_BF16}
