@@ -267,7 +267,7 @@ int kfac_precondition_batched_scaled(kfac_ctx *ctx, int n, const kfac_precond_it
  * or behind offsets[experts]-1 belong to nobody.  Offsets are read as if clamped to [0, rows]; where they descend, which
  * expert's result a row gets is undefined, but nothing outside the matrices is touched.
  * The calls allocate nothing, copy nothing from the host and may be captured into a graph, which reads the offsets anew at every
- * replay.  A few large sums over many rows are cut into parts that meet in the context's workspace (kfac_experts_workspace_bytes());
+ * replay.  Outputs must not share elements with inputs (the columns of one buffer may hold both).  A few large sums over many rows are cut into parts that meet in the context's workspace (kfac_experts_workspace_bytes());
  * with less of it there are fewer parts, and with none the sums are whole: slower, never refused.  (So graphs captured from one
  * context must not run at the same time.)  Sample matrices have a row pitch (in elements, at most 2^20) and may start at any
  * element; a bf16 matrix whose rows all start on 16 bytes is read fastest.
@@ -324,7 +324,8 @@ int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int 
  * step_dev, lr_dev and grad_scale its replays take another step each.  */
 typedef struct {
     void *param;             /* in/out, [n]                                                                */
-    int param_dtype;         /* bf16 parameters are rounded half to even                                  */
+    int param_dtype;         /* bf16 parameters are rounded half to even: what a step moves by less than 2^-9 or so of the
+                                parameter is lost, so training keeps fp32 ones and takes the copy below     */
     const void *grad;        /* [n]                                                                        */
     int grad_dtype;
     void *m, *v;             /* in/out, [n]                                                                */
