@@ -267,10 +267,11 @@ int kfac_precondition_batched_scaled(kfac_ctx *ctx, int n, const kfac_precond_it
  * or behind offsets[experts]-1 belong to nobody.  Offsets are read as if clamped to [0, rows]; where they descend, which
  * expert's result a row gets is undefined, but nothing outside the matrices is touched.
  * The calls allocate nothing, copy nothing from the host and may be captured into a graph, which reads the offsets anew at every
- * replay.  Outputs must not share elements with inputs (the columns of one buffer may hold both).  A few large sums over many rows are cut into parts that meet in the context's workspace (kfac_experts_workspace_bytes());
- * with less of it there are fewer parts, and with none the sums are whole: slower, never refused.  (So graphs captured from one
- * context must not run at the same time.)  Sample matrices have a row pitch (in elements, at most 2^20) and may start at any
- * element; a bf16 matrix whose rows all start on 16 bytes is read fastest.
+ * replay.  Outputs must not share elements with inputs (the columns of one buffer may hold both).  A few large sums over many rows
+ * are cut into parts that meet in the context's workspace (kfac_experts_workspace_bytes()); with less of it there are fewer parts, and
+ * with none the sums are whole: slower, never refused.  (So graphs captured from one context must not run at the same time.)  Sample
+ * matrices have a row pitch (in elements, at most 2^20) and may start at any element; a bf16 matrix whose rows all start on 16 bytes
+ * is read fastest.
  *   append_ones : 1: the weights carry the bias as their last column, as the gradients that kfac_precondition() takes do */
 typedef struct {
     int experts;             /* 1 .. 4096                                                                  */
