@@ -7,6 +7,7 @@ paper_2007_00784_amd.build`` or ``__graft_entry__.build()``); there is no fallba
 """
 import ctypes
 import os
+import warnings
 
 KFAC_OK, KFAC_EINVAL, KFAC_ENOCONV, KFAC_EHIP, KFAC_EWORKSPACE, KFAC_ESCRATCH = 0, -1, -2, -3, -4, -5
 KFAC_F32, KFAC_BF16 = 0, 1
@@ -557,17 +558,32 @@ def _scalar(t, dtype, name):
     return _ptr(t)
 
 
+_told = False
+
+
+def _tell(arr, step):
+    """Says once that a run with 8-bit state has no seed.  (The first steps to nearest do no harm: ExpertRunner.)"""
+    global _told
+    if len(arr) > 0 and arr[0].m_scale and (step is None or step > 8):
+        _told = True
+        warnings.warn("8-bit AdamW state is rounded to nearest without a seed and does not follow its moments over a run: give kfac_adamw_batched() a seed",
+                      RuntimeWarning, stacklevel=3)
+
+
 def kfac_adamw_batched(ctx, items, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1, grad_scale=None, seed=0):
     """One AdamW step over a list of tensors (see adamw_items()).  lr and step: numbers, or device tensors of one float32 / int64 that the call
     reads on the GPU; grad_scale: None or a device tensor of one float32 that every gradient is multiplied with.
     seed (1 .. 2^64 - 1): training with 8-bit state needs one, together with a step that counts on.  Codes are then rounded up or down
-    at random, so that the state follows its moments; with 0 they are rounded half to even, which loses most steps of a run."""
+    at random, so that the state follows its moments; with 0 they are rounded half to even, which loses most steps of a run (and is warned of
+    once, from the ninth step on)."""
     import torch
     if not 0 <= int(seed) < 1 << 64:
         raise ValueError("seed must be 0 .. 2^64 - 1")
     arr = adamw_items(items) if isinstance(items, list) else items
     lr_dev = _scalar(lr, torch.float32, "lr") if torch.is_tensor(lr) else None
     step_dev = _scalar(step, torch.int64, "step") if torch.is_tensor(step) else None
+    if not (seed or _told):
+        _tell(arr, None if step_dev else step)
     o = kfac_adamw_opts(float(beta1), float(beta2), 0.0 if lr_dev else float(lr), float(eps), float(weight_decay), 1 if step_dev else int(step),
                         _scalar(grad_scale, torch.float32, "grad_scale"), lr_dev, step_dev, int(seed))
     _check(lib().kfac_adamw_batched(ctx, len(arr), arr, ctypes.byref(o)), "kfac_adamw_batched")

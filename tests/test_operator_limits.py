@@ -1,5 +1,6 @@
 """What the Python calls for layers of experts and the optimizer step refuse, on the CPU: numbers that the library's types cannot hold."""
 import ctypes
+import warnings
 
 import pytest
 import torch
@@ -61,3 +62,20 @@ def test_the_largest_tiles_have_no_parts():
             for size in ((1 << 63) - 1, (1 << 64) - 1):
                 plan = f(mode, d, size)
                 assert plan == f(mode, d, need) and (plan // 100 != 3 or plan % 100 == 1)
+
+
+def test_a_run_in_8_bits_without_a_seed_is_warned_of_once(monkeypatch):
+    """(The item is refused by the library, which is behind the warning.)"""
+    def step(told, eight, **kw):
+        monkeypatch.setattr(K, "_told", told)
+        arr = (K.kfac_adamw_item * 1)(K.kfac_adamw_item(n=-1, m_scale=4096 if eight else None, v_scale=4096 if eight else None))
+        with warnings.catch_warnings(record=True) as seen:
+            warnings.simplefilter("always")
+            with pytest.raises(K.KfacError):
+                K.kfac_adamw_batched(CTX, arr, lr=1e-3, **kw)
+        return [w.category for w in seen], K._told
+
+    assert step(False, True, step=9) == ([RuntimeWarning], True)
+    assert step(True, True, step=10) == ([], True)
+    for eight, kw in ((True, dict(step=9, seed=1)), (True, dict(step=8)), (False, dict(step=1000))):
+        assert step(False, eight, **kw) == ([], False)
