@@ -99,8 +99,9 @@ __device__ inline void adam(const Hyper &h, float g, float root, float &m, float
 }
 __device__ inline float next_v(const Hyper &h, float g, float v) { return fmaf(h.b2, v, h.c2 * g * g); }
 // sqrt(v) of this step from that of the last, which need not have a square in fp32 (below 2^-75, from 2^64 on): both terms are brought to a size
-// near one by a power of two first, which changes no bit of what can be squared.
+// near one by a power of two first, which changes no bit of what can be squared.  (With beta2 = 0 the last root does not count: 0, or NaN.)
 __device__ inline float next_root(const Hyper &h, float g, float root) {
+    root = h.b2 > 0.f ? root : root - root;
     const int e = __builtin_amdgcn_frexp_expf(fmaxf(fabsf(g), fabsf(root)));      // (0 for a zero and what is not finite)
     const float x = ldexpf(root, -e);
     return ldexpf(sqrtf(next_v(h, ldexpf(g, -e), x * x)), e);

@@ -252,3 +252,13 @@ def test_values_of_the_smallest_and_largest_scales(ctx):
             there = want.abs() < 2.0 ** 128
             assert bool(there.all()) == (scale <= 246)
             assert scale < 3 or torch.equal(out.cpu().double()[there], want[there])
+
+
+def test_a_large_root_that_does_not_count(ctx):
+    """beta2 = 0: the root is the gradient's size, however large the last one was."""
+    t = eight(256)
+    t["v"].fill_(0x38)                                       # 1
+    t["v_scale"].fill_(127 + 60)
+    t["grad"].fill_(-2.0 ** -20)
+    K.kfac_adamw_batched(ctx.h, [t], lr=1e-3, beta2=0.0, step=2)
+    assert held(ctx.h, t, "v").tolist() == [2.0 ** -20] * 256
