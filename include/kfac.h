@@ -308,6 +308,78 @@ int kfac_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *desc, const 
 int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets /* device */, const void *X, int dtype, int64_t ldx, int d,
                                 int append_ones, int mean, float scale, float decay, float *F);
 
+/* ---- tokens to experts and back ----------------------------------------------------------------------------------
+ * What stands in front of and behind the products of a layer of experts.  Token t has topk slots (t, j); slot (t, j) is for expert ids[t][j],
+ * or for none where that is outside 0 .. experts - 1.  The same expert may occur twice.  Like the products, the calls allocate nothing,
+ * copy nothing from the host and may be captured into a graph; matrices have a row pitch in elements (at most 2^20) and may start at any element, and outputs
+ * must not share elements with inputs unless said so.  All sums are in fp32 in a fixed order: results are the same from run to run.  */
+
+/* The router's choice.  p = softmax(logits[t]) over the experts; ids[t] = the topk experts of the largest logits, in descending order, ties to the lowest
+ * index; weights[t][j] = p of ids[t][j], or with normalize = 1 that over the sum of all topk of them.
+ * A logit of -inf (an expert out of use, all of a padded token's) has p = 0 and is never chosen: where nothing else is left the id is -1
+ * and the weight 0.  A NaN counts as +inf, the first to be chosen, and a token with either has weights that are NaN.
+ *   tokens * topk < 2^28, 1 <= experts <= 4096, 1 <= topk <= 64 and <= experts;  logits [tokens][experts] with pitch ldl, dtype
+ *   ids [tokens][topk], weights [tokens][topk] fp32: written  */
+int kfac_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize, int *ids, float *weights);
+
+/* The gradient of the logits from that of the weights (ids and normalize as they were; the choice itself has no gradient):
+ *   normalize = 0: dlogits_e = p_e (sum over j with ids_j = e of dweights_j  -  sum_j p_{ids_j} dweights_j)
+ *   normalize = 1: dlogits at ids_j = w_j (dweights_j - sum_i w_i dweights_i), 0 for an expert that was not chosen
+ * Slots without an expert do not count.  dlogits [tokens][experts] with pitch ldd, of the logits' dtype: written, rounded once.  */
+int kfac_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, const int *ids /* device */,
+                            const float *dweights, int normalize, void *dlogits, int64_t ldd);
+
+typedef struct {
+    int tokens, topk;        /* tokens * topk < 2^28, 1 <= topk <= 64                                      */
+    int rows;                /* of the experts' sample matrices; below 2^28, at least tokens * topk for kfac_experts_dispatch()   */
+    int d;                   /* 1 .. 65536                                                                 */
+    int dtype;               /* of X, Xs, Y, Ys and their gradients                                        */
+} kfac_slot_desc;
+
+/* Sorts the slots by expert and copies the tokens there: offsets[e] .. offsets[e+1] - 1 are the rows of expert e, in the order of their slots (t, then j),
+ * rows[t][j] the row of slot (t, j) or -1, and Xs[rows[t][j]] = X[t].  offsets and Xs are what the products for layers of experts take.
+ *   ids [tokens][topk];  offsets [experts + 1], rows [tokens][topk]: written;  X [tokens][d] with pitch ldx, Xs [rows][d] with pitch lds
+ *   X = Xs = NULL: the order alone (d and the pitches are not looked at).  Rows of Xs from offsets[experts] on are left as they were.
+ * More than 1024 slots make use of kfac_experts_dispatch_workspace_bytes() of the context's workspace; with less of it the sort takes longer.  */
+int kfac_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *desc, int experts, const int *ids /* device */, const void *X, int64_t ldx, int *offsets, int *rows,
+                          void *Xs, int64_t lds);
+size_t kfac_experts_dispatch_workspace_bytes(int tokens, int topk, int experts);
+
+/* Xs[rows[t][j]] = X[t] with rows as kfac_experts_dispatch() left them: the sorted tokens once more, for a backward pass that did not keep them.
+ * (Here and below a slot whose row is outside 0 .. desc->rows - 1 is one without an expert.  The rows of a call must differ.)  */
+int kfac_experts_gather(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows /* device */, const void *X, int64_t ldx, void *Xs, int64_t lds);
+
+/* Y[t] = add[t] + sum_j weights[t][j] Ys[rows[t][j]], rounded once.  Slots without an expert count for nothing, whatever their weight is.
+ *   weights : NULL: ones.  That is the gradient of kfac_experts_dispatch(): dX[t] = sum_j dXs[rows[t][j]]
+ *   add     : [tokens][d] with pitch lda, e.g. the residual, or a gradient that the tokens have already; may be Y itself (with its pitch); NULL: zero  */
+int kfac_experts_combine(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows /* device */, const float *weights, const void *Ys, int64_t ldys,
+                         const void *add, int64_t lda, void *Y, int64_t ldy);
+
+/* The gradients of that sum (the one of add is dY itself):  dYs[rows[t][j]] = weights[t][j] dY[t],  dweights[t][j] = <dY[t], Ys[rows[t][j]]>, 0 for a slot
+ * without an expert.  Rows of dYs that no slot has are left as they were.  */
+int kfac_experts_combine_grad(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows /* device */, const float *weights, const void *dY, int64_t lddy,
+                              const void *Ys, int64_t ldys, void *dYs, int64_t lddys, float *dweights);
+
+/* ---- the global gradient norm ------------------------------------------------------------------------------------
+ *   norm = |s| sqrt(sum over all tensors of grad^2),   coef = s min(1, max_norm / norm),   s = *grad_scale (1 if NULL), e.g. one over the loss scale
+ * Squares and sums in 64 bits, in a fixed order; nothing is copied to the host.  coef is what kfac_adamw_batched() takes as grad_scale, so that a step of
+ * AdamW needs no pass of its own for clipping.  A norm that is NaN makes coef NaN; an infinite one (a gradient is) makes it 0 (if max_norm is finite).  */
+typedef struct {
+    const void *grad;        /* [n]                                                                        */
+    int grad_dtype;
+    void *out;               /* kfac_clip_grads_batched(): grad itself (of the same dtype) or a buffer of its own; kfac_grad_norm_batched(): not looked at */
+    int out_dtype;
+    int64_t n;               /* may be 0                                                                   */
+} kfac_grad_item;
+/*   max_norm : > 0; infinite: coef is s.   norm, coef : DEVICE pointers to one float each, written; coef may be NULL
+ * Workspace: kfac_grad_norm_workspace_bytes() (16 KB for each 100 tensors at most).  */
+int kfac_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items /* host */, float max_norm, const float *grad_scale /* device */, float *norm, float *coef);
+size_t kfac_grad_norm_workspace_bytes(int n, const kfac_grad_item *items /* host; no pointer is looked at */);
+
+/* The same, and out = coef * grad for every tensor (one product in fp32, rounded once to out_dtype); a tensor that is its own output is not touched
+ * where coef is 1.  Outputs must not overlap one another, nor gradients other than their own.  norm and coef must not be NULL.  */
+int kfac_clip_grads_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items /* host */, float max_norm, const float *grad_scale /* device */, float *norm, float *coef);
+
 /* ---- the optimizer step behind the preconditioner --------------------------------------------------------------
  * The preconditioned gradient stands in place and any optimizer may follow (Listing 1); this is AdamW over a list of tensors:
  *   g = grad * grad_scale;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2

@@ -34,6 +34,9 @@
 #include <algorithm>
 #include <cmath>
 #include "kfac_internal.h"
+#include "elements.h"
+
+using namespace kfac;
 
 namespace {
 
@@ -107,24 +110,6 @@ __device__ inline float next_root(const Hyper &h, float g, float root) {
     return ldexpf(sqrtf(next_v(h, ldexpf(g, -e), x * x)), e);
 }
 
-// N consecutive elements from anywhere: tensors may start at any element, and the loads are as wide as N allows all the same (global memory
-// takes unaligned vectors).
-template <typename T, int N> struct Vec { T x[N]; };
-template <typename T, int N> __device__ inline Vec<T, N> load(const void *p, int64_t i) {
-    Vec<T, N> r;
-    __builtin_memcpy(&r, (const char *)p + i * (int64_t)sizeof(T), sizeof(r));
-    return r;
-}
-template <typename T, int N> __device__ inline void store(void *p, int64_t i, const Vec<T, N> &r) {
-    __builtin_memcpy((char *)p + i * (int64_t)sizeof(T), &r, sizeof(r));
-}
-__device__ inline float widen(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
-__device__ inline unsigned short round_bf16(float x) {   // half to even; NaN stays NaN
-    const unsigned u = __float_as_uint(x);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (unsigned short)((u >> 16) | 0x40u);
-    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-}
-
 // N elements from i on as fp32, or in bf16; `in` of them exist (N: all, as one vector).
 template <int N> __device__ inline void fetch(const void *p, bool bf, int64_t i, int in, float (&x)[N]) {
     if (in == N) {
@@ -166,15 +151,6 @@ template <int N> __device__ inline void put(void *p, bool bf, int64_t i, int in,
 }
 
 // ---- 8-bit state: eight elements a thread, so sixteen lanes (one row of the cross-lane moves) hold a block ----
-__device__ inline float row_max(float x) {
-#define KFAC_ROW_STEP(ctrl) x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 0xf, 0xf, true)))
-    KFAC_ROW_STEP(0xB1);     // lanes 1 0 3 2
-    KFAC_ROW_STEP(0x4E);     // lanes 2 3 0 1
-    KFAC_ROW_STEP(0x141);    // the other four of each eight
-    KFAC_ROW_STEP(0x140);    // the other eight of the sixteen
-#undef KFAC_ROW_STEP
-    return x;
-}
 __device__ inline void decode8(const Vec<unsigned, 2> &c, int s, float (&x)[8]) {
 #pragma unroll
     for (int w = 0; w < 2; ++w) {

@@ -309,7 +309,7 @@ int kfac_profile_end(kfac_ctx *ctx, kfac_kernel_stat *out, int max, int *n) {
                                           "eig_pivot_solve", "eig_apply", "eig_misc", "eig_post_gemm", "eig_copy", "eig_outer_cols",
                                           "precond_scale", "syrk_bf16", "precond_gemm_split", "eig_outer_rows", "factor_inverse",
                                           "eig_reduce_mv", "eig_reduce_vec", "eig_reduce_update", "eig_tridiag_solve", "eig_back",
-                                          "experts", "experts_bf16", "adamw"};
+                                          "experts", "experts_bf16", "adamw", "experts_route", "experts_tokens", "grad_norm"};
     ctx->prof_on = false;
     KFAC_HIP_CHECK(hipStreamSynchronize(ctx->stream));
     kfac_kernel_stat acc[KC_COUNT] = {};
@@ -416,6 +416,122 @@ int kfac_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int 
     const KfacDeviceScope dev(ctx->device);
     if (!dev.ok) return KFAC_EHIP;
     return kfac_launch_update_factors_experts(ctx, experts, rows, offsets, X, dtype, ldx, d, append_ones, mean, scale, decay, F);
+}
+
+static bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
+
+static bool valid_router(int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize) {
+    if (tokens < 0 || experts < 1 || experts > KFAC_MAX_EXPERTS || topk < 1 || topk > KFAC_MAX_TOPK || topk > experts) return false;
+    return (int64_t)tokens * topk < KFAC_MAX_EXPERT_ROWS && (tokens == 0 || logits) && valid_dtype(dtype) && valid_pitch(ldl, experts) && (normalize == 0 || normalize == 1);
+}
+
+int kfac_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize, int *ids, float *weights) {
+    if (!ctx || !valid_router(tokens, experts, topk, logits, dtype, ldl, normalize)) return KFAC_EINVAL;
+    if (tokens == 0) return KFAC_OK;
+    if (!ids || !weights || !aligned4(ids) || !aligned4(weights) || (void *)ids == logits || (void *)weights == logits || (void *)ids == (void *)weights) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_route(ctx, tokens, experts, topk, logits, dtype, ldl, normalize, ids, weights);
+}
+
+int kfac_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, const int *ids, const float *dweights,
+                            int normalize, void *dlogits, int64_t ldd) {
+    if (!ctx || !valid_router(tokens, experts, topk, logits, dtype, ldl, normalize) || !valid_pitch(ldd, experts)) return KFAC_EINVAL;
+    if (tokens == 0) return KFAC_OK;
+    if (!ids || !dweights || !dlogits || !aligned4(ids) || !aligned4(dweights)) return KFAC_EINVAL;
+    if (dlogits == logits || dlogits == (const void *)ids || dlogits == (const void *)dweights) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_route_grad(ctx, tokens, experts, topk, logits, dtype, ldl, ids, dweights, normalize, dlogits, ldd);
+}
+
+static bool valid_slots(const kfac_slot_desc *d, bool columns = true) {
+    if (!d || d->tokens < 0 || d->topk < 1 || d->topk > KFAC_MAX_TOPK || (int64_t)d->tokens * d->topk >= KFAC_MAX_EXPERT_ROWS) return false;
+    if (d->rows < 0 || d->rows >= KFAC_MAX_EXPERT_ROWS || !valid_dtype(d->dtype)) return false;
+    return !columns || (d->d >= 1 && d->d <= KFAC_MAX_EXPERT_D);
+}
+
+size_t kfac_experts_dispatch_workspace_bytes(int tokens, int topk, int experts) {
+    if (tokens < 0 || topk < 1 || topk > KFAC_MAX_TOPK || (int64_t)tokens * topk >= KFAC_MAX_EXPERT_ROWS || experts < 1 || experts > KFAC_MAX_EXPERTS) return 0;
+    return kfac_experts_dispatch_ws_bytes_impl(tokens, topk, experts);
+}
+
+int kfac_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *desc, int experts, const int *ids, const void *X, int64_t ldx, int *offsets, int *rows, void *Xs, int64_t lds) {
+    const bool copies = X || Xs;
+    if (!ctx || !valid_slots(desc, copies) || experts < 1 || experts > KFAC_MAX_EXPERTS || !offsets || !aligned4(offsets)) return KFAC_EINVAL;
+    if (copies && (!valid_pitch(ldx, desc->d) || !valid_pitch(lds, desc->d))) return KFAC_EINVAL;
+    if ((int64_t)desc->tokens * desc->topk > desc->rows) return KFAC_EINVAL;
+    if (desc->tokens > 0) {
+        if (!ids || !rows || !aligned4(ids) || !aligned4(rows) || ids == rows || ids == offsets || rows == offsets) return KFAC_EINVAL;
+        if (copies && (!X || !Xs || X == Xs || X == rows || X == offsets || Xs == ids || Xs == rows || Xs == offsets)) return KFAC_EINVAL;
+    }
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_dispatch(ctx, desc, experts, ids, desc->tokens > 0 ? X : nullptr, ldx, offsets, rows, Xs, lds);
+}
+
+int kfac_experts_gather(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows, const void *X, int64_t ldx, void *Xs, int64_t lds) {
+    if (!ctx || !valid_slots(desc) || !valid_pitch(ldx, desc->d) || !valid_pitch(lds, desc->d)) return KFAC_EINVAL;
+    if (desc->tokens == 0 || desc->rows == 0) return KFAC_OK;
+    if (!rows || !aligned4(rows) || !X || !Xs || X == Xs || Xs == rows) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_gather(ctx, desc, rows, X, ldx, Xs, lds);
+}
+
+int kfac_experts_combine(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows, const float *weights, const void *Ys, int64_t ldys, const void *add, int64_t lda,
+                         void *Y, int64_t ldy) {
+    if (!ctx || !valid_slots(desc) || !valid_pitch(ldys, desc->d) || !valid_pitch(ldy, desc->d) || (add && !valid_pitch(lda, desc->d))) return KFAC_EINVAL;
+    if (desc->tokens == 0) return KFAC_OK;
+    if (!rows || !aligned4(rows) || !aligned4(weights) || !Y || (desc->rows > 0 && !Ys) || Y == Ys || Y == rows || Y == (const void *)weights) return KFAC_EINVAL;
+    if (add == Y && lda != ldy) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_combine(ctx, desc, rows, weights, Ys, ldys, add, lda, Y, ldy);
+}
+
+int kfac_experts_combine_grad(kfac_ctx *ctx, const kfac_slot_desc *desc, const int *rows, const float *weights, const void *dY, int64_t lddy, const void *Ys, int64_t ldys,
+                              void *dYs, int64_t lddys, float *dweights) {
+    if (!ctx || !valid_slots(desc) || !valid_pitch(lddy, desc->d) || !valid_pitch(ldys, desc->d) || !valid_pitch(lddys, desc->d)) return KFAC_EINVAL;
+    if (desc->tokens == 0) return KFAC_OK;
+    if (!rows || !weights || !dweights || !aligned4(rows) || !aligned4(weights) || !aligned4(dweights) || !dY || (desc->rows > 0 && (!Ys || !dYs))) return KFAC_EINVAL;
+    for (const void *in : {(const void *)rows, (const void *)weights, dY, Ys})
+        if (in && (in == dYs || in == (const void *)dweights)) return KFAC_EINVAL;
+    if (dYs == (void *)dweights) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_experts_combine_grad(ctx, desc, rows, weights, dY, lddy, Ys, ldys, dYs, lddys, dweights);
+}
+
+static bool valid_grads(int n, const kfac_grad_item *items, bool pointers, bool out) {
+    if (n < 0 || (n > 0 && !items)) return false;
+    for (int i = 0; i < n; ++i) {
+        const kfac_grad_item &t = items[i];
+        if (t.n < 0 || !valid_dtype(t.grad_dtype) || (out && !valid_dtype(t.out_dtype))) return false;
+        if (!pointers || t.n == 0) continue;
+        if (!t.grad || (out && !t.out) || (out && t.out == t.grad && t.out_dtype != t.grad_dtype)) return false;
+    }
+    return true;
+}
+
+size_t kfac_grad_norm_workspace_bytes(int n, const kfac_grad_item *items) {
+    return valid_grads(n, items, false, false) ? kfac_grad_norm_ws_bytes_impl(n, items) : 0;
+}
+
+int kfac_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef) {
+    if (!ctx || !valid_grads(n, items, true, false) || !(max_norm > 0.f) || !norm || norm == coef || norm == grad_scale) return KFAC_EINVAL;
+    if (!aligned4(norm) || !aligned4(coef) || !aligned4(grad_scale)) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_grad_norm_batched(ctx, n, items, max_norm, grad_scale, norm, coef, false);
+}
+
+int kfac_clip_grads_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef) {
+    if (!ctx || !valid_grads(n, items, true, true) || !(max_norm > 0.f) || !norm || !coef || norm == coef || norm == grad_scale || coef == grad_scale) return KFAC_EINVAL;
+    if (!aligned4(norm) || !aligned4(coef) || !aligned4(grad_scale)) return KFAC_EINVAL;
+    const KfacDeviceScope dev(ctx->device);
+    if (!dev.ok) return KFAC_EHIP;
+    return kfac_launch_grad_norm_batched(ctx, n, items, max_norm, grad_scale, norm, coef, true);
 }
 
 int kfac_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items, const kfac_adamw_opts *o) {

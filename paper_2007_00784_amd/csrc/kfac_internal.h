@@ -20,7 +20,7 @@ enum KfacKernelClass {
     KC_UNFOLD = 0, KC_SYRK, KC_SYRK_REDUCE, KC_PRECOND_GEMM, KC_EIG_SMALL, KC_EIG_SOLVE, KC_EIG_APPLY,
     KC_EIG_MISC, KC_EIG_POST, KC_EIG_COPY, KC_EIG_OUTER, KC_PRECOND_SCALE, KC_SYRK_B16, KC_PRECOND_GEMM_X3, KC_EIG_OUTER_ROWS, KC_INVERSE,
     KC_EIG_REDUCE_MV, KC_EIG_REDUCE_VEC, KC_EIG_REDUCE_GEMM, KC_EIG_TRI, KC_EIG_BACK,
-    KC_EXPERTS, KC_EXPERTS_B16, KC_ADAMW, KC_COUNT
+    KC_EXPERTS, KC_EXPERTS_B16, KC_ADAMW, KC_ROUTE, KC_TOKENS, KC_NORM, KC_COUNT
 };
 struct KfacProfRec { int cls; hipEvent_t t0, t1; double flops, bytes, share; };   // share: of the launch's time
 
@@ -120,6 +120,7 @@ constexpr int KFAC_EIG_B = 32;       // block size of the blocked Jacobi path (s
 constexpr int KFAC_MAX_D = 8192;
 constexpr int KFAC_MAX_EXPERTS = 4096;
 constexpr int KFAC_MAX_EXPERT_ROWS = 1 << 28;
+constexpr int KFAC_MAX_TOPK = 64;          // slots of a token
 constexpr int KFAC_MAX_EXPERT_D = 65536;   // sides of an expert's weights
 constexpr int64_t KFAC_MAX_PITCH = 1 << 20; // elements between the rows of samples: 32-bit offsets inside a tile
 constexpr int KFAC_EIG_SPLIT_MIN = 2048;   // factors from here on use split-fp16 products where an option allows them
@@ -176,6 +177,19 @@ int kfac_launch_experts_weight_grad(kfac_ctx *ctx, const kfac_expert_desc *d, co
 int kfac_launch_update_factors_experts(kfac_ctx *ctx, int experts, int rows, const int *offsets, const void *X, int dtype, int64_t ldx, int d, int append_ones,
                                        int mean, float scale, float decay, float *F);
 size_t kfac_experts_ws_bytes_impl(const kfac_expert_desc *d);
+int kfac_launch_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize, int *ids, float *weights);
+int kfac_launch_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, const int *ids, const float *dweights,
+                                   int normalize, void *dlogits, int64_t ldd);
+size_t kfac_experts_dispatch_ws_bytes_impl(int tokens, int topk, int experts);
+int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int experts, const int *ids, const void *X, int64_t ldx, int *offsets, int *rows, void *Xs,
+                                 int64_t lds);
+int kfac_launch_experts_gather(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const void *X, int64_t ldx, void *Xs, int64_t lds);
+int kfac_launch_experts_combine(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const float *weights, const void *Ys, int64_t ldys, const void *add, int64_t lda,
+                                void *Y, int64_t ldy);
+int kfac_launch_experts_combine_grad(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const float *weights, const void *dY, int64_t lddy, const void *Ys,
+                                     int64_t ldys, void *dYs, int64_t lddys, float *dweights);
+size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items);
+int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef, bool clip);
 int kfac_launch_adamw_batched(kfac_ctx *ctx, int n, const kfac_adamw_item *items, const kfac_adamw_opts *opts);
 int kfac_launch_adamw_state_values(kfac_ctx *ctx, const void *codes, const unsigned char *scale, int64_t n, void *out, int dtype);
 int kfac_launch_eig(kfac_ctx *ctx, int batch, const float *const *F, const int *d, float *const *Q,

@@ -1,0 +1,776 @@
+// Tokens to experts and back: the router's choice with its gradient, tokens sorted by expert, the weighted sum of the experts' results
+// with its gradients.  Token t has k slots s = t k + j, each for an expert ids[s] or for none, and the sample matrices of the products for
+// layers of experts have one row for each slot that has an expert: those of expert 0 first, each expert's in the order of the slots.
+//
+//   route         ids = the k largest of p = softmax(logits[t]), weights p[ids] (or those over their sum)
+//   route_grad    dlogits = p (.) (dw at ids - <p, dw>)
+//   dispatch      offsets, rows[s], Xs[rows[s]] = X[t]
+//   combine       Y[t] = add[t] + sum_j w[s] Ys[rows[s]]
+//   combine_grad  dYs[rows[s]] = w[s] dY[t],  dw[s] = <dY[t], Ys[rows[s]]>
+//
+// Everything is bound by memory (training batches) or by the length of a launch's chain of loads (single tokens).
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include "kfac_internal.h"
+#include "elements.h"
+
+using namespace kfac;
+
+namespace {
+
+constexpr int THREADS = 256;
+
+// ---------------------------------------------------------------- the router's choice
+// A group of L lanes takes a token, each lane V consecutive logits, so what has to cross lanes is one value a choice.
+
+template <int L> __device__ inline float group_max(float x) {
+    if (L >= 16) {
+        x = row_max(x);
+#pragma unroll
+        for (int m = 16; m < L; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+    } else {
+#pragma unroll
+        for (int m = 1; m < L; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+    }
+    return x;
+}
+template <int L> __device__ inline int group_min(int x) {
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) x = min(x, __shfl_xor(x, m));
+    return x;
+}
+template <int L> __device__ inline float group_sum(float x) {
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) x += __shfl_xor(x, m);
+    return x;
+}
+
+// The logits base .. base + V - 1 of a token, -inf behind the last.  A NaN counts as +inf: it is chosen first, and every weight becomes NaN by
+// the difference of two infinities.
+template <typename T, int V> __device__ inline void logits_of(const void *p, int64_t row, int base, int E, bool in, float (&x)[V]) {
+    constexpr int N = V * (int)sizeof(T) < 16 ? V : 16 / (int)sizeof(T);
+    if (in && base + V <= E) {
+#pragma unroll
+        for (int u = 0; u < V; u += N) {
+            const auto r = load<T, N>(p, row + base + u);
+#pragma unroll
+            for (int v = 0; v < N; ++v) x[u + v] = value_of(r.x[v]);
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = in && base + v < E ? value_of(((const T *)p)[row + base + v]) : -INFINITY;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = x[v] == x[v] ? x[v] : INFINITY;
+}
+
+struct RouteArgs {
+    const void *logits;
+    int64_t ldl;
+    int T, E, k, normalize;
+    int *ids;
+    float *weights;
+};
+
+template <typename T, int L, int V> __global__ __launch_bounds__(THREADS) void route_kernel(const RouteArgs g) {
+    constexpr int C = L >= 64 ? 1 : 4;                   // choices of a token in a lane (k <= 64, and at most E)
+    const int lane = threadIdx.x % L, base = lane * V;
+    const int64_t t = (int64_t)blockIdx.x * (THREADS / L) + threadIdx.x / L;
+    const bool in = t < g.T;
+    float x[V];
+    logits_of<T, V>(g.logits, t * g.ldl, base, g.E, in, x);
+    float top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) top = fmaxf(top, x[v]);
+    top = group_max<L>(top);
+    float total = 0.f;
+    if (!g.normalize) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) total += expf(x[v] - top);
+        total = group_sum<L>(total);
+    }
+    int id[C];
+    float w[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        id[c] = -1;
+        w[c] = 0.f;
+        for (int j = c * L; j < min(g.k, (c + 1) * L); ++j) {
+            float best = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < V; ++v) best = fmaxf(best, x[v]);
+            best = group_max<L>(best);
+            int e = INT_MAX;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) e = x[v] == best ? base + v : e;
+            e = group_min<L>(e);
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = base + v == e ? -INFINITY : x[v];
+            if (j - c * L == lane && best > -INFINITY) {
+                id[c] = e;
+                w[c] = expf(best - top);
+            }
+        }
+    }
+    if (g.normalize) {
+        float sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum += w[c];
+        total = group_sum<L>(sum);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int j = c * L + lane;
+        if (in && j < g.k) {
+            g.ids[t * g.k + j] = id[c];
+            g.weights[t * g.k + j] = id[c] >= 0 ? w[c] / total : 0.f;
+        }
+    }
+}
+
+struct RouteGradArgs {
+    const void *logits;
+    int64_t ldl;
+    int T, E, k, normalize;
+    const int *ids;
+    const float *dw;
+    void *out;
+    int64_t ldo;
+};
+
+template <typename T, int L, int V> __global__ __launch_bounds__(THREADS) void route_grad_kernel(const RouteGradArgs g) {
+    constexpr int N = V * (int)sizeof(T) < 16 ? V : 16 / (int)sizeof(T);
+    const int lane = threadIdx.x % L, base = lane * V;
+    const int64_t t = (int64_t)blockIdx.x * (THREADS / L) + threadIdx.x / L;
+    const bool in = t < g.T;
+    float x[V], d[V];                                    // p, and what the choices add to the gradient of p, or of the logits
+#pragma unroll
+    for (int v = 0; v < V; ++v) d[v] = 0.f;
+    if (g.normalize) {
+        // the softmax over the choices: its sums first, then each choice's share
+        const T *row = (const T *)g.logits + t * g.ldl;
+        const auto logit = [](T x) { const float y = value_of(x); return y == y ? y : INFINITY; };
+        float top = -INFINITY, sum = 0.f, inner = 0.f;
+        for (int j = lane; in && j < g.k; j += L) {
+            const int e = g.ids[t * g.k + j];
+            if ((unsigned)e < (unsigned)g.E) top = fmaxf(top, logit(row[e]));
+        }
+        top = group_max<L>(top);
+        const bool some = top > -INFINITY;               // (else there is nothing to share)
+        for (int j = lane; in && some && j < g.k; j += L) {
+            const int e = g.ids[t * g.k + j];
+            if ((unsigned)e >= (unsigned)g.E) continue;
+            const float y = expf(logit(row[e]) - top);
+            sum += y;
+            inner = fmaf(y, g.dw[t * g.k + j], inner);
+        }
+        sum = group_sum<L>(sum);
+        inner = group_sum<L>(inner) / sum;
+        for (int j = 0; in && some && j < g.k; ++j) {
+            const int e = g.ids[t * g.k + j];
+            if ((unsigned)e >= (unsigned)g.E) continue;
+            const float y = expf(logit(row[e]) - top) / sum * (g.dw[t * g.k + j] - inner);
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] += base + v == e ? y : 0.f;
+        }
+    } else {
+        logits_of<T, V>(g.logits, t * g.ldl, base, g.E, in, x);
+        float top = -INFINITY, sum = 0.f, inner = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) top = fmaxf(top, x[v]);
+        top = group_max<L>(top);
+        const bool some = top > -INFINITY;               // (all masked: the gradient is zero)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] = some ? expf(x[v] - top) : 0.f;
+            sum += x[v];
+        }
+        sum = group_sum<L>(sum);
+        for (int j = 0; in && j < g.k; ++j) {
+            const int e = g.ids[t * g.k + j];
+            const float y = g.dw[t * g.k + j];
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] += base + v == e ? y : 0.f;
+        }
+        const float over = some ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] *= over;
+            inner = fmaf(x[v], d[v], inner);
+        }
+        inner = group_sum<L>(inner);
+#pragma unroll
+        for (int v = 0; v < V; ++v) d[v] = x[v] * (d[v] - inner);
+    }
+    if (!in) return;
+    const int64_t at = t * g.ldo + base;
+    if (base + V <= g.E) {
+#pragma unroll
+        for (int u = 0; u < V; u += N) {
+            Vec<T, N> r;
+#pragma unroll
+            for (int v = 0; v < N; ++v) r.x[v] = element_of<T>(d[u + v]);
+            store(g.out, at + u, r);
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (base + v < g.E) ((T *)g.out)[at + v] = element_of<T>(d[v]);
+    }
+}
+
+// ---------------------------------------------------------------- the order of the slots
+struct SortArgs {
+    const int *ids;
+    int S, E, k;             // slots, experts, slots of a token
+    int per, runs;           // slots of a run (a wave's, multiple of 64), runs
+    int *offsets;            // [E + 1]
+    int *rows;               // [S]
+    int *base;               // [runs][E]: slots of the expert in a run, then the row of the first of them
+};
+
+__device__ inline int expert_of(int id, int E) { return (unsigned)id < (unsigned)E ? id : E; }
+
+// Each wave counts its run's slots by expert and leaves at rows[s] how many of its own expert are in front of s in the run.  Sixty-four
+// slots at a time: the lanes of one expert are found by the ballots of its number's bits, the counts before stand in LDS.
+__global__ __launch_bounds__(THREADS) void sort_count_kernel(const SortArgs g) {
+    extern __shared__ int shared[];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int run = blockIdx.x * (blockDim.x >> 6) + wave;
+    int *const seen = shared + wave * (g.E + 1);
+    for (int e = lane; e <= g.E; e += 64) seen[e] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)run * g.per;
+    if (run < g.runs) {
+        const int bits = 32 - __builtin_clz(g.E);         // of 0 .. E
+        const int last = (int)min(first + g.per, (int64_t)g.S);
+        for (int64_t s0 = first; s0 < last; s0 += 64) {
+            const int64_t s = s0 + lane;
+            const int e = s < last ? expert_of(g.ids[s], g.E) : g.E;
+            unsigned long long same = ~0ull;
+            for (int b = 0; b < bits; ++b) {
+                const unsigned long long set = __ballot((e >> b) & 1);
+                same &= (e >> b) & 1 ? set : ~set;
+            }
+            const int before = __popcll(same & ((1ull << lane) - 1));
+            const int had = seen[e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (all lanes have read before one writes: a wave's LDS accesses keep their order)
+            if (before == 0) seen[e] = had + __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (s < last) g.rows[s] = e < g.E ? had + before : -1;
+        }
+    }
+    __syncthreads();
+    if (run < g.runs)
+        for (int e = lane; e < g.E; e += 64) g.base[(int64_t)run * g.E + e] = seen[e];
+}
+
+// Exclusive sums over the lanes of a workgroup of WAVES waves, and the total; `shared`: WAVES ints.
+template <int WAVES> __device__ inline int scan_workgroup(int x, int *shared, int &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int incl = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 63) shared[wave] = incl;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += shared[w];
+        total += shared[w];
+    }
+    __syncthreads();
+    return before + incl - x;
+}
+
+// One workgroup: the counts of the runs become the rows at which each run's slots of an expert begin.
+constexpr int SCAN = 1024;
+__global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
+    __shared__ int part[SCAN], waves[SCAN / 64];
+    int at = 0;                                           // rows of the experts before e0
+    // W experts at a time, one for each of W threads, whose runs SCAN / W threads share
+    int W = 1;
+    while (W < g.E && W < SCAN) W <<= 1;
+    const int shares = SCAN / W, col = threadIdx.x % W, share = threadIdx.x / W;
+    const int each = (g.runs + shares - 1) / shares;
+    const int r0 = min(share * each, g.runs), r1 = min(r0 + each, g.runs);
+    for (int e0 = 0; e0 < g.E; e0 += W) {
+        const int e = e0 + col;
+        int sum = 0;
+        if (e < g.E)
+            for (int r = r0; r < r1; ++r) sum += g.base[(int64_t)r * g.E + e];
+        part[threadIdx.x] = sum;
+        __syncthreads();
+        int whole = 0, before = 0;                        // of the expert; of its shares before this one
+        for (int i = 0; i < shares; ++i) {
+            const int c = part[i * W + col];
+            whole += c;
+            before += i < share ? c : 0;
+        }
+        int total;
+        const int start = scan_workgroup<SCAN / 64>(share == 0 ? whole : 0, waves, total);
+        if (share == 0) {
+            part[col] = at + start;
+            if (e < g.E) g.offsets[e] = at + start;
+        }
+        __syncthreads();
+        int row = part[col] + before;
+        if (e < g.E)
+            for (int r = r0; r < r1; ++r) {
+                const int c = g.base[(int64_t)r * g.E + e];
+                g.base[(int64_t)r * g.E + e] = row;
+                row += c;
+            }
+        at += total;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) g.offsets[g.E] = at;
+}
+
+__device__ inline int ranked_row(const SortArgs &g, unsigned s) {
+    const int local = g.rows[s];
+    return local < 0 ? -1 : g.base[(int64_t)(s / (unsigned)g.per) * g.E + g.ids[s]] + local;
+}
+__global__ __launch_bounds__(THREADS) void sort_rows_kernel(const SortArgs g) {
+    const unsigned s = blockIdx.x * THREADS + threadIdx.x;
+    if (s < (unsigned)g.S) g.rows[s] = ranked_row(g, s);
+}
+
+// ---------------------------------------------------------------- rows of tokens to rows of experts
+struct MoveArgs {
+    int T, k, R, d;          // tokens, slots of a token, rows of the experts' matrices, width
+    const int *rows;         // [T][k]
+    const float *w;          // [T][k] or NULL
+    const void *x;           // the tokens' matrix, or the experts' (combine)
+    int64_t ldx;
+    const void *y;           // combine: what is added, or NULL; combine_grad: the experts' results
+    int64_t ldy;
+    void *out;
+    int64_t ldo;
+    float *dw;               // combine_grad
+    int part;                // columns of a workgroup (a launch's second dimension goes over them)
+    SortArgs sort;           // dispatch
+};
+
+// Where a workgroup gets the rows of its slots from: they are given; or the runs' counts and first rows are; or there are so few slots that
+// every workgroup counts those in front of its own, and a launch needs no other before it.
+enum { GIVEN = 0, RANKED = 1, COUNTED = 2 };
+constexpr int FEW_SLOTS = 1024;
+
+// The offsets from the counts of all slots, by the launch's last workgroup.
+__device__ inline void count_offsets(const SortArgs &g, const int *expert /* LDS */, int *count /* LDS, [E] */, int *waves) {
+    for (int e = threadIdx.x; e < g.E; e += THREADS) count[e] = 0;
+    __syncthreads();
+    for (int s = threadIdx.x; s < g.S; s += THREADS)
+        if (expert[s] < g.E) atomicAdd(&count[expert[s]], 1);      // (whole numbers: the order changes nothing)
+    __syncthreads();
+    const int each = (g.E + THREADS - 1) / THREADS, e0 = min((int)threadIdx.x * each, g.E), e1 = min(e0 + each, g.E);
+    int sum = 0, total;
+    for (int e = e0; e < e1; ++e) sum += count[e];
+    int at = scan_workgroup<THREADS / 64>(sum, waves, total);
+    for (int e = e0; e < e1; ++e) {
+        g.offsets[e] = at;
+        at += count[e];
+    }
+    if (threadIdx.x == 0) g.offsets[g.E] = total;
+}
+
+// Xs[rows[s]] = X[t]: every token is read once and stored k times.  LANES lanes take a token.
+template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS) void scatter_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), U = 2;
+    extern __shared__ int shared[];                       // rows of the workgroup's slots [TOK k]; COUNTED: experts of all slots [S], counts [E]
+    __shared__ int waves[THREADS / 64];
+    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int mine = (int)min((int64_t)TOK, max((int64_t)g.T - t0, (int64_t)0)) * g.k;
+    if (MODE == COUNTED) {
+        int *const expert = shared + TOK * g.k;
+        for (int s = threadIdx.x; s < g.sort.S; s += THREADS) expert[s] = expert_of(g.sort.ids[s], g.sort.E);
+        __syncthreads();
+        if (blockIdx.x == gridDim.x - 1) {
+            if (blockIdx.y == 0) count_offsets(g.sort, expert, expert + g.sort.S, waves);
+            return;
+        }
+        const int lane = threadIdx.x & 63;
+        for (int i = threadIdx.x >> 6; i < mine; i += THREADS / 64) {
+            const int s = (int)t0 * g.k + i, e = expert[s];
+            int row = 0;
+            for (int o = 0; o < g.sort.S; o += 64) {
+                const int f = o + lane < g.sort.S ? expert[o + lane] : g.sort.E;
+                row += __popcll(__ballot(f < e || (f == e && o + lane < s)));
+            }
+            if (lane == 0) {
+                shared[i] = row = e < g.sort.E ? row : -1;
+                if (blockIdx.y == 0) g.sort.rows[s] = row;
+            }
+        }
+    } else {
+        for (int i = threadIdx.x; i < mine; i += THREADS) {
+            const int64_t s = t0 * g.k + i;
+            const int row = MODE == RANKED ? ranked_row(g.sort, (unsigned)s) : g.rows[s];
+            if (MODE == RANKED) g.sort.rows[s] = row;
+            shared[i] = row;
+        }
+    }
+    __syncthreads();
+    const int64_t t = t0 + threadIdx.x / LANES;
+    if (t >= g.T) return;
+    const int *const rows = shared + threadIdx.x / LANES * g.k;
+    const int c0 = blockIdx.y * g.part, c1 = min(g.d, c0 + g.part);
+    for (int i = c0 + (int)(threadIdx.x % LANES) * N; i < c1; i += LANES * N * U) {
+        if (i + (U - 1) * LANES * N + N <= c1) {
+            Vec<T, N> r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = load<T, N>(g.x, t * g.ldx + i + u * LANES * N);
+            for (int j = 0; j < g.k; ++j) {
+                const int row = rows[j];
+                if ((unsigned)row >= (unsigned)g.R) continue;
+#pragma unroll
+                for (int u = 0; u < U; ++u) store(g.out, row * g.ldo + i + u * LANES * N, r[u]);
+            }
+        } else {
+            for (int u = 0; u < U; ++u) {
+                const int b = i + u * LANES * N, in = min(N, c1 - b);
+                Vec<T, N> r{};
+                if (in == N) r = load<T, N>(g.x, t * g.ldx + b);
+                else
+                    for (int n = 0; n < in; ++n) r.x[n] = ((const T *)g.x)[t * g.ldx + b + n];
+                for (int j = 0; j < g.k; ++j) {
+                    const int row = rows[j];
+                    if ((unsigned)row >= (unsigned)g.R) continue;
+                    if (in == N) store(g.out, row * g.ldo + b, r);
+                    else
+                        for (int n = 0; n < in; ++n) ((T *)g.out)[row * g.ldo + b + n] = r.x[n];
+                }
+            }
+        }
+    }
+}
+
+// N elements from i on as fp32; `in` of them exist.
+template <typename T, int N> __device__ inline void fetch(const void *p, int64_t i, int in, float (&x)[N]) {
+    if (in >= N) {
+        const auto r = load<T, N>(p, i);
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = value_of(r.x[n]);
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = n < in ? value_of(((const T *)p)[i + n]) : 0.f;
+    }
+}
+template <typename T, int N> __device__ inline void put(void *p, int64_t i, int in, const float (&x)[N]) {
+    if (in >= N) {
+        Vec<T, N> r;
+#pragma unroll
+        for (int n = 0; n < N; ++n) r.x[n] = element_of<T>(x[n]);
+        store(p, i, r);
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (n < in) ((T *)p)[i + n] = element_of<T>(x[n]);
+    }
+}
+
+// Rows and weights of a workgroup's slots in LDS: a row outside the matrix is -1.
+__device__ inline void slots_of(const MoveArgs &g, int64_t t0, int mine, int *rows, float *w) {
+    for (int i = threadIdx.x; i < mine; i += THREADS) {
+        const int row = g.rows[t0 * g.k + i];
+        rows[i] = (unsigned)row < (unsigned)g.R ? row : -1;
+        w[i] = g.w ? g.w[t0 * g.k + i] : 1.f;
+    }
+    __syncthreads();
+}
+
+// Y[t] = add[t] + sum_j w[s] Ys[rows[s]]: sums in fp32 in the order of j, rounded once.  KB rows are asked for at a time.
+template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) void combine_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T);
+    extern __shared__ int shared[];
+    float *const weights = (float *)(shared + TOK * g.k);
+    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
+    const int64_t t = t0 + threadIdx.x / LANES;
+    if (t >= g.T) return;
+    const int *const rows = shared + threadIdx.x / LANES * g.k;
+    const float *const w = weights + threadIdx.x / LANES * g.k;
+    const int c0 = blockIdx.y * g.part, c1 = min(g.d, c0 + g.part);
+    for (int i = c0 + (int)(threadIdx.x % LANES) * N; i < c1; i += LANES * N) {
+        const int in = c1 - i;
+        float sum[N];
+        if (g.y) fetch<T, N>(g.y, t * g.ldy + i, in, sum);
+        else
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[n] = 0.f;
+        for (int j0 = 0; j0 < g.k; j0 += KB) {
+            float x[KB][N];
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                const int row = rows[min(j0 + j, g.k - 1)];
+                if (row >= 0) fetch<T, N>(g.x, row * g.ldx + i, in, x[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j0 + j < g.k && rows[j0 + j] >= 0)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sum[n] = fmaf(w[j0 + j], x[j][n], sum[n]);
+        }
+        put<T, N>(g.out, t * g.ldo + i, in, sum);
+    }
+}
+
+// dYs[rows[s]] = w[s] dY[t] and dw[s] = <dY[t], Ys[rows[s]]>, KB slots of a token at a time.  A lane's share of a product is summed in fp32 in
+// the order of the columns, the lanes' then by halves: the same order from run to run.
+template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T);
+    extern __shared__ int shared[];
+    __shared__ float partial[THREADS / 64][KB];
+    float *const weights = (float *)(shared + TOK * g.k);
+    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
+    const int64_t t = t0 + threadIdx.x / LANES;
+    const bool there = t < g.T;
+    const int lane = threadIdx.x % LANES;
+    const int *const rows = shared + threadIdx.x / LANES * g.k;
+    const float *const w = weights + threadIdx.x / LANES * g.k;
+    for (int j0 = 0; j0 < g.k; j0 += KB) {
+        float dot[KB];
+#pragma unroll
+        for (int j = 0; j < KB; ++j) dot[j] = 0.f;
+        for (int i = lane * N; there && i < g.d; i += LANES * N) {
+            const int in = g.d - i;
+            float dy[N], x[KB][N];
+            fetch<T, N>(g.x, t * g.ldx + i, in, dy);
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j0 + j < g.k && rows[j0 + j] >= 0) fetch<T, N>(g.y, rows[j0 + j] * g.ldy + i, in, x[j]);
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j0 + j < g.k && rows[j0 + j] >= 0) {
+                    float o[N];
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        dot[j] = n < in ? fmaf(dy[n], x[j][n], dot[j]) : dot[j];
+                        o[n] = w[j0 + j] * dy[n];
+                    }
+                    put<T, N>(g.out, rows[j0 + j] * g.ldo + i, in, o);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
+            dot[j] = group_sum<(LANES < 64 ? LANES : 64)>(dot[j]);
+            if (LANES > 64 && (threadIdx.x & 63) == 0) partial[threadIdx.x >> 6][j] = dot[j];
+        }
+        if (LANES > 64) __syncthreads();
+        if (there && lane < KB && j0 + lane < g.k) {
+            float s = 0.f;
+            if (LANES > 64) {
+                for (int v = 0; v < LANES / 64; ++v) s += partial[v][lane];
+            } else {
+#pragma unroll
+                for (int j = 0; j < KB; ++j) s = j == lane ? dot[j] : s;
+            }
+            g.dw[t * g.k + j0 + lane] = s;
+        }
+        if (LANES > 64) __syncthreads();
+    }
+}
+
+// Lanes for a token: sixteen where its row is sixteen vectors or less, a wave up to 128, else a workgroup.
+int lanes_of(int d, int es) {
+    const int vectors = (d * es + 15) / 16;
+    return vectors <= 16 ? 16 : vectors <= 128 ? 64 : 256;
+}
+// Columns of a workgroup: a few long rows are cut until 512 workgroups share them, into parts of a vector for each lane at least.
+int part_of(int T, int d, int es, int lanes) {
+    const int step = lanes * (16 / es), tok = THREADS / lanes;
+    const int64_t wgs = ((int64_t)T + tok - 1) / tok;
+    const int most = (d + step - 1) / step, want = (int)std::max<int64_t>(1, 512 / std::max<int64_t>(wgs, 1));
+    const int parts = std::max(1, std::min(most, want)), steps = std::max(1, (most + parts - 1) / parts);
+    return steps * step;
+}
+
+template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, double bytes) {
+    const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
+    g.part = MODE == RANKED ? (1 << 30) : part_of(g.T, g.d, sizeof(T), lanes);   // (a second workgroup of a slot would find its rank replaced)
+    const unsigned parts = MODE == RANKED ? 1 : std::max(1, (g.d + g.part - 1) / g.part);     // (no columns: the order of the slots alone)
+    const dim3 grid((unsigned)(((int64_t)g.T + tok - 1) / tok + (MODE == COUNTED ? 1 : 0)), parts);
+    const size_t lds = 4 * ((size_t)tok * g.k + (MODE == COUNTED ? g.sort.S + g.sort.E : 0));
+    KfacProfScope prof(ctx, KC_TOKENS, 0.0, bytes);
+    const auto kernel = lanes == 16 ? scatter_kernel<T, 16, MODE> : lanes == 64 ? scatter_kernel<T, 64, MODE> : scatter_kernel<T, 256, MODE>;
+    hipLaunchKernelGGL(kernel, grid, dim3(THREADS), lds, ctx->stream, g);
+    KFAC_HIP_CHECK(hipGetLastError());
+    return KFAC_OK;
+}
+
+template <typename T, int KB> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
+    const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
+    const unsigned wgs = (unsigned)(((int64_t)g.T + tok - 1) / tok);
+    const size_t lds = 8 * (size_t)tok * g.k;
+    KfacProfScope prof(ctx, KC_TOKENS, flops, bytes);
+    if (g.dw) {
+        const auto kernel = lanes == 16 ? combine_grad_kernel<T, 16, KB> : lanes == 64 ? combine_grad_kernel<T, 64, KB> : combine_grad_kernel<T, 256, KB>;
+        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(THREADS), lds, ctx->stream, g);
+    } else {
+        g.part = part_of(g.T, g.d, sizeof(T), lanes);
+        const auto kernel = lanes == 16 ? combine_kernel<T, 16, KB> : lanes == 64 ? combine_kernel<T, 64, KB> : combine_kernel<T, 256, KB>;
+        hipLaunchKernelGGL(kernel, dim3(wgs, (unsigned)((g.d + g.part - 1) / g.part)), dim3(THREADS), lds, ctx->stream, g);
+    }
+    KFAC_HIP_CHECK(hipGetLastError());
+    return KFAC_OK;
+}
+template <typename T> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
+    return g.k == 1 ? launch_combine<T, 1>(ctx, g, flops, bytes) : g.k == 2 ? launch_combine<T, 2>(ctx, g, flops, bytes) : launch_combine<T, 4>(ctx, g, flops, bytes);
+}
+
+template <typename T, int L, int V> void launch_route(kfac_ctx *ctx, const RouteArgs &g) {
+    hipLaunchKernelGGL((route_kernel<T, L, V>), dim3((g.T + THREADS / L - 1) / (THREADS / L)), dim3(THREADS), 0, ctx->stream, g);
+}
+template <typename T, int L, int V> void launch_route(kfac_ctx *ctx, const RouteGradArgs &g) {
+    hipLaunchKernelGGL((route_grad_kernel<T, L, V>), dim3((g.T + THREADS / L - 1) / (THREADS / L)), dim3(THREADS), 0, ctx->stream, g);
+}
+// The smallest group of lanes that holds the logits of a token.
+template <typename T, typename Args> void launch_route(kfac_ctx *ctx, const Args &g) {
+    if (g.E <= 16) launch_route<T, 4, 4>(ctx, g);
+    else if (g.E <= 64) launch_route<T, 16, 4>(ctx, g);
+    else if (g.E <= 128) launch_route<T, 16, 8>(ctx, g);
+    else if (g.E <= 256) launch_route<T, 16, 16>(ctx, g);
+    else if (g.E <= 512) launch_route<T, 64, 8>(ctx, g);
+    else if (g.E <= 1024) launch_route<T, 64, 16>(ctx, g);
+    else launch_route<T, 64, 64>(ctx, g);
+}
+
+// Runs of a sort: short ones while their counts are few, as many as the workspace holds.  With a single one its counts become the
+// offsets themselves, where they are.
+constexpr int RUN = 256;
+constexpr int64_t COUNTS = 1 << 16;
+int runs_of(int64_t S, int E, size_t ws_bytes) {
+    const int64_t most = std::min<int64_t>((S + RUN - 1) / RUN, std::max<int64_t>(COUNTS / E, 64));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)(std::min<size_t>(ws_bytes, (size_t)1 << 40) / ((size_t)E * sizeof(int)))));
+}
+
+}  // namespace
+
+size_t kfac_experts_dispatch_ws_bytes_impl(int tokens, int topk, int experts) {
+    const int64_t S = (int64_t)tokens * topk;
+    if (S <= FEW_SLOTS) return 0;
+    return kfac_align_up((size_t)runs_of(S, experts, SIZE_MAX) * experts * sizeof(int), 256);
+}
+
+int kfac_launch_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize, int *ids, float *weights) {
+    const RouteArgs g{logits, ldl, tokens, experts, topk, normalize, ids, weights};
+    const double n = (double)tokens * experts, es = dtype == KFAC_BF16 ? 2.0 : 4.0;
+    KfacProfScope prof(ctx, KC_ROUTE, n * (4 + topk), n * es + 8.0 * tokens * topk);
+    if (dtype == KFAC_BF16) launch_route<unsigned short>(ctx, g);
+    else launch_route<float>(ctx, g);
+    KFAC_HIP_CHECK(hipGetLastError());
+    return KFAC_OK;
+}
+
+int kfac_launch_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, const int *ids, const float *dweights,
+                                   int normalize, void *dlogits, int64_t ldd) {
+    const RouteGradArgs g{logits, ldl, tokens, experts, topk, normalize, ids, dweights, dlogits, ldd};
+    const double n = (double)tokens * experts, s = (double)tokens * topk, es = dtype == KFAC_BF16 ? 2.0 : 4.0;
+    KfacProfScope prof(ctx, KC_ROUTE, normalize ? 4.0 * s : 6.0 * n, es * (n + (normalize ? s : n)) + 8.0 * s);
+    if (dtype == KFAC_BF16) launch_route<unsigned short>(ctx, g);
+    else launch_route<float>(ctx, g);
+    KFAC_HIP_CHECK(hipGetLastError());
+    return KFAC_OK;
+}
+
+int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int experts, const int *ids, const void *X, int64_t ldx, int *offsets, int *rows, void *Xs,
+                                 int64_t lds) {
+    const int64_t S = (int64_t)d->tokens * d->topk;
+    const bool bf = d->dtype == KFAC_BF16;
+    const double bytes = 8.0 * (double)S + 4.0 * experts + (X ? (bf ? 2.0 : 4.0) * d->d * ((double)d->tokens + (double)S) : 0.0);
+    MoveArgs g{};
+    g.T = d->tokens;
+    g.k = d->topk;
+    g.R = d->rows;
+    g.d = X ? d->d : 0;
+    g.rows = rows;
+    g.x = X;
+    g.ldx = ldx;
+    g.out = Xs;
+    g.ldo = lds;
+    SortArgs &s = g.sort;
+    s.ids = ids;
+    s.S = (int)S;
+    s.E = experts;
+    s.k = d->topk;
+    s.offsets = offsets;
+    s.rows = rows;
+    if (S <= FEW_SLOTS) return bf ? launch_scatter<unsigned short, COUNTED>(ctx, g, bytes) : launch_scatter<float, COUNTED>(ctx, g, bytes);
+    s.runs = runs_of(S, experts, ctx->ws_bytes);
+    s.per = (int)(((S + s.runs - 1) / s.runs + 63) / 64 * 64);
+    s.runs = (int)((S + s.per - 1) / s.per);
+    s.base = s.runs > 1 ? (int *)ctx->ws : offsets;
+    {
+        KfacProfScope prof(ctx, KC_TOKENS, 0.0, 8.0 * (double)S);
+        const int waves = experts <= 1024 ? THREADS / 64 : 1;      // of a workgroup, for its counts in LDS
+        hipLaunchKernelGGL(sort_count_kernel, dim3((s.runs + waves - 1) / waves), dim3(64 * waves), waves * sizeof(int) * (experts + 1), ctx->stream, s);
+        hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(SCAN), 0, ctx->stream, s);
+    }
+    KFAC_HIP_CHECK(hipGetLastError());
+    if (X) return bf ? launch_scatter<unsigned short, RANKED>(ctx, g, bytes) : launch_scatter<float, RANKED>(ctx, g, bytes);
+    hipLaunchKernelGGL(sort_rows_kernel, dim3((unsigned)((S + THREADS - 1) / THREADS)), dim3(THREADS), 0, ctx->stream, s);
+    KFAC_HIP_CHECK(hipGetLastError());
+    return KFAC_OK;
+}
+
+int kfac_launch_experts_gather(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const void *X, int64_t ldx, void *Xs, int64_t lds) {
+    MoveArgs g{};
+    g.T = d->tokens;
+    g.k = d->topk;
+    g.R = d->rows;
+    g.d = d->d;
+    g.rows = rows;
+    g.x = X;
+    g.ldx = ldx;
+    g.out = Xs;
+    g.ldo = lds;
+    const double S = (double)d->tokens * d->topk, bytes = 4.0 * S + (d->dtype == KFAC_BF16 ? 2.0 : 4.0) * d->d * (d->tokens + S);
+    return d->dtype == KFAC_BF16 ? launch_scatter<unsigned short, GIVEN>(ctx, g, bytes) : launch_scatter<float, GIVEN>(ctx, g, bytes);
+}
+
+int kfac_launch_experts_combine(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const float *weights, const void *Ys, int64_t ldys, const void *add, int64_t lda,
+                                void *Y, int64_t ldy) {
+    MoveArgs g{};
+    g.T = d->tokens;
+    g.k = d->topk;
+    g.R = d->rows;
+    g.d = d->d;
+    g.rows = rows;
+    g.w = weights;
+    g.x = Ys;
+    g.ldx = ldys;
+    g.y = add;
+    g.ldy = lda;
+    g.out = Y;
+    g.ldo = ldy;
+    const double S = (double)d->tokens * d->topk, es = d->dtype == KFAC_BF16 ? 2.0 : 4.0;
+    const double bytes = (weights ? 8.0 : 4.0) * S + es * d->d * (S + d->tokens * (add ? 2.0 : 1.0)), flops = 2.0 * S * d->d;
+    return d->dtype == KFAC_BF16 ? launch_combine<unsigned short>(ctx, g, flops, bytes) : launch_combine<float>(ctx, g, flops, bytes);
+}
+
+int kfac_launch_experts_combine_grad(kfac_ctx *ctx, const kfac_slot_desc *d, const int *rows, const float *weights, const void *dY, int64_t lddy, const void *Ys,
+                                     int64_t ldys, void *dYs, int64_t lddys, float *dweights) {
+    MoveArgs g{};
+    g.T = d->tokens;
+    g.k = d->topk;
+    g.R = d->rows;
+    g.d = d->d;
+    g.rows = rows;
+    g.w = weights;
+    g.x = dY;
+    g.ldx = lddy;
+    g.y = Ys;
+    g.ldy = ldys;
+    g.out = dYs;
+    g.ldo = lddys;
+    g.dw = dweights;
+    const double S = (double)d->tokens * d->topk, es = d->dtype == KFAC_BF16 ? 2.0 : 4.0;
+    const double bytes = 12.0 * S + es * d->d * (2.0 * S + d->tokens), flops = 3.0 * S * d->d;
+    return d->dtype == KFAC_BF16 ? launch_combine<unsigned short>(ctx, g, flops, bytes) : launch_combine<float>(ctx, g, flops, bytes);
+}

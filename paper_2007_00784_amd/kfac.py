@@ -26,6 +26,8 @@ EXPORTS = (
     "kfac_precondition_inverse_batched", "kfac_precondition_inverse_workspace_bytes",
     "kfac_experts_forward", "kfac_experts_input_grad", "kfac_experts_weight_grad", "kfac_update_factors_experts",
     "kfac_experts_workspace_bytes", "kfac_adamw_batched", "kfac_adamw_state_values",
+    "kfac_experts_route", "kfac_experts_route_grad", "kfac_experts_dispatch", "kfac_experts_dispatch_workspace_bytes", "kfac_experts_gather",
+    "kfac_experts_combine", "kfac_experts_combine_grad", "kfac_grad_norm_batched", "kfac_grad_norm_workspace_bytes", "kfac_clip_grads_batched",
 )
 
 
@@ -69,6 +71,14 @@ class kfac_factor_item(ctypes.Structure):
 class kfac_expert_desc(ctypes.Structure):
     _fields_ = [("experts", ctypes.c_int), ("rows", ctypes.c_int), ("d_in", ctypes.c_int), ("d_out", ctypes.c_int),
                 ("append_ones", ctypes.c_int), ("dtype", ctypes.c_int), ("offsets", ctypes.c_void_p)]
+
+
+class kfac_slot_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int), ("topk", ctypes.c_int), ("rows", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class kfac_grad_item(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("grad_dtype", ctypes.c_int), ("out", ctypes.c_void_p), ("out_dtype", ctypes.c_int), ("n", ctypes.c_int64)]
 
 
 class kfac_adamw_item(ctypes.Structure):
@@ -144,13 +154,27 @@ def lib():
     L.kfac_update_factors_experts.argtypes = [vp, i, i, vp, vp, i, i64, i, i, i, f, f, vp]
     L.kfac_adamw_batched.argtypes = [vp, i, ctypes.POINTER(kfac_adamw_item), ctypes.POINTER(kfac_adamw_opts)]
     L.kfac_adamw_state_values.argtypes = [vp, vp, vp, i64, vp, i]
+    sp, gp = ctypes.POINTER(kfac_slot_desc), ctypes.POINTER(kfac_grad_item)
+    L.kfac_experts_route.argtypes = [vp, i, i, i, vp, i, i64, i, vp, vp]
+    L.kfac_experts_route_grad.argtypes = [vp, i, i, i, vp, i, i64, vp, vp, i, vp, i64]
+    L.kfac_experts_dispatch.argtypes = [vp, sp, i, vp, vp, i64, vp, vp, vp, i64]
+    L.kfac_experts_dispatch_workspace_bytes.argtypes = [i, i, i]
+    L.kfac_experts_dispatch_workspace_bytes.restype = sz
+    L.kfac_experts_gather.argtypes = [vp, sp, vp, vp, i64, vp, i64]
+    L.kfac_experts_combine.argtypes = [vp, sp, vp, vp, vp, i64, vp, i64, vp, i64]
+    L.kfac_experts_combine_grad.argtypes = [vp, sp, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    L.kfac_grad_norm_batched.argtypes = [vp, i, gp, f, vp, vp, vp]
+    L.kfac_grad_norm_workspace_bytes.argtypes = [i, gp]
+    L.kfac_grad_norm_workspace_bytes.restype = sz
+    L.kfac_clip_grads_batched.argtypes = [vp, i, gp, f, vp, vp, vp]
     L.kfac_profile_begin.argtypes = [vp]
     L.kfac_profile_end.argtypes = [vp, ctypes.POINTER(kfac_kernel_stat), i, ip]
     for name in EXPORTS:
         if name not in ("kfac_workspace_bytes", "kfac_eig_workspace_bytes", "kfac_strerror",
                         "kfac_precondition_workspace_bytes", "kfac_update_factors_workspace_bytes",
                         "kfac_unfold_workspace_bytes", "kfac_static_scratch_bytes", "kfac_invert_workspace_bytes",
-                        "kfac_precondition_inverse_workspace_bytes", "kfac_experts_workspace_bytes"):
+                        "kfac_precondition_inverse_workspace_bytes", "kfac_experts_workspace_bytes",
+                        "kfac_experts_dispatch_workspace_bytes", "kfac_grad_norm_workspace_bytes"):
             getattr(L, name).restype = i
     _lib = L
     return L
@@ -503,6 +527,202 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
     _on_gpu(X, offsets, F)
     _check(lib().kfac_update_factors_experts(ctx, _c_int(experts), _c_int(X.shape[0]), offsets.data_ptr(), xp, _dtype_code(X), ldx, _c_int(d), ones,
                                              int(bool(mean)), float(scale), float(decay), _ptr(F)), "kfac_update_factors_experts")
+
+
+# ---- tokens to experts and back ----
+def _slots(t, name, dtype, shape=None):
+    """A contiguous matrix [tokens, topk] of one entry for each slot."""
+    if t.dtype != dtype or t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError("%s must be %s [tokens, topk]" % (name, dtype))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def kfac_experts_route(ctx, logits, ids, weights, normalize=False):
+    """ids[t] = the experts of the topk largest logits of token t (ties to the lowest index; -1 where only logits of -inf are left), weights[t] their
+    softmax over all experts, or with normalize over those chosen.  logits [tokens, experts] (any row pitch), ids int32 and weights float32
+    [tokens, topk]: written."""
+    import torch
+    ip = _slots(ids, "ids", torch.int32)
+    wp = _slots(weights, "weights", torch.float32, ids.shape)
+    if logits.dim() != 2 or logits.shape[0] != ids.shape[0]:
+        raise ValueError("logits must be [tokens, experts]")
+    tokens, experts = logits.shape
+    lp, ldl = _rows(logits, "logits", experts)
+    code = _dtype_code(logits)
+    _on_gpu(logits, ids, weights)
+    _check(lib().kfac_experts_route(ctx, _c_int(tokens), _c_int(experts), _c_int(ids.shape[1]), lp, code, ldl, int(bool(normalize)), ip, wp), "kfac_experts_route")
+
+
+def kfac_experts_route_grad(ctx, logits, ids, dweights, dlogits, normalize=False):
+    """The gradient of the logits (written to dlogits, of their shape and dtype) from that of the weights; logits, ids and normalize as in
+    kfac_experts_route()."""
+    import torch
+    ip = _slots(ids, "ids", torch.int32)
+    wp = _slots(dweights, "dweights", torch.float32, ids.shape)
+    if logits.dim() != 2 or logits.shape[0] != ids.shape[0]:
+        raise ValueError("logits must be [tokens, experts]")
+    _same(logits, dlogits, "logits and dlogits")
+    tokens, experts = logits.shape
+    if dlogits.dim() != 2 or dlogits.shape[0] != tokens:
+        raise ValueError("logits and dlogits must have one shape")
+    lp, ldl = _rows(logits, "logits", experts)
+    dp, ldd = _rows(dlogits, "dlogits", experts)
+    code = _dtype_code(logits)
+    _on_gpu(logits, ids, dweights, dlogits)
+    _check(lib().kfac_experts_route_grad(ctx, _c_int(tokens), _c_int(experts), _c_int(ids.shape[1]), lp, code, ldl, ip, wp, int(bool(normalize)), dp, ldd),
+           "kfac_experts_route_grad")
+
+
+def kfac_experts_dispatch_workspace_bytes(tokens, topk, experts):
+    """Bytes of workspace that sorting so many slots makes use of (it works with less)."""
+    return int(lib().kfac_experts_dispatch_workspace_bytes(_c_int(int(tokens)), _c_int(int(topk)), _c_int(int(experts))))
+
+
+def kfac_experts_dispatch(ctx, ids, X, offsets, rows, Xs):
+    """Sorts the slots by expert and copies the tokens there: offsets (int32 [experts + 1]) and Xs [at least tokens * topk, d] are what the products for
+    layers of experts take, rows (int32 [tokens, topk]) says where each slot went (-1: it has no expert, its id is outside 0 .. experts - 1).
+    X [tokens, d]; ids int32 [tokens, topk].  X = Xs = None: the order alone."""
+    import torch
+    ip = _slots(ids, "ids", torch.int32)
+    rp = _slots(rows, "rows", torch.int32, ids.shape)
+    if offsets.dim() != 1 or offsets.shape[0] < 2:
+        raise ValueError("offsets must be int32 [experts + 1]")
+    experts = offsets.shape[0] - 1
+    _offsets(offsets, experts)
+    tokens, topk = ids.shape
+    if (X is None) != (Xs is None):
+        raise ValueError("both X and Xs or none")
+    xp = sp = None
+    ldx = lds = 0
+    if X is None:
+        d = kfac_slot_desc(_c_int(tokens), _c_int(topk), _c_int(tokens * topk), 0, KFAC_F32)
+    else:
+        if X.dim() != 2 or X.shape[0] != tokens:
+            raise ValueError("X must be [tokens, d]")
+        _same(X, Xs, "X and Xs")
+        if Xs.shape[0] < tokens * topk:
+            raise ValueError("Xs must have a row for each slot")
+        xp, ldx = _rows(X, "X", X.shape[1])
+        sp, lds = _rows(Xs, "Xs", X.shape[1])
+        d = kfac_slot_desc(_c_int(tokens), _c_int(topk), _c_int(Xs.shape[0]), _c_int(X.shape[1]), _dtype_code(X))
+    _on_gpu(ids, X, offsets, rows, Xs)
+    _check(lib().kfac_experts_dispatch(ctx, ctypes.byref(d), _c_int(experts), ip, xp, ldx, offsets.data_ptr(), rp, sp, lds), "kfac_experts_dispatch")
+
+
+def kfac_experts_gather(ctx, rows, X, Xs):
+    """Xs[rows[t, j]] = X[t], rows as kfac_experts_dispatch() left them."""
+    import torch
+    rp = _slots(rows, "rows", torch.int32)
+    if X.dim() != 2 or X.shape[0] != rows.shape[0]:
+        raise ValueError("X must be [tokens, d]")
+    _same(X, Xs, "X and Xs")
+    xp, ldx = _rows(X, "X", X.shape[1])
+    sp, lds = _rows(Xs, "Xs", X.shape[1])
+    d = kfac_slot_desc(_c_int(rows.shape[0]), _c_int(rows.shape[1]), _c_int(Xs.shape[0]), _c_int(X.shape[1]), _dtype_code(X))
+    _on_gpu(rows, X, Xs)
+    _check(lib().kfac_experts_gather(ctx, ctypes.byref(d), rp, xp, ldx, sp, lds), "kfac_experts_gather")
+
+
+def kfac_experts_combine(ctx, Ys, rows, weights, Y, add=None):
+    """Y[t] = add[t] + sum over j of weights[t, j] Ys[rows[t, j]].  Ys [R, d], rows int32 [tokens, topk], weights float32 [tokens, topk] or None (ones: the
+    gradient of kfac_experts_dispatch()), Y [tokens, d], add [tokens, d] or None, or Y itself."""
+    import torch
+    rp = _slots(rows, "rows", torch.int32)
+    wp = None if weights is None else _slots(weights, "weights", torch.float32, rows.shape)
+    if Y.dim() != 2 or Y.shape[0] != rows.shape[0]:
+        raise ValueError("Y must be [tokens, d]")
+    _same(Ys, Y, "Ys and Y")
+    tokens, width = Y.shape
+    sp, lds = _rows(Ys, "Ys", width)
+    yp, ldy = _rows(Y, "Y", width)
+    ap, lda = None, 0
+    if add is not None:
+        _same(add, Y, "add and Y")
+        if add.shape[0] != tokens:
+            raise ValueError("add and Y must have as many rows")
+        ap, lda = _rows(add, "add", width)
+    d = kfac_slot_desc(_c_int(tokens), _c_int(rows.shape[1]), _c_int(Ys.shape[0]), _c_int(width), _dtype_code(Y))
+    _on_gpu(Ys, rows, weights, Y, add)
+    _check(lib().kfac_experts_combine(ctx, ctypes.byref(d), rp, wp, sp, lds, ap, lda, yp, ldy), "kfac_experts_combine")
+
+
+def kfac_experts_combine_grad(ctx, dY, Ys, rows, weights, dYs, dweights):
+    """dYs[rows[t, j]] = weights[t, j] dY[t] and dweights[t, j] = <dY[t], Ys[rows[t, j]]>: the gradients of kfac_experts_combine().  dY [tokens, d], Ys and dYs
+    [R, d], weights and dweights float32 [tokens, topk]."""
+    import torch
+    rp = _slots(rows, "rows", torch.int32)
+    wp = _slots(weights, "weights", torch.float32, rows.shape)
+    gp = _slots(dweights, "dweights", torch.float32, rows.shape)
+    if dY.dim() != 2 or dY.shape[0] != rows.shape[0]:
+        raise ValueError("dY must be [tokens, d]")
+    _same(dY, Ys, "dY and Ys")
+    _same(dY, dYs, "dY and dYs")
+    if dYs.shape[0] != Ys.shape[0]:
+        raise ValueError("Ys and dYs must have as many rows")
+    tokens, width = dY.shape
+    yp, ldy = _rows(dY, "dY", width)
+    sp, lds = _rows(Ys, "Ys", width)
+    op, ldo = _rows(dYs, "dYs", width)
+    d = kfac_slot_desc(_c_int(tokens), _c_int(rows.shape[1]), _c_int(Ys.shape[0]), _c_int(width), _dtype_code(dY))
+    _on_gpu(dY, Ys, rows, weights, dYs, dweights)
+    _check(lib().kfac_experts_combine_grad(ctx, ctypes.byref(d), rp, wp, yp, ldy, sp, lds, op, ldo, gp), "kfac_experts_combine_grad")
+
+
+# ---- the global gradient norm ----
+def grad_items(grads, out=None):
+    """The marshalled item array of kfac_grad_norm_batched() and kfac_clip_grads_batched() for a list of device tensors (float32 or bfloat16, contiguous), reusable
+    while they live.  out: for clipping, a list of as many tensors of the same sizes that take the clipped gradients, each the gradient
+    itself or a buffer of its own."""
+    if out is not None and len(out) != len(grads):
+        raise ValueError("as many outputs as gradients")
+    arr = (kfac_grad_item * len(grads))()
+    written, read = set(), {}
+    for j, (d, g) in enumerate(zip(arr, grads)):
+        d.grad, d.grad_dtype, d.n = _ptr(g), _dtype_code(g), g.numel()
+        o = None if out is None else out[j]
+        if o is not None:
+            if o.numel() != d.n:
+                raise ValueError("buffers of different lengths")
+            d.out, d.out_dtype = _ptr(o), _dtype_code(o)
+            if d.n > 0:
+                if d.out in written:
+                    raise ValueError("an output occurs twice")
+                written.add(d.out)
+                if d.out == d.grad and d.out_dtype != d.grad_dtype:
+                    raise ValueError("a gradient can only be clipped in place in its own dtype")
+        _on_gpu(g, o)
+        if d.n > 0:
+            read.setdefault(d.grad, []).append(d.out)
+    # a gradient that is written must be read by its own item alone
+    for a, outs in read.items():
+        if a in written and (len(outs) > 1 or outs[0] != a):
+            raise ValueError("an output is another tensor's gradient")
+    return arr
+
+
+def kfac_grad_norm_workspace_bytes(items):
+    """items: the array that grad_items() made."""
+    return int(lib().kfac_grad_norm_workspace_bytes(len(items), items))
+
+
+def kfac_grad_norm_batched(ctx, items, norm, max_norm=None, grad_scale=None, coef=None):
+    """norm = |s| times the root of the sum of all gradients' squares, coef = s min(1, max_norm / norm) (None: s), s = grad_scale (None: 1).  items: a list of
+    gradients, or the array of grad_items(); norm, coef, grad_scale: device tensors of one float32.  coef is what kfac_adamw_batched() takes as
+    grad_scale."""
+    import torch
+    arr = grad_items(items) if isinstance(items, list) else items
+    _check(lib().kfac_grad_norm_batched(ctx, len(arr), arr, float("inf") if max_norm is None else float(max_norm), _scalar(grad_scale, torch.float32, "grad_scale"),
+                                        _scalar(norm, torch.float32, "norm"), _scalar(coef, torch.float32, "coef")), "kfac_grad_norm_batched")
+
+
+def kfac_clip_grads_batched(ctx, items, max_norm, norm, coef, grad_scale=None):
+    """As kfac_grad_norm_batched(), then every gradient times coef goes to its output (see grad_items()); a list of gradients is clipped in place."""
+    import torch
+    arr = grad_items(items, items) if isinstance(items, list) else items
+    _check(lib().kfac_clip_grads_batched(ctx, len(arr), arr, float(max_norm), _scalar(grad_scale, torch.float32, "grad_scale"), _scalar(norm, torch.float32, "norm"),
+                                         _scalar(coef, torch.float32, "coef")), "kfac_clip_grads_batched")
 
 
 # ---- the optimizer step ----

@@ -56,6 +56,7 @@ class KfacRunner:
         need = K.kfac_eig_workspace_bytes(dims)
         need = max(need, K.kfac_update_factors_workspace_bytes(self._factor_items(0, 0.0, sizing=True)))
         need = max(need, K.kfac_precondition_workspace_bytes([(l.d_a, l.d_g) for l in self.layers]))
+        need = max(need, K.kfac_grad_norm_workspace_bytes(K.grad_items(self.grad)))
         need = max(need, K.kfac_workspace_bytes(max(dims), 1, max(l.rows(self.N) for l in self.layers)))  # SYRK partials, precondition
         self.ws = torch.empty(need + 4096, dtype=torch.uint8, device=self.dev)
         self.stream = torch.cuda.current_stream(self.dev)
@@ -140,6 +141,14 @@ class KfacRunner:
             self.nu = torch.zeros(1, dtype=torch.float32, device=self.dev)
             K.kfac_precondition_batched_scaled(self.ctx, kappa=kappa, lr=lr, nu=self.nu, items=self._marshalled[key])
 
+    def clip(self, max_norm):
+        """The gradients, in place, times min(1, max_norm / their global norm).  The norm and what they were multiplied with stay on the GPU: self.norm
+        and self.coef."""
+        if "clip" not in self._marshalled:
+            self._marshalled["clip"] = K.grad_items(self.grad, self.grad)
+            self.norm, self.coef = (torch.zeros(1, dtype=torch.float32, device=self.dev) for _ in range(2))
+        K.kfac_clip_grads_batched(self.ctx, self._marshalled["clip"], max_norm, self.norm, self.coef)
+
     # ---- the explicit-inverse method (Sec. II-C, Eq. (kfac-damped)): the paper's other way to the same step ----
     def invert_factors(self, damping=None):
         """(A + gamma I)^-1 and (G + gamma I)^-1 of every layer by blocked Cholesky (buffers allocated on first use)."""
@@ -190,7 +199,7 @@ class ExpertRunner:
     # codes at least: until then an 8-bit state is rounded to nearest, which is off by less; from then on by the seed, or it would stand still.
     NEAREST_STEPS = 8
 
-    def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0", seed=1):
+    def __init__(self, experts, rows, d_in, d_out, bias=True, bf16=True, state_bits=32, damping=1e-3, device="cuda:0", seed=1, more_workspace=0):
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         self.dev = device_of(device)
@@ -206,22 +215,31 @@ class ExpertRunner:
         self.A, self.G = torch.zeros((experts, dA, dA), **f32), torch.zeros((experts, d_out, d_out), **f32)
         self.QA, self.QG = torch.zeros_like(self.A), torch.zeros_like(self.G)
         self.lamA, self.lamG = torch.zeros((experts, dA), **f32), torch.zeros((experts, d_out), **f32)
-        n = self.param.numel()
-        if state_bits == 8:
-            state = {k: torch.zeros(n, dtype=torch.uint8, device=self.dev) for k in ("m", "v")}
-            state.update({k: torch.zeros((n + 127) // 128, dtype=torch.uint8, device=self.dev) for k in ("m_scale", "v_scale")})
-        else:
-            state = {k: torch.zeros(n, **f32) for k in ("m", "v")}
-        self.state = state
+        self.state_bits = state_bits
+        self.state = self._state(self.param)
+        self._grads = K.grad_items([self.grad])
+        self.norm, self.coef = torch.zeros(1, **f32), torch.zeros(1, **f32)
         self.steps, self.seed = 0, seed
         dims = [dA] * experts + [d_out] * experts
         need = max(K.kfac_eig_workspace_bytes(dims), K.kfac_precondition_workspace_bytes([(dA, d_out)] * experts),
-                   K.kfac_experts_workspace_bytes(experts, rows, d_in, d_out, self.bias, K.KFAC_BF16 if bf16 else K.KFAC_F32))
+                   K.kfac_experts_workspace_bytes(experts, rows, d_in, d_out, self.bias, K.KFAC_BF16 if bf16 else K.KFAC_F32),
+                   K.kfac_grad_norm_workspace_bytes(self._grads), more_workspace)
         self.ws = torch.empty(need + 4096, dtype=torch.uint8, device=self.dev)
         self.stream = torch.cuda.current_stream(self.dev)
         self.ctx = K.kfac_create(self.dev.index, self.stream.cuda_stream, self.ws)
-        self._adamw = K.adamw_items([dict(param=self.param, grad=self.grad, **state, **(dict(copy=self.weight) if bf16 else {}))])
+        self._adamw = K.adamw_items([self._item(self.param, self.grad, self.state, self.weight)])
         self._precond = K.precond_items(list(self.QA), list(self.lamA), list(self.QG), list(self.lamG), damping, list(self.grad))
+
+    def _state(self, param):
+        n = param.numel()
+        if self.state_bits == 32:
+            return {k: torch.zeros(n, dtype=torch.float32, device=self.dev) for k in ("m", "v")}
+        state = {k: torch.zeros(n, dtype=torch.uint8, device=self.dev) for k in ("m", "v")}
+        state.update({k: torch.zeros((n + 127) // 128, dtype=torch.uint8, device=self.dev) for k in ("m_scale", "v_scale")})
+        return state
+
+    def _item(self, param, grad, state, weight):
+        return dict(param=param, grad=grad, **state, **(dict(copy=weight) if weight is not param else {}))
 
     def close(self):
         torch.cuda.synchronize(self.dev)
@@ -255,7 +273,71 @@ class ExpertRunner:
     def precondition(self):
         K.kfac_precondition_batched(self.ctx, items=self._precond)
 
+    def clip(self, max_norm, grad_scale=None):
+        """What step() takes as grad_scale to clip the gradients by their global norm (which stays in self.norm): a device tensor, nothing waits."""
+        K.kfac_grad_norm_batched(self.ctx, self._grads, self.norm, max_norm=max_norm, grad_scale=grad_scale, coef=self.coef)
+        return self.coef
+
     def step(self, lr, grad_scale=None, **hyper):
         t = self.steps + 1
         K.kfac_adamw_batched(self.ctx, self._adamw, lr=lr, step=t, grad_scale=grad_scale, seed=self.seed if t > self.NEAREST_STEPS else 0, **hyper)
         self.steps = t
+
+
+class RoutedExpertRunner(ExpertRunner):
+    """A layer of experts behind its router, from tokens to tokens: logits (a layer of one expert, the router), each token's topk experts and their
+    weights, tokens sorted by expert, the products, and the weighted sum of each token's results; and the way back.
+
+    x is [tokens, d_in]; the sorted rows of a step stay in self.xs, the gradients of their results in self.gs, where update_factors() takes them.
+    The router's parameters (fp32 [1, experts, d_in], no bias) take the optimizer step together with the experts'.
+    """
+
+    def __init__(self, experts, tokens, topk, d_in, d_out, normalize=True, bias=True, bf16=True, **kw):
+        code = K.KFAC_BF16 if bf16 else K.KFAC_F32
+        need = max(K.kfac_experts_dispatch_workspace_bytes(tokens, topk, experts), K.kfac_experts_workspace_bytes(1, tokens, d_in, experts, False, code),
+                   K.kfac_grad_norm_workspace_bytes((K.kfac_grad_item * 2)(*(K.kfac_grad_item(n=experts * n) for n in (d_out * (d_in + 1), d_in)))))
+        super().__init__(experts, tokens * topk, d_in, d_out, bias=bias, bf16=bf16, more_workspace=need, **kw)
+        self.tokens, self.topk, self.normalize = tokens, topk, normalize
+        f32, i32 = dict(dtype=torch.float32, device=self.dev), dict(dtype=torch.int32, device=self.dev)
+        new = lambda *shape: torch.zeros(shape, dtype=self.dt, device=self.dev)  # noqa: E731
+        self.router = torch.zeros((1, experts, d_in), **f32)
+        self.router_weight = torch.zeros_like(self.router, dtype=self.dt) if bf16 else self.router
+        self.router_grad = torch.zeros_like(self.router)
+        self.router_state = self._state(self.router)
+        self.logits, self.dlogits = new(tokens, experts), new(tokens, experts)
+        self.ids, self.row = torch.zeros((tokens, topk), **i32), torch.zeros((tokens, topk), **i32)
+        self.weights, self.dweights = torch.zeros((tokens, topk), **f32), torch.zeros((tokens, topk), **f32)
+        self.all, self.offsets = torch.tensor([0, tokens], **i32), torch.zeros(experts + 1, **i32)
+        self.xs, self.gs = new(tokens * topk, d_in), new(tokens * topk, d_out)
+        self.out, self.dtokens = new(tokens, d_out), new(tokens, d_in)
+        self._adamw = K.adamw_items([self._item(self.param, self.grad, self.state, self.weight),
+                                     self._item(self.router, self.router_grad, self.router_state, self.router_weight)])
+        self._grads = K.grad_items([self.grad, self.router_grad])
+
+    def load(self, param, router):
+        super().load(param)
+        self.router.copy_(router)
+        if self.router_weight is not self.router:
+            self.router_weight.copy_(self.router)
+
+    def forward(self, x, add=None):
+        """[tokens, d_out]: add (or zero) plus the weighted results of each token's experts."""
+        K.kfac_experts_forward(self.ctx, x, self.router_weight, self.all, self.logits)
+        K.kfac_experts_route(self.ctx, self.logits, self.ids, self.weights, normalize=self.normalize)
+        K.kfac_experts_dispatch(self.ctx, self.ids, x, self.offsets, self.row, self.xs)
+        super().forward(self.xs, self.offsets)
+        K.kfac_experts_combine(self.ctx, self.y, self.row, self.weights, self.out, add=add)
+        return self.out
+
+    def backward(self, x, g, accumulate=False):
+        """The tokens' gradient (returned), every expert's (self.grad) and the router's (self.router_grad) from the output's.  (What was added passes g on.)"""
+        K.kfac_experts_combine_grad(self.ctx, g, self.y, self.row, self.weights, self.gs, self.dweights)
+        super().backward(self.xs, self.gs, self.offsets, accumulate=accumulate)
+        K.kfac_experts_route_grad(self.ctx, self.logits, self.ids, self.dweights, self.dlogits, normalize=self.normalize)
+        K.kfac_experts_input_grad(self.ctx, self.dlogits, self.router_weight, self.all, self.dtokens)
+        K.kfac_experts_weight_grad(self.ctx, self.dlogits, x, self.all, self.router_grad, accumulate=accumulate)
+        K.kfac_experts_combine(self.ctx, self.dx, self.row, None, self.dtokens, add=self.dtokens)
+        return self.dtokens
+
+    def update_factors(self, decay):
+        super().update_factors(self.xs, self.gs, self.offsets, decay)

@@ -1,0 +1,118 @@
+"""A layer of experts behind its router through two training steps -- choice, sort, products, weighted sum, all gradients, preconditioning, clipping,
+AdamW -- against autograd in float64 on the library's own parameters and choices of each step."""
+import math
+
+import pytest
+import torch
+
+from paper_2007_00784_amd.runner import ExpertRunner, KfacRunner, RoutedExpertRunner
+from paper_2007_00784_amd import synthetic as S
+from gpu_util import relfro
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(run, x, g, add):
+    """Output and gradients (tokens, experts' weights, router) by autograd in float64, with the run's ids."""
+    f = lambda t: t.detach().double().cpu()  # noqa: E731
+    X, W, Wr = f(x).requires_grad_(), f(run.weight).requires_grad_(), f(run.router_weight)[0].requires_grad_()
+    ids = run.ids.cpu().long()
+    d = X.shape[1]
+    logits = X @ Wr.t()
+    w = torch.gather(torch.softmax(logits, 1), 1, ids)
+    if run.normalize:
+        w = w / w.sum(1, keepdim=True)
+    pick = W[ids]                                                        # [T, k, d_out, d + 1]
+    y = (pick[..., :d] * X[:, None, None, :]).sum(3) + (pick[..., d] if run.bias else 0.0)
+    out = (y * w[:, :, None]).sum(1)
+    if add is not None:
+        out = out + f(add)
+    out.backward(f(g))
+    return [t.detach() for t in (logits, out, X.grad, W.grad, Wr.grad)]
+
+
+@pytest.mark.parametrize("bf16,bits,normalize,T,k", [(True, 8, True, 200, 2), (True, 32, False, 700, 3), (False, 32, True, 700, 3), (False, 8, False, 33, 1)])
+def test_two_steps(bf16, bits, normalize, T, k):
+    E, d_in, d_out, lr = 5, 48, 40, 1e-2
+    gen = torch.Generator().manual_seed(7)
+    run = RoutedExpertRunner(E, T, k, d_in, d_out, normalize=normalize, bf16=bf16, state_bits=bits)
+    rand = lambda *s, scale=1.0: torch.randn(*s, generator=gen) * scale  # noqa: E731
+    run.load(rand(E, d_out, d_in + 1, scale=d_in ** -0.5), rand(1, E, d_in, scale=d_in ** -0.5))
+    moments = None
+    for step in range(2):
+        x, g, add = (rand(T, n).to(run.dt).to(run.dev) for n in (d_in, d_out, d_out))
+        if step == 0:
+            add = None
+        y = run.forward(x, add).clone()
+        dx = run.backward(x, g).clone()
+        ref = reference(run, x, g, add)
+        # fp32: sums of some ten thousand products at most.  bf16: logits, rows, their results and gradients are rounded one after another, each by 2^-9 on
+        # average and 2^-8 at most, and a logit's rounding moves its weight by as much: a path has at most eight of them
+        tol = 8 * 2.0 ** -8 if bf16 else 2e-5
+        for name, got, want in zip(("logits", "out", "tokens", "experts", "router"), (run.logits, y, dx, run.grad, run.router_grad[0]), ref):
+            assert relfro(got.double().cpu(), want) <= tol, name
+        # the choice is that of the logits
+        left = run.logits.double().cpu()
+        assert torch.equal(run.ids.cpu().long(), torch.sort(left, dim=1, descending=True, stable=True)[1][:, :k])
+        run.update_factors(0.0 if step == 0 else 0.9)
+        run.eig()
+        run.precondition()
+        grads = [run.grad.double().cpu(), run.router_grad.double().cpu()]
+        want = math.sqrt(sum(float((t ** 2).sum()) for t in grads))
+        before = [run.param.double().cpu(), run.router.double().cpu()]
+        coef = run.clip(want / 3)
+        run.step(lr, grad_scale=coef)
+        torch.cuda.synchronize()
+        assert abs(float(run.norm) - want) <= 1e-6 * want and abs(float(coef) - 1 / 3) <= 1e-6
+        if bits == 32:
+            c = [t / 3 for t in grads]
+            moments = [(0.1 * t, 0.001 * t * t) if moments is None else (0.9 * m + 0.1 * t, 0.999 * v + 0.001 * t * t) for t, (m, v) in zip(c, moments or [(0, 0)] * 2)]
+            for p, b, (m, v) in zip((run.param, run.router), before, moments):
+                t = step + 1
+                upd = (m / (1 - 0.9 ** t)) / (torch.sqrt(v / (1 - 0.999 ** t)) + 1e-8)
+                # (the coefficient's 1e-6 counts beside eps only; a dozen roundings of an update of up to 3)
+                assert ((p.double().cpu() - (b - lr * 0.01 * b - lr * upd)).abs() <= 2.0 ** -22 * b.abs() + lr * (2e-6 + 64 * 2.0 ** -24) * (1 + upd.abs())).all()
+        if bf16:
+            assert torch.equal(run.weight, run.param.to(run.dt)) and torch.equal(run.router_weight, run.router.to(run.dt))
+    run.close()
+
+
+def test_accumulated_batches():
+    """Two batches before one step: gradients add up, the tokens' do not."""
+    run = RoutedExpertRunner(3, 50, 2, 24, 16, bf16=False)
+    gen = torch.Generator().manual_seed(1)
+    run.load(torch.randn(3, 16, 25, generator=gen) * 0.2, torch.randn(1, 3, 24, generator=gen) * 0.2)
+    sums = [torch.zeros_like(run.grad), torch.zeros_like(run.router_grad)]
+    batches = [(torch.randn(50, 24, generator=gen).to(run.dev), torch.randn(50, 16, generator=gen).to(run.dev)) for _ in range(2)]
+    alone = []
+    for x, g in batches:
+        run.forward(x)
+        alone.append(run.backward(x, g).clone())
+        for s, t in zip(sums, (run.grad, run.router_grad)):
+            s += t
+    for i, (x, g) in enumerate(batches):
+        run.forward(x)
+        assert torch.equal(run.backward(x, g, accumulate=i > 0), alone[i])
+    for s, t in zip(sums, (run.grad, run.router_grad)):
+        assert relfro(t.double().cpu(), s.double().cpu()) <= 1e-6
+    run.close()
+
+
+def test_clip_of_other_runners():
+    """The gradients of a network in place, and the coefficient of a layer of experts."""
+    run = KfacRunner(S.workload("resnet32_cifar"), n_updates=1, batch=2, layers=[0, 3, 33])
+    run.restore_gradients()
+    raw = [g.double().cpu() for g in run.grad]
+    want = math.sqrt(sum(float((g ** 2).sum()) for g in raw))
+    run.clip(want / 2)
+    for g, r in zip(run.grad, raw):
+        assert relfro(g.double().cpu(), r / 2) <= 1e-6
+    assert abs(float(run.norm) - want) <= 1e-6 * want
+    run.clip(want)
+    assert float(run.coef) == 1.0
+    run.close()
+    run = ExpertRunner(2, 10, 8, 8)
+    run.grad.fill_(2.0)
+    n = math.sqrt(run.grad.numel() * 4.0)
+    assert abs(float(run.clip(n / 4, grad_scale=torch.full((1,), 0.5, device=run.dev))) - 0.25) <= 1e-6 and abs(float(run.norm) - n / 2) <= 1e-6 * n
+    run.close()

@@ -1,0 +1,517 @@
+"""The router's choice, tokens sorted by expert and back, and their gradients against their formulas in float64.
+
+Bounds.  An fp32 operation is off by at most 2^-24 of its result; exp by 2^-22 at most, and its argument, the difference of two logits, by 2^-24 of
+itself, which moves the result by that times D, the largest such difference: (D + 8) 2^-24 together.  A sum of K terms in any order is off by at most
+(K + 2) 2^-24 S (S: their magnitudes), products inside it by fma; one rounding to bf16 adds 2^-8 of the result, one to fp32 2^-24.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2007_00784_amd import kfac as K
+from gpu_util import Ctx
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = Ctx(8 << 20)
+    yield c
+    c.close()
+
+
+def half_step(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def near(got, want, bound):
+    got = got.detach().double().cpu()
+    bad = ~((got - want).abs() <= bound + 1e-37)
+    bad &= ~(got.isnan() & want.isnan())
+    assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
+
+
+def matrix(host, dt, pad=0, start=0, fill=math.nan):
+    """(device view of host in a buffer with a pitch and a start of its own, the buffer, whether an element of it is the view's)"""
+    R, d = host.shape
+    buf = torch.full((start + R * (d + pad),), fill, dtype=dt)
+    view = torch.as_strided(buf, (R, d), (d + pad, 1), start)
+    view.copy_(host)
+    mine = torch.zeros(buf.shape, dtype=torch.bool)
+    torch.as_strided(mine, (R, d), (d + pad, 1), start).fill_(True)
+    b = buf.to(DEV)
+    return torch.as_strided(b, (R, d), (d + pad, 1), start), b, mine
+
+
+STYLES = [dict(), dict(pad=8), dict(pad=3, start=1)]
+
+
+# ---------------------------------------------------------------- the router
+def choice(x, k):
+    """ids by a stable sort of float64 values (NaN as +inf, -inf never)."""
+    x = torch.where(x.isnan(), math.inf, x)
+    top, ids = torch.sort(x, dim=1, descending=True, stable=True)
+    return torch.where(top[:, :k] > -math.inf, ids[:, :k], -1).int()
+
+
+def softmax(x):
+    x = torch.where(x.isnan(), math.inf, x)
+    m = x.amax(1, keepdim=True)
+    e = torch.where(x > -math.inf, torch.exp(x - torch.where(m > -math.inf, m, 0.0)), 0.0)
+    e = torch.where(torch.isinf(m) & (m > 0), math.nan, e)
+    s = e.sum(1, keepdim=True)
+    return e / torch.where(s == 0, 1.0, s)
+
+
+def spread(x):
+    """D of the bounds, for each token."""
+    f = torch.where(x.isfinite(), x, math.nan)
+    top = torch.nan_to_num(f, nan=-1e9).amax(1, keepdim=True)
+    return torch.nan_to_num(top - f, nan=0.0).clamp(max=104.0).amax(1, keepdim=True)
+
+
+def weights_of(x, ids, normalize):
+    has = ids >= 0
+    chosen = torch.where(has, torch.gather(x, 1, ids.clamp(min=0).long()), -math.inf)
+    p = softmax(chosen) if normalize else torch.gather(softmax(x), 1, ids.clamp(min=0).long())
+    return torch.where(has, p, 0.0)
+
+
+def logits_for(T, E, kind, gen):
+    x = torch.randn(T, E, generator=gen) * 3
+    if kind == "ties":
+        x = (x * 0.7).round()
+    if kind == "masked":
+        x[torch.rand(T, E, generator=gen) < 0.5] = -math.inf
+        x[::3] = -math.inf
+        if T > 1:
+            x[1, 1:] = -math.inf
+    if kind == "lowest":
+        x[torch.rand(T, E, generator=gen) < 0.5] = torch.finfo(torch.bfloat16).min
+    return x
+
+
+ROUTES = [(1, 1, 1), (5, 2, 2), (33, 3, 1), (7, 15, 4), (70, 16, 16), (9, 17, 3), (130, 64, 8), (31, 65, 6), (257, 128, 8), (12, 129, 64), (6, 200, 2), (5, 256, 64), (3, 257, 8),
+          (4, 512, 4), (3, 513, 10), (2, 1000, 64), (3, 1024, 1), (2, 1025, 8), (2, 4095, 64), (1, 4096, 2)]
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties", "masked", "lowest"])
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("shape", ROUTES, ids=str)
+def test_route(ctx, shape, bf16, kind):
+    T, E, k = shape
+    gen = torch.Generator().manual_seed(T * 7919 + E)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    host = logits_for(T, E, kind, gen).to(dt)
+    x = host.double()
+    dw = torch.randn(T, k, generator=gen)
+    for normalize in (False, True):
+        style = STYLES[(T + E + normalize) % 3]
+        logits = matrix(host, dt, **style)[0]
+        ids = torch.full((T, k), 77, dtype=torch.int32, device=DEV)
+        w = torch.full((T, k), math.nan, device=DEV)
+        K.kfac_experts_route(ctx.h, logits, ids, w, normalize=normalize)
+        want = choice(x, k)
+        assert torch.equal(ids.cpu(), want)
+        ww = weights_of(x, want, normalize)
+        near(w, ww, (2 * (spread(x) + 8) + E + 4) * U * ww)
+        # the way back, with the smallest and largest index of nobody among the ids
+        given = want.clone()
+        if k > 1:
+            given[0, -1] = -2 ** 31
+            given[-1, 0] = E
+        out, buf, mine = matrix(torch.zeros(T, E), dt, fill=5.0, **style)
+        K.kfac_experts_route_grad(ctx.h, logits, given.to(DEV), dw.to(DEV), out, normalize=normalize)
+        given = torch.where((given >= 0) & (given < E), given, -1)
+        g, has, at = dw.double(), given >= 0, given.clamp(min=0).long()
+        if normalize:
+            p = weights_of(x, given, True)
+            d = p * (g - (p * g).sum(1, keepdim=True))
+            size = p * (g.abs() + (p * g.abs()).sum(1, keepdim=True))
+            grad, size = (torch.zeros_like(x).scatter_add_(1, at, torch.where(has, v, 0.0)) for v in (d, size))
+        else:
+            p = softmax(x)
+            at_e, size = (torch.zeros_like(x).scatter_add_(1, at, torch.where(has, v, 0.0)) for v in (g, g.abs()))
+            grad = p * (at_e - (p * at_e).sum(1, keepdim=True))
+            size = p * (size + (p * size).sum(1, keepdim=True))
+        # two softmaxes' errors (of p itself and inside the sum), the sum's and four operations
+        near(out, grad, (4 * (spread(x) + 8) + 2 * (E + 4) + k + 8) * U * size + half_step(dt) * grad.abs())
+        assert bool((buf.cpu()[~mine] == 5.0).all())
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("E", [9, 64, 300])
+def test_route_not_finite(ctx, E, bf16):
+    """NaN and +inf are chosen first and make the weights NaN, and the gradients of what they reach; -inf never."""
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x = torch.randn(6, E, generator=torch.Generator().manual_seed(E))
+    x[0, 3] = math.nan
+    x[1, E - 1] = math.inf
+    x[2, :] = math.nan
+    x[3, :] = -math.inf
+    x[4, 2], x[4, 5] = -math.inf, math.nan
+    logits = x.to(dt)
+    for normalize in (False, True):
+        ids = torch.zeros(6, 4, dtype=torch.int32, device=DEV)
+        w = torch.zeros(6, 4, device=DEV)
+        K.kfac_experts_route(ctx.h, logits.to(DEV), ids, w, normalize=normalize)
+        want = choice(logits.double(), 4)
+        assert torch.equal(ids.cpu(), want)
+        assert ids[0, 0] == 3 and ids[1, 0] == E - 1 and ids[2].tolist() == [0, 1, 2, 3] and ids[3].tolist() == [-1] * 4
+        assert w[[0, 1, 2, 4]].isnan().all() and (w[3] == 0).all() and w[5].isfinite().all()
+        out = torch.zeros(6, E, dtype=dt, device=DEV)
+        K.kfac_experts_route_grad(ctx.h, logits.to(DEV), ids, torch.ones(6, 4, device=DEV), out, normalize=normalize)
+        assert (out[3] == 0).all() and out[5].isfinite().all()
+        for t in (0, 1, 2, 4):
+            assert out[t][ids[t].long()].isnan().all()
+
+
+def test_route_gradient_by_differences(ctx):
+    """The gradient of a weighted sum of the weights against its central differences, by the kernel's own weights (fp32; where the choice stays)."""
+    T, E, k, h = 8, 24, 3, 2.0 ** -6
+    gen = torch.Generator().manual_seed(5)
+    x = (torch.randperm(T * E, generator=gen).view(T, E).float() / E).to(DEV)          # neighbours differ by 1 / 24 at least: more than 2 h
+    dw = torch.randn(T, k, generator=gen).to(DEV)
+    for normalize in (False, True):
+        ids, w = torch.zeros(T, k, dtype=torch.int32, device=DEV), torch.zeros(T, k, device=DEV)
+        out = torch.zeros(T, E, device=DEV)
+        K.kfac_experts_route(ctx.h, x, ids, w, normalize=normalize)
+        K.kfac_experts_route_grad(ctx.h, x, ids, dw, out, normalize=normalize)
+        for e in range(E):
+            loss = []
+            for s in (h, -h):
+                y = x.clone()
+                y[:, e] += s
+                i2, w2 = torch.zeros_like(ids), torch.zeros_like(w)
+                K.kfac_experts_route(ctx.h, y, i2, w2, normalize=normalize)
+                assert torch.equal(ids.sort(1)[0], i2.sort(1)[0])
+                order = (ids[:, :, None] == i2[:, None, :]).int().argmax(2)
+                loss.append((torch.gather(w2, 1, order).double() * dw.double()).sum(1))
+            diff = (loss[0] - loss[1]) / (2 * h)
+            # third derivatives of a softmax are below 1: h^2 / 6 |dw| each; weights are off by some 2^-20, over 2 h
+            bound = dw.double().abs().sum(1) * (h * h / 6 + 2 * 2.0 ** -20 / (2 * h))
+            assert ((diff - out[:, e].double()).abs() <= bound).all()
+
+
+# ---------------------------------------------------------------- the order of the slots
+def order_of(ids, E):
+    """(offsets, rows) in plain Python's order."""
+    flat = ids.reshape(-1).numpy()
+    good = (flat >= 0) & (flat < E)
+    order = np.argsort(np.where(good, flat, E), kind="stable")
+    rows = np.empty(flat.size, dtype=np.int64)
+    rows[order] = np.arange(flat.size)
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(flat[good], minlength=E))])
+    return torch.from_numpy(offsets).int(), torch.from_numpy(np.where(good, rows, -1)).int().view(ids.shape)
+
+
+def random_ids(T, k, E, gen, nobody=True):
+    """Skewed, the same expert more than once, and numbers of nobody: -1, E, the smallest and the largest."""
+    ids = (torch.rand(T, k, generator=gen) ** 2 * E).int().clamp(max=E - 1)
+    if nobody:
+        odd = torch.rand(T, k, generator=gen) < 0.1
+        ids[odd] = torch.tensor([-1, E, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32)[torch.randint(4, (int(odd.sum()),), generator=gen)]
+    return ids
+
+
+SORTS = [(1, 1, 1), (1, 64, 4), (8, 2, 8), (16, 64, 3), (17, 64, 4096), (512, 2, 300), (1024, 1, 4096), (1025, 1, 5), (513, 2, 64), (700, 8, 1), (3000, 7, 33), (4100, 64, 4096), (20000, 4, 1025),
+         (65536, 8, 128), (9, 3, 2)]
+
+
+@pytest.mark.parametrize("ws", [0, 5000, 8 << 20])
+@pytest.mark.parametrize("shape", SORTS, ids=str)
+def test_order(shape, ws):
+    """The order alone, with the workspace that it asks for, some and none."""
+    T, k, E = shape
+    c = Ctx(max(ws, 256))
+    try:
+        if ws == 0:
+            K.kfac_destroy(c.h)
+            c.h = K.kfac_create(0, c.stream.cuda_stream, None)
+        assert K.kfac_experts_dispatch_workspace_bytes(T, k, E) <= 8 << 20
+        ids = random_ids(T, k, E, torch.Generator().manual_seed(T + E))
+        offsets = torch.full((E + 1,), -7, dtype=torch.int32, device=DEV)
+        rows = torch.full((T, k), -7, dtype=torch.int32, device=DEV)
+        K.kfac_experts_dispatch(c.h, ids.to(DEV), None, offsets, rows, None)
+        want = order_of(ids, E)
+        assert torch.equal(offsets.cpu(), want[0]) and torch.equal(rows.cpu(), want[1])
+    finally:
+        c.close()
+
+
+def test_order_of_nothing(ctx):
+    """No tokens, or none with an expert."""
+    offsets = torch.full((9,), -7, dtype=torch.int32, device=DEV)
+    none = torch.zeros(0, 2, dtype=torch.int32, device=DEV)
+    K.kfac_experts_dispatch(ctx.h, none, torch.zeros(0, 16, device=DEV), offsets, none.clone(), torch.zeros(4, 16, device=DEV))
+    assert (offsets == 0).all()
+    for T in (3, 2000):
+        offsets.fill_(-7)
+        ids, rows = torch.full((T, 2), -1, dtype=torch.int32, device=DEV), torch.zeros(T, 2, dtype=torch.int32, device=DEV)
+        Xs = torch.full((2 * T, 24), 3.0, device=DEV)
+        K.kfac_experts_dispatch(ctx.h, ids, torch.ones(T, 24, device=DEV), offsets, rows, Xs)
+        assert (offsets == 0).all() and (rows == -1).all() and (Xs == 3.0).all()
+
+
+# T, k, E, d: few slots and many, rows of one lane, a wave's, a workgroup's and longer ones, cut among workgroups or not
+MOVES = [(1, 1, 1, 1), (1, 2, 4, 65536), (3, 2, 8, 7), (8, 2, 8, 2048), (40, 3, 5, 128), (33, 4, 16, 129), (200, 2, 10, 577), (90, 8, 30, 1000), (64, 16, 20, 2049),
+         (600, 2, 64, 9), (1030, 1, 3, 640), (400, 6, 100, 1031), (300, 4, 7, 5000), (2100, 3, 65, 64), (20, 64, 64, 260), (17, 64, 4096, 33)]
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("shape", range(len(MOVES)))
+def test_there_and_back(ctx, shape, bf16):
+    T, k, E, d = MOVES[shape]
+    gen = torch.Generator().manual_seed(shape)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    style = STYLES[shape % 3]
+    new = lambda R: torch.randn(R, d, generator=gen).to(dt)  # noqa: E731
+    ids = random_ids(T, k, E, gen)
+    R = T * k + shape % 4
+    offsets, rows = torch.zeros(E + 1, dtype=torch.int32, device=DEV), torch.zeros(T, k, dtype=torch.int32, device=DEV)
+    want_off, want_rows = order_of(ids, E)
+    has, at = want_rows >= 0, want_rows.clamp(min=0).long()
+    used = int(want_off[-1])
+    # there
+    x = new(T)
+    X = matrix(x, dt, **style)[0]
+    want = torch.full((R, d), 3.0, dtype=dt)
+    want[want_rows[has].long()] = x.repeat_interleave(k, 0)[has.view(-1)]
+    for again in (False, True):
+        Xs, buf, mine = matrix(torch.full((R, d), 3.0), dt, fill=5.0, **style)
+        if again:
+            K.kfac_experts_gather(ctx.h, rows, X, Xs)
+        else:
+            K.kfac_experts_dispatch(ctx.h, ids.to(DEV), X, offsets, rows, Xs)
+            assert torch.equal(offsets.cpu(), want_off) and torch.equal(rows.cpu(), want_rows)
+        assert torch.equal(Xs.cpu(), want) and bool((buf.cpu()[~mine] == 5.0).all())
+    # back; rows and weights of no slot are NaN
+    y = new(R)
+    y[used:] = math.nan
+    Ys = matrix(y, dt, **style)[0]
+    w = torch.randn(T, k, generator=gen)
+    w[~has] = math.nan
+    odd = rows.clone()
+    odd[~has.to(DEV)] = torch.tensor([-1, R, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32, device=DEV)[torch.arange(int((~has).sum()), device=DEV) % 4]
+    taken = torch.where(has[:, :, None], torch.nan_to_num(y[:, :].double())[at], 0.0)
+    a = new(T)
+    for weights in (w, None):
+        ww = torch.where(has, w.double(), 0.0)[:, :, None] if weights is not None else 1.0
+        for add in (False, True, "in place"):
+            out, buf, mine = matrix(a if add == "in place" else torch.full((T, d), 3.0), dt, fill=5.0, **style)
+            A = None if not add else out if add == "in place" else matrix(a, dt, **STYLES[(shape + 1) % 3])[0]
+            K.kfac_experts_combine(ctx.h, Ys, odd, None if weights is None else weights.to(DEV), out, add=A)
+            want = (taken * ww).sum(1) + (a.double() if add else 0.0)
+            size = (taken * ww).abs().sum(1) + (a.double().abs() if add else 0.0)
+            near(out, want, (k + 2) * U * size + half_step(dt) * want.abs())
+            assert bool((buf.cpu()[~mine] == 5.0).all())
+    # and its gradients
+    g = new(T)
+    dYs, buf, mine = matrix(torch.full((R, d), 3.0), dt, fill=5.0, **style)
+    dw = torch.full((T, k), math.nan, device=DEV)
+    K.kfac_experts_combine_grad(ctx.h, matrix(g, dt, **style)[0], Ys, odd, w.to(DEV), dYs, dw)
+    want = torch.full((R, d), 3.0, dtype=torch.float64)
+    want[want_rows[has].long()] = (w.double()[:, :, None] * g.double()[:, None, :])[has]
+    near(dYs, want, (U + half_step(dt)) * want.abs())
+    assert bool((dYs[used:] == 3.0).all()) and bool((buf.cpu()[~mine] == 5.0).all())
+    near(dw, (taken * g.double()[:, None, :]).sum(2), (d + 2) * U * (taken * g.double()[:, None, :]).abs().sum(2))
+
+
+def test_values_pass_unchanged(ctx):
+    """Copies are copies, a weight of one changes nothing, and what is not finite passes: every bf16 there is."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(256, 256)
+    x = bits.view(torch.bfloat16).to(DEV)
+    ids = torch.randint(0, 5, (256, 1), generator=torch.Generator().manual_seed(1), dtype=torch.int32).to(DEV)
+    offsets, rows = torch.zeros(6, dtype=torch.int32, device=DEV), torch.zeros(256, 1, dtype=torch.int32, device=DEV)
+    Xs, Y, dYs = (torch.zeros_like(x) for _ in range(3))
+    K.kfac_experts_dispatch(ctx.h, ids, x, offsets, rows, Xs)
+    assert torch.equal(Xs.view(torch.int16)[rows[:, 0].long()], x.view(torch.int16))
+    one, dw = torch.ones(256, 1, device=DEV), torch.zeros(256, 1, device=DEV)
+    K.kfac_experts_combine(ctx.h, Xs, rows, one, Y)
+    K.kfac_experts_combine_grad(ctx.h, x, Xs, rows, one, dYs, dw)
+    same = lambda a: (a == x) | (a.isnan() & x.isnan())  # noqa: E731
+    assert same(Y).all() and same(dYs[rows[:, 0].long()]).all()
+    # halves go to the even neighbour: 1 + 2^-8 (3 times) between two bf16 numbers
+    v = torch.tensor([[1.0, 1.0078125, 1.015625, -1.0078125] * 4], dtype=torch.bfloat16, device=DEV)
+    y = torch.zeros(1, 16, dtype=torch.bfloat16, device=DEV)
+    w = torch.tensor([[1.0 + 2.0 ** -8]], device=DEV)
+    K.kfac_experts_combine(ctx.h, v, torch.zeros(1, 1, dtype=torch.int32, device=DEV), w, y)
+    assert torch.equal(y, (v.float() * w).to(torch.bfloat16))
+
+
+def test_no_rows(ctx):
+    """An experts' matrix without rows: every slot is nobody's."""
+    rows = torch.zeros(3, 2, dtype=torch.int32, device=DEV)
+    w, dw = torch.ones(3, 2, device=DEV), torch.full((3, 2), 9.0, device=DEV)
+    empty, Y, add = torch.zeros(0, 20, device=DEV), torch.full((3, 20), 9.0, device=DEV), torch.randn(3, 20, device=DEV)
+    K.kfac_experts_combine(ctx.h, empty, rows, w, Y)
+    assert (Y == 0).all()
+    K.kfac_experts_combine(ctx.h, empty, rows, None, Y, add=add)
+    assert torch.equal(Y, add)
+    K.kfac_experts_combine_grad(ctx.h, add, empty, rows, w, empty.clone(), dw)
+    assert (dw == 0).all()
+    K.kfac_experts_gather(ctx.h, rows, add, empty)
+
+
+def test_combine_gradient_by_differences(ctx):
+    """<G, Y> is linear in the weights and in the rows, so its differences are its gradient but for roundings."""
+    T, k, E, d = 6, 2, 4, 40
+    gen = torch.Generator().manual_seed(2)
+    ids = torch.randint(0, E, (T, k), generator=gen, dtype=torch.int32)
+    rows = order_of(ids, E)[1].to(DEV)
+    Ys, w, G = torch.randn(T * k, d, generator=gen).to(DEV), torch.randn(T, k, generator=gen).to(DEV), torch.randn(T, d, generator=gen).to(DEV)
+    dYs, dw = torch.zeros_like(Ys), torch.zeros_like(w)
+    K.kfac_experts_combine_grad(ctx.h, G, Ys, rows, w, dYs, dw)
+
+    def loss(Ys, w):
+        Y = torch.zeros(T, d, device=DEV)
+        K.kfac_experts_combine(ctx.h, Ys, rows, w, Y)
+        return (Y.double() * G.double()).sum()
+
+    size = float((torch.zeros(T, d, device=DEV).add_(1.0) * G.abs()).sum()) * 12       # of the sums: |w Ys| stays below six here
+    for t, j in ((0, 0), (3, 1), (5, 0)):
+        step = torch.zeros_like(w)
+        step[t, j] = 1.0
+        assert abs(float(loss(Ys, w + step) - loss(Ys, w) - dw[t, j])) <= 64 * U * size
+    for r, c in ((0, 0), (7, 39), (11, 8)):
+        step = torch.zeros_like(Ys)
+        step[r, c] = 1.0
+        assert abs(float(loss(Ys + step, w) - loss(Ys, w) - dYs[r, c])) <= 64 * U * size
+
+
+# ---------------------------------------------------------------- as they are used
+class Chain:
+    """Route, sort, product, back, and the way back again, over buffers of one batch."""
+
+    def __init__(self, T, E, k, d, d_out, dt, normalize):
+        new = lambda *s, dtype=dt: torch.zeros(*s, dtype=dtype, device=DEV)  # noqa: E731
+        self.normalize = normalize
+        self.logits, self.dlogits = new(T, E), new(T, E)
+        self.ids, self.rows = new(T, k, dtype=torch.int32), new(T, k, dtype=torch.int32)
+        self.w, self.dw = new(T, k, dtype=torch.float32), new(T, k, dtype=torch.float32)
+        self.offsets = new(E + 1, dtype=torch.int32)
+        self.x, self.xs, self.ys, self.y = new(T, d), new(T * k, d), new(T * k, d_out), new(T, d_out)
+        self.g, self.gs, self.dxs, self.dx = new(T, d_out), new(T * k, d_out), new(T * k, d), new(T, d)
+        self.W = (torch.randn(E, d_out, d, generator=torch.Generator().manual_seed(0)) * d ** -0.5).to(dt).to(DEV)
+
+    def fill(self, seed):
+        gen = torch.Generator().manual_seed(seed)
+        for t in (self.logits, self.x, self.g):
+            t.copy_(torch.randn(t.shape, generator=gen))
+        self.logits[torch.arange(seed % 3, self.logits.shape[0], 5)] = -math.inf
+        torch.cuda.synchronize()
+
+    def run(self, h):
+        K.kfac_experts_route(h, self.logits, self.ids, self.w, normalize=self.normalize)
+        K.kfac_experts_dispatch(h, self.ids, self.x, self.offsets, self.rows, self.xs)
+        K.kfac_experts_forward(h, self.xs, self.W, self.offsets, self.ys)
+        K.kfac_experts_combine(h, self.ys, self.rows, self.w, self.y, add=None)
+        K.kfac_experts_combine_grad(h, self.g, self.ys, self.rows, self.w, self.gs, self.dw)
+        K.kfac_experts_input_grad(h, self.gs, self.W, self.offsets, self.dxs)
+        K.kfac_experts_combine(h, self.dxs, self.rows, None, self.dx)
+        K.kfac_experts_route_grad(h, self.logits, self.ids, self.dw, self.dlogits, normalize=self.normalize)
+
+    def outputs(self):
+        return [t.clone() for t in (self.ids, self.w, self.offsets, self.rows, self.y, self.dx, self.dw, self.dlogits)]
+
+
+@pytest.mark.parametrize("T,E,k", [(40, 8, 2), (700, 40, 3)])
+def test_captured(T, E, k):
+    """A captured run against eager ones of the same inputs, over several replays with eager work between them."""
+    side = torch.cuda.Stream()
+    ws = torch.empty(8 << 20, dtype=torch.uint8, device=DEV)
+    eager = Ctx(8 << 20)
+    with torch.cuda.stream(side):
+        h = K.kfac_create(0, side.cuda_stream, ws)
+    try:
+        a, b = Chain(T, E, k, 72, 40, torch.bfloat16, True), Chain(T, E, k, 72, 40, torch.bfloat16, True)
+        a.fill(0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            a.run(h)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            a.run(h)
+        for seed in (1, 2, 3):
+            a.fill(seed)
+            b.fill(seed)
+            graph.replay()
+            torch.cuda.synchronize()
+            b.run(eager.h)
+            torch.cuda.synchronize()
+            for x, y in zip(a.outputs(), b.outputs()):
+                assert torch.equal(x, y)
+    finally:
+        torch.cuda.synchronize()
+        K.kfac_destroy(h)
+        eager.close()
+
+
+def test_two_contexts_at_once():
+    """Contexts of two streams, each with its own workspace, run side by side."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.empty(8 << 20, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    handles = [K.kfac_create(0, s.cuda_stream, w) for s, w in zip(streams, spaces)]
+    alone = Ctx(8 << 20)
+    try:
+        chains = [Chain(2000, 24, 4, 136, 72, torch.float32, False) for _ in range(3)]
+        for i, c in enumerate(chains[:2]):
+            c.fill(i + 10)
+        for _ in range(3):
+            for c, h in zip(chains, handles):
+                c.run(h)
+        torch.cuda.synchronize()
+        for i in range(2):
+            chains[2].fill(i + 10)
+            chains[2].run(alone.h)
+            torch.cuda.synchronize()
+            for x, y in zip(chains[i].outputs(), chains[2].outputs()):
+                assert torch.equal(x, y)
+    finally:
+        torch.cuda.synchronize()
+        for h in handles:
+            K.kfac_destroy(h)
+        alone.close()
+
+
+def test_far_elements(ctx):
+    """Matrices whose last row begins behind 2^31 elements: the same results as from small ones."""
+    T, k, E, d, pitch = 1100, 2, 5, 72, 1 << 20
+    gen = torch.Generator().manual_seed(4)
+    ids = random_ids(T, k, E, gen).to(DEV)
+    far = [torch.empty((2 * T - 1) * pitch + d, dtype=torch.bfloat16, device=DEV).as_strided((2 * T, d), (pitch, 1)) for _ in range(2)]
+    assert (2 * T - 1) * pitch > 1 << 31
+    x, g = torch.randn(T, d, generator=gen).bfloat16().to(DEV), torch.randn(T, d, generator=gen).bfloat16().to(DEV)
+    w = torch.rand(T, k, generator=gen).to(DEV)
+    results = []
+    for Xs, dYs in (far, [torch.empty(2 * T, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]):
+        offsets, rows = torch.zeros(E + 1, dtype=torch.int32, device=DEV), torch.zeros(T, k, dtype=torch.int32, device=DEV)
+        for m in (Xs, dYs):
+            m.zero_()
+        Y, dw = torch.zeros(T, d, dtype=torch.bfloat16, device=DEV), torch.zeros(T, k, device=DEV)
+        K.kfac_experts_dispatch(ctx.h, ids, x, offsets, rows, Xs)
+        K.kfac_experts_combine(ctx.h, Xs, rows, w, Y)
+        K.kfac_experts_combine_grad(ctx.h, g, Xs, rows, w, dYs, dw)
+        results.append([offsets, rows, Xs.clone(), Y, dYs.clone(), dw])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    # and logits
+    n = 2100
+    wide = torch.empty((n - 1) * pitch + 40, dtype=torch.bfloat16, device=DEV).as_strided((n, 40), (pitch, 1))
+    logits = torch.randn(n, 40, generator=gen).bfloat16().to(DEV)
+    wide.copy_(logits)
+    results = []
+    for m in (wide, logits):
+        ids, w = torch.zeros(n, 4, dtype=torch.int32, device=DEV), torch.zeros(n, 4, device=DEV)
+        K.kfac_experts_route(ctx.h, m, ids, w)
+        out = far[0].as_strided((n, 40), (pitch, 1)) if m is wide else torch.empty_like(logits)
+        K.kfac_experts_route_grad(ctx.h, m, ids, w, out)
+        results.append([ids, w, out.clone()])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
