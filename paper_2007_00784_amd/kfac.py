@@ -191,13 +191,17 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_codes = {}              # torch dtype -> kfac_dtype; filled at the first use, so that importing this module does not import torch
+
+
 def _dtype_code(t):
-    import torch
-    if t.dtype == torch.float32:
-        return KFAC_F32
-    if t.dtype == torch.bfloat16:
-        return KFAC_BF16
-    raise ValueError("unsupported dtype %s" % t.dtype)
+    dtype = t.dtype
+    if dtype not in _codes:
+        import torch
+        _codes.update({torch.float32: KFAC_F32, torch.bfloat16: KFAC_BF16})
+        if dtype not in _codes:
+            raise ValueError("unsupported dtype %s" % dtype)
+    return _codes[dtype]
 
 
 def _check(rc, where, allow=()):
@@ -428,13 +432,16 @@ def _c_int(n):
 
 def _rows(t, name, d):
     """(address, row pitch) of a matrix of samples [R][d]: any pitch, but the elements of a row side by side."""
-    if t.dim() != 2 or t.shape[1] != d:
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != d:
         raise ValueError("%s must be [R, %d]" % (name, d))
-    if t.shape[0] == 0:
+    if shape[0] == 0:
         return None, d
-    if d > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if d > 1 and step != 1:
         raise ValueError("the rows of %s must be contiguous" % name)
-    ld = t.stride(0) if t.shape[0] > 1 else d
+    if shape[0] == 1:
+        ld = d
     if ld < d:
         raise ValueError("the rows of %s overlap" % name)
     return t.data_ptr(), ld
@@ -530,48 +537,77 @@ def kfac_update_factors_experts(ctx, X, offsets, F, append_ones=False, scale=1.0
 
 
 # ---- tokens to experts and back ----
-def _slots(t, name, dtype, shape=None):
-    """A contiguous matrix [tokens, topk] of one entry for each slot."""
-    if t.dtype != dtype or t.dim() != 2 or (shape is not None and t.shape != shape):
-        raise ValueError("%s must be %s [tokens, topk]" % (name, dtype))
+# (Calls of a few microseconds: what a tensor is asked for, it is asked once.)
+_slot_types = {}         # torch dtype -> whether it is the one of ids and rows
+
+
+def _slots(t, name, shape=None, ints=True):
+    """(address, shape) of a contiguous matrix [tokens, topk] with an int32 or a float32 for each slot."""
+    mine = t.shape
+    if len(mine) != 2 or (shape is not None and mine != shape):
+        raise ValueError("%s must be [tokens, topk]" % name)
+    dtype = t.dtype
+    if dtype not in _slot_types:
+        import torch
+        _slot_types.update({torch.int32: True, torch.float32: False})
+    if _slot_types.get(dtype) is not ints:
+        raise ValueError("%s must be %s" % (name, "int32" if ints else "float32"))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr()
+    return t.data_ptr(), mine
+
+
+def _matrix(t, name, dtype, rows=None, width=None):
+    """(address, row pitch, rows, columns) of a matrix of samples: any pitch, but the elements of a row side by side."""
+    shape = t.shape
+    n, d = shape if len(shape) == 2 else (-1, -1)
+    if d < 0 or (rows is not None and n != rows) or (width is not None and d != width):
+        raise ValueError("%s must be [%s, %s]" % (name, "R" if rows is None else rows, "d" if width is None else width))
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s as the others" % (name, dtype))
+    if n == 0:
+        return None, d, n, d
+    ld, step = t.stride()
+    if d > 1 and step != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    if n == 1:
+        ld = d
+    if ld < d:
+        raise ValueError("the rows of %s overlap" % name)
+    return t.data_ptr(), ld, n, d
+
+
+_MOST = (1 << 31) - 1    # of a C int
+
+
+def _slot_desc(tokens, topk, rows, width, dtype):
+    if tokens > _MOST or topk > _MOST or rows > _MOST or width > _MOST:      # (refused by the library; ctypes would cut it)
+        tokens = -1
+    return ctypes.byref(kfac_slot_desc(tokens, topk, rows, width, dtype))
 
 
 def kfac_experts_route(ctx, logits, ids, weights, normalize=False):
     """ids[t] = the experts of the topk largest logits of token t (ties to the lowest index; -1 where only logits of -inf are left), weights[t] their
     softmax over all experts, or with normalize over those chosen.  logits [tokens, experts] (any row pitch), ids int32 and weights float32
     [tokens, topk]: written."""
-    import torch
-    ip = _slots(ids, "ids", torch.int32)
-    wp = _slots(weights, "weights", torch.float32, ids.shape)
-    if logits.dim() != 2 or logits.shape[0] != ids.shape[0]:
-        raise ValueError("logits must be [tokens, experts]")
-    tokens, experts = logits.shape
-    lp, ldl = _rows(logits, "logits", experts)
     code = _dtype_code(logits)
+    ip, shape = _slots(ids, "ids")
+    wp, _ = _slots(weights, "weights", shape, False)
+    lp, ldl, tokens, experts = _matrix(logits, "logits", logits.dtype, shape[0])
     _on_gpu(logits, ids, weights)
-    _check(lib().kfac_experts_route(ctx, _c_int(tokens), _c_int(experts), _c_int(ids.shape[1]), lp, code, ldl, int(bool(normalize)), ip, wp), "kfac_experts_route")
+    _check(lib().kfac_experts_route(ctx, _c_int(tokens), _c_int(experts), _c_int(shape[1]), lp, code, ldl, 1 if normalize else 0, ip, wp), "kfac_experts_route")
 
 
 def kfac_experts_route_grad(ctx, logits, ids, dweights, dlogits, normalize=False):
     """The gradient of the logits (written to dlogits, of their shape and dtype) from that of the weights; logits, ids and normalize as in
     kfac_experts_route()."""
-    import torch
-    ip = _slots(ids, "ids", torch.int32)
-    wp = _slots(dweights, "dweights", torch.float32, ids.shape)
-    if logits.dim() != 2 or logits.shape[0] != ids.shape[0]:
-        raise ValueError("logits must be [tokens, experts]")
-    _same(logits, dlogits, "logits and dlogits")
-    tokens, experts = logits.shape
-    if dlogits.dim() != 2 or dlogits.shape[0] != tokens:
-        raise ValueError("logits and dlogits must have one shape")
-    lp, ldl = _rows(logits, "logits", experts)
-    dp, ldd = _rows(dlogits, "dlogits", experts)
-    code = _dtype_code(logits)
+    code, dtype = _dtype_code(logits), logits.dtype
+    ip, shape = _slots(ids, "ids")
+    wp, _ = _slots(dweights, "dweights", shape, False)
+    lp, ldl, tokens, experts = _matrix(logits, "logits", dtype, shape[0])
+    dp, ldd, _, _ = _matrix(dlogits, "dlogits", dtype, tokens, experts)
     _on_gpu(logits, ids, dweights, dlogits)
-    _check(lib().kfac_experts_route_grad(ctx, _c_int(tokens), _c_int(experts), _c_int(ids.shape[1]), lp, code, ldl, ip, wp, int(bool(normalize)), dp, ldd),
+    _check(lib().kfac_experts_route_grad(ctx, _c_int(tokens), _c_int(experts), _c_int(shape[1]), lp, code, ldl, ip, wp, 1 if normalize else 0, dp, ldd),
            "kfac_experts_route_grad")
 
 
@@ -584,90 +620,67 @@ def kfac_experts_dispatch(ctx, ids, X, offsets, rows, Xs):
     """Sorts the slots by expert and copies the tokens there: offsets (int32 [experts + 1]) and Xs [at least tokens * topk, d] are what the products for
     layers of experts take, rows (int32 [tokens, topk]) says where each slot went (-1: it has no expert, its id is outside 0 .. experts - 1).
     X [tokens, d]; ids int32 [tokens, topk].  X = Xs = None: the order alone."""
-    import torch
-    ip = _slots(ids, "ids", torch.int32)
-    rp = _slots(rows, "rows", torch.int32, ids.shape)
-    if offsets.dim() != 1 or offsets.shape[0] < 2:
+    ip, shape = _slots(ids, "ids")
+    rp, _ = _slots(rows, "rows", shape)
+    tokens, topk = shape
+    experts = offsets.numel() - 1
+    if experts < 1:
         raise ValueError("offsets must be int32 [experts + 1]")
-    experts = offsets.shape[0] - 1
-    _offsets(offsets, experts)
-    tokens, topk = ids.shape
+    op = _offsets(offsets, experts).data_ptr()
     if (X is None) != (Xs is None):
         raise ValueError("both X and Xs or none")
     xp = sp = None
     ldx = lds = 0
     if X is None:
-        d = kfac_slot_desc(_c_int(tokens), _c_int(topk), _c_int(tokens * topk), 0, KFAC_F32)
+        d = _slot_desc(tokens, topk, tokens * topk, 0, KFAC_F32)
     else:
-        if X.dim() != 2 or X.shape[0] != tokens:
-            raise ValueError("X must be [tokens, d]")
-        _same(X, Xs, "X and Xs")
-        if Xs.shape[0] < tokens * topk:
+        code, dtype = _dtype_code(X), X.dtype
+        xp, ldx, _, width = _matrix(X, "X", dtype, tokens)
+        sp, lds, R, _ = _matrix(Xs, "Xs", dtype, None, width)
+        if R < tokens * topk:
             raise ValueError("Xs must have a row for each slot")
-        xp, ldx = _rows(X, "X", X.shape[1])
-        sp, lds = _rows(Xs, "Xs", X.shape[1])
-        d = kfac_slot_desc(_c_int(tokens), _c_int(topk), _c_int(Xs.shape[0]), _c_int(X.shape[1]), _dtype_code(X))
+        d = _slot_desc(tokens, topk, R, width, code)
     _on_gpu(ids, X, offsets, rows, Xs)
-    _check(lib().kfac_experts_dispatch(ctx, ctypes.byref(d), _c_int(experts), ip, xp, ldx, offsets.data_ptr(), rp, sp, lds), "kfac_experts_dispatch")
+    _check(lib().kfac_experts_dispatch(ctx, d, _c_int(experts), ip, xp, ldx, op, rp, sp, lds), "kfac_experts_dispatch")
 
 
 def kfac_experts_gather(ctx, rows, X, Xs):
     """Xs[rows[t, j]] = X[t], rows as kfac_experts_dispatch() left them."""
-    import torch
-    rp = _slots(rows, "rows", torch.int32)
-    if X.dim() != 2 or X.shape[0] != rows.shape[0]:
-        raise ValueError("X must be [tokens, d]")
-    _same(X, Xs, "X and Xs")
-    xp, ldx = _rows(X, "X", X.shape[1])
-    sp, lds = _rows(Xs, "Xs", X.shape[1])
-    d = kfac_slot_desc(_c_int(rows.shape[0]), _c_int(rows.shape[1]), _c_int(Xs.shape[0]), _c_int(X.shape[1]), _dtype_code(X))
+    rp, (tokens, topk) = _slots(rows, "rows")
+    code, dtype = _dtype_code(X), X.dtype
+    xp, ldx, _, width = _matrix(X, "X", dtype, tokens)
+    sp, lds, R, _ = _matrix(Xs, "Xs", dtype, None, width)
     _on_gpu(rows, X, Xs)
-    _check(lib().kfac_experts_gather(ctx, ctypes.byref(d), rp, xp, ldx, sp, lds), "kfac_experts_gather")
+    _check(lib().kfac_experts_gather(ctx, _slot_desc(tokens, topk, R, width, code), rp, xp, ldx, sp, lds), "kfac_experts_gather")
 
 
 def kfac_experts_combine(ctx, Ys, rows, weights, Y, add=None):
     """Y[t] = add[t] + sum over j of weights[t, j] Ys[rows[t, j]].  Ys [R, d], rows int32 [tokens, topk], weights float32 [tokens, topk] or None (ones: the
     gradient of kfac_experts_dispatch()), Y [tokens, d], add [tokens, d] or None, or Y itself."""
-    import torch
-    rp = _slots(rows, "rows", torch.int32)
-    wp = None if weights is None else _slots(weights, "weights", torch.float32, rows.shape)
-    if Y.dim() != 2 or Y.shape[0] != rows.shape[0]:
-        raise ValueError("Y must be [tokens, d]")
-    _same(Ys, Y, "Ys and Y")
-    tokens, width = Y.shape
-    sp, lds = _rows(Ys, "Ys", width)
-    yp, ldy = _rows(Y, "Y", width)
-    ap, lda = None, 0
-    if add is not None:
-        _same(add, Y, "add and Y")
-        if add.shape[0] != tokens:
-            raise ValueError("add and Y must have as many rows")
-        ap, lda = _rows(add, "add", width)
-    d = kfac_slot_desc(_c_int(tokens), _c_int(rows.shape[1]), _c_int(Ys.shape[0]), _c_int(width), _dtype_code(Y))
+    rp, shape = _slots(rows, "rows")
+    wp = None if weights is None else _slots(weights, "weights", shape, False)[0]
+    tokens, topk = shape
+    code, dtype = _dtype_code(Y), Y.dtype
+    yp, ldy, _, width = _matrix(Y, "Y", dtype, tokens)
+    sp, lds, R, _ = _matrix(Ys, "Ys", dtype, None, width)
+    ap, lda, _, _ = (None, 0, 0, 0) if add is None else _matrix(add, "add", dtype, tokens, width)
     _on_gpu(Ys, rows, weights, Y, add)
-    _check(lib().kfac_experts_combine(ctx, ctypes.byref(d), rp, wp, sp, lds, ap, lda, yp, ldy), "kfac_experts_combine")
+    _check(lib().kfac_experts_combine(ctx, _slot_desc(tokens, topk, R, width, code), rp, wp, sp, lds, ap, lda, yp, ldy), "kfac_experts_combine")
 
 
 def kfac_experts_combine_grad(ctx, dY, Ys, rows, weights, dYs, dweights):
     """dYs[rows[t, j]] = weights[t, j] dY[t] and dweights[t, j] = <dY[t], Ys[rows[t, j]]>: the gradients of kfac_experts_combine().  dY [tokens, d], Ys and dYs
     [R, d], weights and dweights float32 [tokens, topk]."""
-    import torch
-    rp = _slots(rows, "rows", torch.int32)
-    wp = _slots(weights, "weights", torch.float32, rows.shape)
-    gp = _slots(dweights, "dweights", torch.float32, rows.shape)
-    if dY.dim() != 2 or dY.shape[0] != rows.shape[0]:
-        raise ValueError("dY must be [tokens, d]")
-    _same(dY, Ys, "dY and Ys")
-    _same(dY, dYs, "dY and dYs")
-    if dYs.shape[0] != Ys.shape[0]:
-        raise ValueError("Ys and dYs must have as many rows")
-    tokens, width = dY.shape
-    yp, ldy = _rows(dY, "dY", width)
-    sp, lds = _rows(Ys, "Ys", width)
-    op, ldo = _rows(dYs, "dYs", width)
-    d = kfac_slot_desc(_c_int(tokens), _c_int(rows.shape[1]), _c_int(Ys.shape[0]), _c_int(width), _dtype_code(dY))
+    rp, shape = _slots(rows, "rows")
+    wp, _ = _slots(weights, "weights", shape, False)
+    gp, _ = _slots(dweights, "dweights", shape, False)
+    tokens, topk = shape
+    code, dtype = _dtype_code(dY), dY.dtype
+    yp, ldy, _, width = _matrix(dY, "dY", dtype, tokens)
+    sp, lds, R, _ = _matrix(Ys, "Ys", dtype, None, width)
+    op, ldo, _, _ = _matrix(dYs, "dYs", dtype, R, width)
     _on_gpu(dY, Ys, rows, weights, dYs, dweights)
-    _check(lib().kfac_experts_combine_grad(ctx, ctypes.byref(d), rp, wp, yp, ldy, sp, lds, op, ldo, gp), "kfac_experts_combine_grad")
+    _check(lib().kfac_experts_combine_grad(ctx, _slot_desc(tokens, topk, R, width, code), rp, wp, yp, ldy, sp, lds, op, ldo, gp), "kfac_experts_combine_grad")
 
 
 # ---- the global gradient norm ----

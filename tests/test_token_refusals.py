@@ -199,9 +199,9 @@ def test_counts_that_no_c_int_holds(monkeypatch):
     """2^32 + 6 tokens are not six tokens: the library gets a number that it refuses."""
     many = (1 << 32) + 6
     monkeypatch.setattr(K, "_on_gpu", lambda *tensors: None)
-    monkeypatch.setattr(K, "_slots", lambda t, name, dtype, shape=None: 64)
-    rows = K._rows
-    monkeypatch.setattr(K, "_rows", lambda t, name, d: (128 if name in ("X", "Ys", "logits") else 256, rows(t, name, d)[1]))
+    monkeypatch.setattr(K, "_slots", lambda t, name, shape=None, ints=True: (64, t.shape))
+    matrix = K._matrix
+    monkeypatch.setattr(K, "_matrix", lambda t, name, *a: (128 if name in ("X", "Ys", "logits") else 256,) + matrix(t, name, *a)[1:])
     empty = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="meta")  # noqa: E731
     ids, w, X, Xs = empty(many, 2), empty(many, 2), empty(many, 8), empty(2 * many, 8)
     off = torch.zeros(5, dtype=torch.int32)
