@@ -16,6 +16,16 @@ template <typename T, int N> __device__ inline Vec<T, N> load(const void *p, int
 template <typename T, int N> __device__ inline void store(void *p, int64_t i, const Vec<T, N> &r) {
     __builtin_memcpy((char *)p + i * (int64_t)sizeof(T), &r, sizeof(r));
 }
+// The same past the caches, for what is too long to stay there or is not read again by this launch.
+typedef unsigned AnyVector __attribute__((ext_vector_type(4), aligned(1)));
+template <typename T, int N> __device__ inline Vec<T, N> load_past(const void *p, int64_t i) {
+    static_assert(sizeof(Vec<T, N>) == 16, "one vector");
+    return __builtin_bit_cast(Vec<T, N>, (AnyVector)__builtin_nontemporal_load((const AnyVector *)((const char *)p + i * (int64_t)sizeof(T))));
+}
+template <typename T, int N> __device__ inline void store_past(void *p, int64_t i, const Vec<T, N> &r) {
+    static_assert(sizeof(Vec<T, N>) == 16, "one vector");
+    __builtin_nontemporal_store(__builtin_bit_cast(AnyVector, r), (AnyVector *)((char *)p + i * (int64_t)sizeof(T)));
+}
 __device__ inline float widen(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
 __device__ inline unsigned short round_bf16(float x) {   // half to even; NaN stays NaN
     const unsigned u = __float_as_uint(x);

@@ -3,8 +3,8 @@
 //   norm = |scale| sqrt(sum over all tensors of g^2);  coef = scale min(1, max_norm / norm);  clip: out = g coef
 //
 // Squares and sums are in 64 bits: the square of an fp32 gradient need not have one in fp32 (above 2^64, below 2^-75), and of many small terms
-// behind a large sum fp32 would lose most.  A first launch leaves one sum for each workgroup, a second of one workgroup adds them in a fixed
-// order, so the result is the same from run to run.  Both are bound by memory.
+// behind a large sum fp32 would lose most.  A first launch leaves one sum for each workgroup; a second adds them in a fixed order, so that the
+// result is the same from run to run: one workgroup for the norm alone, every workgroup for itself where it goes on to clip.  Bound by memory.
 #include <algorithm>
 #include <cmath>
 #include "kfac_internal.h"
@@ -16,9 +16,9 @@ namespace {
 
 constexpr int ITEMS = 100;           // tensors of a launch: the table and the rest of the arguments stay below 4 KB
 constexpr int THREADS = 256;
-constexpr int BYTES = 16;            // of a vector
-constexpr int UNROLL = 4;            // vectors of a thread and chunk
-constexpr int MOST = 2048;           // workgroups of a launch that sums
+constexpr int UNROLL = 4;            // vectors of 16 bytes of a thread and chunk
+constexpr int64_t CHUNK = 16 * THREADS * UNROLL;      // bytes
+constexpr int MOST = 1024;           // workgroups of a launch that sums
 
 struct GradItem {
     const void *g;
@@ -32,9 +32,8 @@ struct GradLaunch {
     int n;
     uint32_t chunks;
     double *part;                    // one sum for each workgroup
-    const float *coef;
 };
-static_assert(sizeof(GradLaunch) <= 4096, "arguments of a launch");
+static_assert(sizeof(GradLaunch) <= 4000, "arguments of a launch");
 
 __device__ inline int item_of(const GradLaunch &a, unsigned chunk) {   // the last tensor whose first chunk is not behind this one
     const int lane = threadIdx.x & 63;
@@ -43,36 +42,37 @@ __device__ inline int item_of(const GradLaunch &a, unsigned chunk) {   // the la
     return __builtin_amdgcn_readfirstlane(before - 1);
 }
 
-template <typename T> constexpr int64_t chunk_elements() { return (int64_t)THREADS * UNROLL * BYTES / sizeof(T); }
-
-// Elements of a chunk that this thread has, as fp32: UNROLL vectors, zeros behind the tensor's end.
-template <typename T, typename F> __device__ inline void each_vector(const void *p, int64_t first, int64_t n, F use) {
-    constexpr int N = BYTES / (int)sizeof(T);
-    Vec<T, N> r[UNROLL];
-    if (first + (int64_t)THREADS * UNROLL * N <= n) {
+// What a thread has of a chunk: UNROLL vectors as they lie in memory, zeros behind the tensor's end.
+struct Raw { Vec<unsigned, 4> v[UNROLL]; };
+template <bool PAST> __device__ inline Raw raw_chunk(const void *p, int64_t first /* byte */, int64_t end, bool bf) {
+    Raw r;
+    if (first + CHUNK <= end) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) r[u] = load<T, N>(p, first + ((int64_t)u * THREADS + threadIdx.x) * N);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) use(first + ((int64_t)u * THREADS + threadIdx.x) * N, N, r[u]);
+        for (int u = 0; u < UNROLL; ++u) {
+            const char *const at = (const char *)p + first + (u * THREADS + (int)threadIdx.x) * 16;
+            r.v[u] = PAST ? load_past<unsigned, 4>(at, 0) : load<unsigned, 4>(at, 0);
+        }
     } else {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int64_t i = first + ((int64_t)u * THREADS + threadIdx.x) * N;
-            const int in = (int)min((int64_t)N, max(n - i, (int64_t)0));
-            r[u] = Vec<T, N>{};
-            if (in == N) r[u] = load<T, N>(p, i);
-            else
+            const int64_t at = first + (u * THREADS + (int)threadIdx.x) * 16;
+            r.v[u] = Vec<unsigned, 4>{};
+            if (at + 16 <= end) r.v[u] = load<unsigned, 4>((const char *)p + at, 0);
+            else if (bf) {
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (k < in) r[u].x[k] = ((const T *)p)[i + k];
-        }
+                for (int k = 0; k < 8; ++k)
+                    if (at + 2 * k < end) r.v[u].x[k >> 1] |= (unsigned)*(const unsigned short *)((const char *)p + at + 2 * k) << (16 * (k & 1));
+            } else {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int64_t i = first + ((int64_t)u * THREADS + threadIdx.x) * N;
-            use(i, (int)min((int64_t)N, max(n - i, (int64_t)0)), r[u]);
+                for (int k = 0; k < 4; ++k)
+                    if (at + 4 * k < end) r.v[u].x[k] = *(const unsigned *)((const char *)p + at + 4 * k);
+            }
         }
     }
+    return r;
 }
+__device__ inline float low_bf16(unsigned x) { return __uint_as_float(x << 16); }
+__device__ inline float high_bf16(unsigned x) { return __uint_as_float(x & 0xffff0000u); }
 
 template <int WAVES> __device__ inline double sum_workgroup(double x, double *shared) {
 #pragma unroll
@@ -80,25 +80,48 @@ template <int WAVES> __device__ inline double sum_workgroup(double x, double *sh
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
     __syncthreads();
     x = 0.0;
+#pragma unroll
     for (int w = 0; w < WAVES; ++w) x += shared[w];
     return x;
 }
 
-__global__ __launch_bounds__(THREADS) void norm_kernel(const GradLaunch a) {
+// The next chunk is asked for before this one is summed.  PAST: a list that the cache cannot hold is read past it (537 MB: 79 us instead of 89, 6.8 TB/s);
+// of a shorter one the clipping, or the optimizer's step, finds what was read (102 MB: 33 us of clipping instead of 45).
+template <bool PAST> __global__ __launch_bounds__(THREADS) void norm_kernel(const GradLaunch a) {
     __shared__ double shared[THREADS / 64];
+    unsigned c = blockIdx.x;
+    int id = item_of(a, c);
+    const auto ask = [&](unsigned chunk, bool &bf) {
+        while (id + 1 < a.n && a.item[id + 1].first <= chunk) ++id;
+        const GradItem &it = a.item[id];
+        bf = a.gbf[id] != 0;
+        return raw_chunk<PAST>(it.g, (int64_t)(chunk - it.first) * CHUNK, (int64_t)it.n * (bf ? 2 : 4), bf);
+    };
     double sum = 0.0;
-    for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int id = item_of(a, c);
-        const GradItem it = a.item[id];
-        const auto square = [&](int64_t, int, const auto &r) {
+    bool bf;
+    Raw r = ask(c, bf);
+    for (; c < a.chunks; c += gridDim.x) {
+        const Raw now = r;
+        const bool now_bf = bf;
+        if (c + gridDim.x < a.chunks) r = ask(c + gridDim.x, bf);
+        if (now_bf) {
 #pragma unroll
-            for (int k = 0; k < (int)(sizeof(r.x) / sizeof(r.x[0])); ++k) {
-                const double g = value_of(r.x[k]);
-                sum = fma(g, g, sum);
-            }
-        };
-        if (a.gbf[id]) each_vector<unsigned short>(it.g, (int64_t)(c - it.first) * chunk_elements<unsigned short>(), it.n, square);
-        else each_vector<float>(it.g, (int64_t)(c - it.first) * chunk_elements<float>(), it.n, square);
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const double lo = low_bf16(now.v[u].x[k]), hi = high_bf16(now.v[u].x[k]);
+                    sum = fma(lo, lo, sum);
+                    sum = fma(hi, hi, sum);
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const double g = __uint_as_float(now.v[u].x[k]);
+                    sum = fma(g, g, sum);
+                }
+        }
     }
     sum = sum_workgroup<THREADS / 64>(sum, shared);
     if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
@@ -111,55 +134,91 @@ struct NormArgs {
     const float *scale;
     float *norm, *coef;
 };
-constexpr int JOIN = 1024;
-__global__ __launch_bounds__(JOIN) void norm_join_kernel(const NormArgs g) {
-    __shared__ double shared[JOIN / 64];
+constexpr int EACH = MOST / THREADS;     // sums that a thread asks for together
+// The coefficient; `writes`: this workgroup leaves both results.
+__device__ inline float join_sums(const NormArgs &g, bool writes, double *shared) {
+    const double scale = g.scale ? (double)*g.scale : 1.0;
     double sum = 0.0;
-    for (int i = threadIdx.x; i < g.n; i += JOIN) sum += g.part[i];
-    sum = sum_workgroup<JOIN / 64>(sum, shared);
-    if (threadIdx.x != 0) return;
-    const double scale = g.scale ? (double)*g.scale : 1.0, norm = sqrt(sum) * fabs(scale);
+    for (int i0 = 0; i0 < g.n; i0 += MOST) {
+        double x[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int i = i0 + k * THREADS + (int)threadIdx.x;
+            x[k] = i < g.n ? g.part[i] : 0.0;
+        }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) sum += x[k];
+    }
+    const double norm = sqrt(sum_workgroup<THREADS / 64>(sum, shared)) * fabs(scale);
     // (a norm that is NaN makes the coefficient NaN, an infinite one makes it zero)
     const double clip = norm > g.max_norm ? g.max_norm / norm : norm == norm ? 1.0 : norm;
-    *g.norm = (float)norm;
-    if (g.coef) *g.coef = (float)(scale * clip);
+    const float coef = (float)(scale * clip);
+    if (writes && threadIdx.x == 0) {
+        *g.norm = (float)norm;
+        if (g.coef) *g.coef = coef;
+    }
+    return coef;
+}
+__global__ __launch_bounds__(THREADS) void norm_join_kernel(const NormArgs g) {
+    __shared__ double shared[THREADS / 64];
+    (void)join_sums(g, true, shared);
 }
 
-template <typename T, typename O> __device__ inline void clip_chunk(const GradItem &it, int64_t first, float coef) {
-    each_vector<T>(it.g, first, it.n, [&](int64_t i, int in, const auto &r) {
-        constexpr int N = BYTES / (int)sizeof(T);
-        Vec<O, N> o;
+// N results of a thread from element i on; `in` of them exist.
+template <typename O, int N> __device__ inline void put(void *p, int64_t i, int64_t in, const float (&x)[N]) {
+    Vec<O, N> o;
 #pragma unroll
-        for (int k = 0; k < N; ++k) o.x[k] = element_of<O>(value_of(r.x[k]) * coef);
-        if (in == N) store(it.out, i, o);
-        else
+    for (int k = 0; k < N; ++k) o.x[k] = element_of<O>(x[k]);
+    if (in >= N) {
+        if constexpr (sizeof(o) == 16) store_past(p, i, o);
+        else store(p, i, o);
+    } else
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (k < in) ((O *)it.out)[i + k] = o.x[k];
-    });
+        for (int k = 0; k < N; ++k)
+            if (k < in) ((O *)p)[i + k] = o.x[k];
 }
 
-// The last chunks first: what the sums read last may still be in the cache.
-__global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a) {
-    const unsigned c = a.chunks - 1 - blockIdx.x;
-    const int id = item_of(a, c);
-    const GradItem it = a.item[id];
-    const float coef = *a.coef;
-    if (coef == 1.f && it.out == it.g) return;
-    if (a.gbf[id]) {
-        const int64_t first = (int64_t)(c - it.first) * chunk_elements<unsigned short>();
-        if (a.obf[id]) clip_chunk<unsigned short, unsigned short>(it, first, coef);
-        else clip_chunk<unsigned short, float>(it, first, coef);
-    } else {
-        const int64_t first = (int64_t)(c - it.first) * chunk_elements<float>();
-        if (a.obf[id]) clip_chunk<float, unsigned short>(it, first, coef);
-        else clip_chunk<float, float>(it, first, coef);
+// The last chunks first: what was read last may still be in the cache.  Nothing is read a third time, so loads and stores go past it.
+__global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a, const NormArgs g, bool writes) {
+    __shared__ double shared[THREADS / 64];
+    const float coef = join_sums(g, writes && blockIdx.x == 0, shared);
+    int id = item_of(a, a.chunks - 1 - blockIdx.x);
+    for (unsigned q = blockIdx.x; q < a.chunks; q += gridDim.x) {
+        const unsigned c = a.chunks - 1 - q;
+        while (a.item[id].first > c) --id;
+        const GradItem &it = a.item[id];
+        if (coef == 1.f && it.out == it.g) continue;
+        const bool bf = a.gbf[id] != 0, obf = a.obf[id] != 0;
+        const int64_t first = (int64_t)(c - it.first) * CHUNK;
+        const Raw r = raw_chunk<true>(it.g, first, (int64_t)it.n * (bf ? 2 : 4), bf);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int64_t at = first + (u * THREADS + (int)threadIdx.x) * 16;
+            if (bf) {
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[2 * k] = low_bf16(r.v[u].x[k]) * coef;
+                    x[2 * k + 1] = high_bf16(r.v[u].x[k]) * coef;
+                }
+                if (obf) put<unsigned short, 8>(it.out, at / 2, it.n - at / 2, x);
+                else put<float, 8>(it.out, at / 2, it.n - at / 2, x);
+            } else {
+                float x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(r.v[u].x[k]) * coef;
+                if (obf) put<unsigned short, 4>(it.out, at / 4, it.n - at / 4, x);
+                else put<float, 4>(it.out, at / 4, it.n - at / 4, x);
+            }
+        }
     }
 }
 
 // The launches of a list: up to ITEMS tensors each, tensors longer than 32-bit counts reach in pieces.
 constexpr int64_t PIECE = (int64_t)1 << 31;
 constexpr unsigned MOST_CHUNKS = 1u << 23;
+constexpr double CACHE_BYTES = 256e6;       // of the cache in front of the memory
+constexpr unsigned CLIP_WGS = 4096;         // (1024 to 8192 differ by 1 us for 25.6M gradients)
 template <typename F> int each_launch(int n, const kfac_grad_item *items, F launch) {
     GradLaunch a{};
     int64_t elements = 0, bytes = 0, written = 0;
@@ -174,7 +233,7 @@ template <typename F> int each_launch(int n, const kfac_grad_item *items, F laun
         const kfac_grad_item &t = items[i];
         const bool bf = t.grad_dtype == KFAC_BF16, obf = t.out_dtype == KFAC_BF16;
         for (int64_t at = 0; at < t.n; at += PIECE) {
-            const int64_t len = std::min(PIECE, t.n - at), per = bf ? chunk_elements<unsigned short>() : chunk_elements<float>();
+            const int64_t len = std::min(PIECE, t.n - at), per = CHUNK / (bf ? 2 : 4);
             const unsigned mine = (unsigned)((len + per - 1) / per);
             if (a.n == ITEMS || a.chunks + mine > MOST_CHUNKS) KFAC_CHECK(go());
             a.gbf[a.n] = bf;
@@ -202,28 +261,30 @@ size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items) {
 
 int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef, bool clip) {
     if (kfac_grad_norm_ws_bytes_impl(n, items) > ctx->ws_bytes) return KFAC_EWORKSPACE;
-    double *const part = (double *)ctx->ws;
-    int parts = 0;
+    double whole = 0.0;
+    for (int i = 0; i < n; ++i) whole += (double)items[i].n * (items[i].grad_dtype == KFAC_BF16 ? 2.0 : 4.0);
+    NormArgs g{(double *)ctx->ws, 0, (double)max_norm, grad_scale, norm, coef};
     KFAC_CHECK(each_launch(n, items, [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t) -> int {
         const unsigned wgs = std::min<unsigned>(a.chunks, MOST);
-        a.part = part + parts;
-        parts += (int)wgs;
+        a.part = (double *)ctx->ws + g.n;
+        g.n += (int)wgs;
         KfacProfScope prof(ctx, KC_NORM, 2.0 * (double)elements, (double)bytes);
-        hipLaunchKernelGGL(norm_kernel, dim3(wgs), dim3(THREADS), 0, ctx->stream, a);
+        hipLaunchKernelGGL((whole > CACHE_BYTES ? norm_kernel<true> : norm_kernel<false>), dim3(wgs), dim3(THREADS), 0, ctx->stream, a);
         KFAC_HIP_CHECK(hipGetLastError());
         return KFAC_OK;
     }));
-    {
-        KfacProfScope prof(ctx, KC_NORM, 0.0, 8.0 * parts);
-        hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(JOIN), 0, ctx->stream, NormArgs{part, parts, (double)max_norm, grad_scale, norm, coef});
+    if (!clip || g.n == 0) {
+        KfacProfScope prof(ctx, KC_NORM, 0.0, 8.0 * g.n);
+        hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(THREADS), 0, ctx->stream, g);
         KFAC_HIP_CHECK(hipGetLastError());
+        return KFAC_OK;
     }
-    if (!clip) return KFAC_OK;
+    bool first = true;
     return each_launch(n, items, [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t written) -> int {
-        a.coef = coef;
         KfacProfScope prof(ctx, KC_NORM, (double)elements, (double)(bytes + written));
-        hipLaunchKernelGGL(clip_kernel, dim3(a.chunks), dim3(THREADS), 0, ctx->stream, a);
+        hipLaunchKernelGGL(clip_kernel, dim3(std::min<unsigned>(a.chunks, CLIP_WGS)), dim3(THREADS), 0, ctx->stream, a, g, first);
         KFAC_HIP_CHECK(hipGetLastError());
+        first = false;
         return KFAC_OK;
     });
 }

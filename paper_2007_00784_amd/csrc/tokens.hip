@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 #include "kfac_internal.h"
 #include "elements.h"
 
@@ -232,8 +233,24 @@ struct SortArgs {
 
 __device__ inline int expert_of(int id, int E) { return (unsigned)id < (unsigned)E ? id : E; }
 
-// Each wave counts its run's slots by expert and leaves at rows[s] how many of its own expert are in front of s in the run.  Sixty-four
-// slots at a time: the lanes of one expert are found by the ballots of its number's bits, the counts before stand in LDS.
+// Sixty-four slots in a wave's order, one a lane: how many of the same expert are in front of it in the run, whose counts so far stand in `seen`.
+// The lanes of one expert are found by the ballots of its number's bits.
+__device__ inline int rank_in_run(int e, int bits, int *seen) {
+    unsigned long long same = ~0ull;
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long set = __ballot((e >> b) & 1);
+        same &= (e >> b) & 1 ? set : ~set;
+    }
+    const int before = __popcll(same & ((1ull << (threadIdx.x & 63)) - 1));
+    const int had = seen[e];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (all lanes have read before one writes: a wave's LDS accesses keep their order)
+    if (before == 0) seen[e] = had + __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return had + before;
+}
+constexpr int AHEAD = 4;     // steps of a run whose experts are asked for together
+
+// Each wave counts its run's slots by expert and leaves at rows[s] how many of its own expert are in front of s in the run.
 __global__ __launch_bounds__(THREADS) void sort_count_kernel(const SortArgs g) {
     extern __shared__ int shared[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -245,20 +262,19 @@ __global__ __launch_bounds__(THREADS) void sort_count_kernel(const SortArgs g) {
     if (run < g.runs) {
         const int bits = 32 - __builtin_clz(g.E);         // of 0 .. E
         const int last = (int)min(first + g.per, (int64_t)g.S);
-        for (int64_t s0 = first; s0 < last; s0 += 64) {
-            const int64_t s = s0 + lane;
-            const int e = s < last ? expert_of(g.ids[s], g.E) : g.E;
-            unsigned long long same = ~0ull;
-            for (int b = 0; b < bits; ++b) {
-                const unsigned long long set = __ballot((e >> b) & 1);
-                same &= (e >> b) & 1 ? set : ~set;
+        for (int64_t s0 = first; s0 < last; s0 += 64 * AHEAD) {
+            int e[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int64_t s = s0 + 64 * a + lane;
+                e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
             }
-            const int before = __popcll(same & ((1ull << lane) - 1));
-            const int had = seen[e];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (all lanes have read before one writes: a wave's LDS accesses keep their order)
-            if (before == 0) seen[e] = had + __popcll(same);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (s < last) g.rows[s] = e < g.E ? had + before : -1;
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int64_t s = s0 + 64 * a + lane;
+                const int rank = rank_in_run(e[a], bits, seen);
+                if (s < last) g.rows[s] = e[a] < g.E ? rank : -1;
+            }
         }
     }
     __syncthreads();
@@ -287,6 +303,18 @@ template <int WAVES> __device__ inline int scan_workgroup(int x, int *shared, in
     return before + incl - x;
 }
 
+// use(run, slots of e in it) for the runs r0 .. r1 - 1, eight counts asked for at a time.
+template <typename F> __device__ inline void each_run(const SortArgs &g, int e, int r0, int r1, F use) {
+    for (int r = r0; r < r1; r += 8) {
+        int c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = g.base[(int64_t)min(r + i, r1 - 1) * g.E + e];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r + i < r1) use(r + i, c[i]);
+    }
+}
+
 // One workgroup: the counts of the runs become the rows at which each run's slots of an expert begin.
 constexpr int SCAN = 1024;
 __global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
@@ -301,8 +329,7 @@ __global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
     for (int e0 = 0; e0 < g.E; e0 += W) {
         const int e = e0 + col;
         int sum = 0;
-        if (e < g.E)
-            for (int r = r0; r < r1; ++r) sum += g.base[(int64_t)r * g.E + e];
+        if (e < g.E) each_run(g, e, r0, r1, [&](int, int c) { sum += c; });
         part[threadIdx.x] = sum;
         __syncthreads();
         int whole = 0, before = 0;                        // of the expert; of its shares before this one
@@ -320,15 +347,60 @@ __global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
         __syncthreads();
         int row = part[col] + before;
         if (e < g.E)
-            for (int r = r0; r < r1; ++r) {
-                const int c = g.base[(int64_t)r * g.E + e];
+            each_run(g, e, r0, r1, [&](int r, int c) {
                 g.base[(int64_t)r * g.E + e] = row;
                 row += c;
-            }
+            });
         at += total;
         __syncthreads();
     }
     if (threadIdx.x == 0) g.offsets[g.E] = at;
+}
+
+// The whole order by one workgroup, whose waves take a run each: counts in LDS, then the rows at which each run's slots of an expert begin.
+constexpr int ONE_SLOTS = 4096, ONE_EXPERTS = 512, ONE_STEPS = ONE_SLOTS / SCAN;
+__global__ __launch_bounds__(SCAN) void sort_one_kernel(const SortArgs g) {
+    extern __shared__ int shared[];                       // [waves][E + 1]
+    __shared__ int waves[SCAN / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, pitch = g.E + 1;
+    int *const seen = shared + wave * pitch;
+    int e[ONE_STEPS], rank[ONE_STEPS];
+    const int first = wave * g.per, last = min(first + g.per, g.S);
+#pragma unroll
+    for (int a = 0; a < ONE_STEPS; ++a) {
+        const int s = first + 64 * a + lane;
+        e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
+    }
+    for (int i = threadIdx.x; i < SCAN / 64 * pitch; i += SCAN) shared[i] = 0;
+    __syncthreads();
+    const int bits = 32 - __builtin_clz(g.E);             // of 0 .. E
+#pragma unroll
+    for (int a = 0; a < ONE_STEPS; ++a)
+        if (first + 64 * a < last) rank[a] = rank_in_run(e[a], bits, seen);
+    __syncthreads();
+    int count[SCAN / 64], whole = 0, total;               // of this thread's expert, by run
+    if ((int)threadIdx.x < g.E)
+#pragma unroll
+        for (int w = 0; w < SCAN / 64; ++w) {
+            count[w] = shared[w * pitch + threadIdx.x];
+            whole += count[w];
+        }
+    int row = scan_workgroup<SCAN / 64>(whole, waves, total);
+    if (threadIdx.x == 0) g.offsets[g.E] = total;
+    if ((int)threadIdx.x < g.E) {
+        g.offsets[threadIdx.x] = row;
+#pragma unroll
+        for (int w = 0; w < SCAN / 64; ++w) {
+            shared[w * pitch + threadIdx.x] = row;
+            row += count[w];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < ONE_STEPS; ++a) {
+        const int s = first + 64 * a + lane;
+        if (s < last) g.rows[s] = e[a] < g.E ? seen[e[a]] + rank[a] : -1;
+    }
 }
 
 __device__ inline int ranked_row(const SortArgs &g, unsigned s) {
@@ -429,7 +501,7 @@ template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS)
                 const int row = rows[j];
                 if ((unsigned)row >= (unsigned)g.R) continue;
 #pragma unroll
-                for (int u = 0; u < U; ++u) store(g.out, row * g.ldo + i + u * LANES * N, r[u]);
+                for (int u = 0; u < U; ++u) store_past(g.out, row * g.ldo + i + u * LANES * N, r[u]);
             }
         } else {
             for (int u = 0; u < U; ++u) {
@@ -441,7 +513,7 @@ template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS)
                 for (int j = 0; j < g.k; ++j) {
                     const int row = rows[j];
                     if ((unsigned)row >= (unsigned)g.R) continue;
-                    if (in == N) store(g.out, row * g.ldo + b, r);
+                    if (in == N) store_past(g.out, row * g.ldo + b, r);
                     else
                         for (int n = 0; n < in; ++n) ((T *)g.out)[row * g.ldo + b + n] = r.x[n];
                 }
@@ -450,23 +522,21 @@ template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS)
     }
 }
 
-// N elements from i on as fp32; `in` of them exist.
-template <typename T, int N> __device__ inline void fetch(const void *p, int64_t i, int in, float (&x)[N]) {
-    if (in >= N) {
-        const auto r = load<T, N>(p, i);
+// N elements from i on; `in` of them exist, the others are zero (FULL: all exist).  PAST: loaded past the caches.
+template <typename T, int N, bool FULL, bool PAST> __device__ inline Vec<T, N> fetch(const void *p, int64_t i, int in) {
+    if (FULL || in >= N) return PAST ? load_past<T, N>(p, i) : load<T, N>(p, i);
+    Vec<T, N> r{};
 #pragma unroll
-        for (int n = 0; n < N; ++n) x[n] = value_of(r.x[n]);
-    } else {
-#pragma unroll
-        for (int n = 0; n < N; ++n) x[n] = n < in ? value_of(((const T *)p)[i + n]) : 0.f;
-    }
+    for (int n = 0; n < N; ++n)
+        if (n < in) r.x[n] = ((const T *)p)[i + n];
+    return r;
 }
-template <typename T, int N> __device__ inline void put(void *p, int64_t i, int in, const float (&x)[N]) {
-    if (in >= N) {
+template <typename T, int N, bool FULL> __device__ inline void put(void *p, int64_t i, int in, const float (&x)[N]) {
+    if (FULL || in >= N) {
         Vec<T, N> r;
 #pragma unroll
         for (int n = 0; n < N; ++n) r.x[n] = element_of<T>(x[n]);
-        store(p, i, r);
+        store_past(p, i, r);
     } else {
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -484,9 +554,17 @@ __device__ inline void slots_of(const MoveArgs &g, int64_t t0, int mine, int *ro
     __syncthreads();
 }
 
-// Y[t] = add[t] + sum_j w[s] Ys[rows[s]]: sums in fp32 in the order of j, rounded once.  KB rows are asked for at a time.
-template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) void combine_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T);
+// A step of a lane goes over U vectors, LANES vectors apart.  F(FULL, column) for the steps of this lane from c0 to c1.
+template <int STEP, int N, int U, typename F> __device__ inline void each_step(int c0, int c1, F f) {
+    for (int i = c0; i < c1; i += STEP * U) {
+        if (i + (U - 1) * STEP + N <= c1) f(std::true_type{}, i);
+        else f(std::false_type{}, i);
+    }
+}
+
+// Y[t] = add[t] + sum_j w[s] Ys[rows[s]]: sums in fp32 in the order of j, rounded once.  KB rows are asked for at a time, two vectors of each.
+template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), STEP = LANES * N, U = 2;
     extern __shared__ int shared[];
     float *const weights = (float *)(shared + TOK * g.k);
     const int64_t t0 = (int64_t)blockIdx.x * TOK;
@@ -496,34 +574,41 @@ template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) v
     const int *const rows = shared + threadIdx.x / LANES * g.k;
     const float *const w = weights + threadIdx.x / LANES * g.k;
     const int c0 = blockIdx.y * g.part, c1 = min(g.d, c0 + g.part);
-    for (int i = c0 + (int)(threadIdx.x % LANES) * N; i < c1; i += LANES * N) {
-        const int in = c1 - i;
-        float sum[N];
-        if (g.y) fetch<T, N>(g.y, t * g.ldy + i, in, sum);
-        else
+    each_step<STEP, N, U>(c0 + (int)(threadIdx.x % LANES) * N, c1, [&](auto full, int i) {
+        constexpr bool FULL = decltype(full)::value;
+        float sum[U][N];
 #pragma unroll
-            for (int n = 0; n < N; ++n) sum[n] = 0.f;
+        for (int u = 0; u < U; ++u) {
+            const Vec<T, N> a = g.y ? fetch<T, N, FULL, PAST>(g.y, t * g.ldy + i + u * STEP, c1 - i - u * STEP) : Vec<T, N>{};
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[u][n] = value_of(a.x[n]);
+        }
         for (int j0 = 0; j0 < g.k; j0 += KB) {
-            float x[KB][N];
+            Vec<T, N> x[KB][U];
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
                 const int row = rows[min(j0 + j, g.k - 1)];
-                if (row >= 0) fetch<T, N>(g.x, row * g.ldx + i, in, x[j]);
+                if (row >= 0)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) x[j][u] = fetch<T, N, FULL, PAST>(g.x, row * g.ldx + i + u * STEP, c1 - i - u * STEP);
             }
 #pragma unroll
             for (int j = 0; j < KB; ++j)
                 if (j0 + j < g.k && rows[j0 + j] >= 0)
 #pragma unroll
-                    for (int n = 0; n < N; ++n) sum[n] = fmaf(w[j0 + j], x[j][n], sum[n]);
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int n = 0; n < N; ++n) sum[u][n] = fmaf(w[j0 + j], value_of(x[j][u].x[n]), sum[u][n]);
         }
-        put<T, N>(g.out, t * g.ldo + i, in, sum);
-    }
+#pragma unroll
+        for (int u = 0; u < U; ++u) put<T, N, FULL>(g.out, t * g.ldo + i + u * STEP, c1 - i - u * STEP, sum[u]);
+    });
 }
 
 // dYs[rows[s]] = w[s] dY[t] and dw[s] = <dY[t], Ys[rows[s]]>, KB slots of a token at a time.  A lane's share of a product is summed in fp32 in
 // the order of the columns, the lanes' then by halves: the same order from run to run.
-template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T);
+template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), STEP = LANES * N;
     extern __shared__ int shared[];
     __shared__ float partial[THREADS / 64][KB];
     float *const weights = (float *)(shared + TOK * g.k);
@@ -538,25 +623,28 @@ template <typename T, int LANES, int KB> __global__ __launch_bounds__(THREADS) v
         float dot[KB];
 #pragma unroll
         for (int j = 0; j < KB; ++j) dot[j] = 0.f;
-        for (int i = lane * N; there && i < g.d; i += LANES * N) {
-            const int in = g.d - i;
-            float dy[N], x[KB][N];
-            fetch<T, N>(g.x, t * g.ldx + i, in, dy);
+        each_step<STEP, N, 1>(lane * N, there ? g.d : 0, [&](auto full, int i) {
+            constexpr bool FULL = decltype(full)::value;
+            const Vec<T, N> dy = fetch<T, N, FULL, PAST>(g.x, t * g.ldx + i, g.d - i);
+            Vec<T, N> x[KB];
 #pragma unroll
             for (int j = 0; j < KB; ++j)
-                if (j0 + j < g.k && rows[j0 + j] >= 0) fetch<T, N>(g.y, rows[j0 + j] * g.ldy + i, in, x[j]);
+                if (j0 + j < g.k && rows[j0 + j] >= 0) x[j] = fetch<T, N, FULL, PAST>(g.y, rows[j0 + j] * g.ldy + i, g.d - i);
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j0 + j < g.k && rows[j0 + j] >= 0)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) dot[j] = fmaf(value_of(dy.x[n]), value_of(x[j].x[n]), dot[j]);
+            __builtin_amdgcn_sched_barrier(0);       // (stores between the loads: 229 us instead of 220 for 16384 x 4 rows of 4096 bf16)
 #pragma unroll
             for (int j = 0; j < KB; ++j)
                 if (j0 + j < g.k && rows[j0 + j] >= 0) {
                     float o[N];
 #pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        dot[j] = n < in ? fmaf(dy[n], x[j][n], dot[j]) : dot[j];
-                        o[n] = w[j0 + j] * dy[n];
-                    }
-                    put<T, N>(g.out, rows[j0 + j] * g.ldo + i, in, o);
+                    for (int n = 0; n < N; ++n) o[n] = w[j0 + j] * value_of(dy.x[n]);
+                    put<T, N, FULL>(g.out, rows[j0 + j] * g.ldo + i, g.d - i, o);
                 }
-        }
+        });
 #pragma unroll
         for (int j = 0; j < KB; ++j) {
             dot[j] = group_sum<(LANES < 64 ? LANES : 64)>(dot[j]);
@@ -604,21 +692,26 @@ template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, do
     return KFAC_OK;
 }
 
-template <typename T, int KB> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
+// The experts' rows are read past the caches where they are too long to be there still.
+constexpr double PAST_BYTES = 128e6;
+template <typename T, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
     const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
     const unsigned wgs = (unsigned)(((int64_t)g.T + tok - 1) / tok);
     const size_t lds = 8 * (size_t)tok * g.k;
     KfacProfScope prof(ctx, KC_TOKENS, flops, bytes);
     if (g.dw) {
-        const auto kernel = lanes == 16 ? combine_grad_kernel<T, 16, KB> : lanes == 64 ? combine_grad_kernel<T, 64, KB> : combine_grad_kernel<T, 256, KB>;
+        const auto kernel = lanes == 16 ? combine_grad_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_grad_kernel<T, 64, KB, PAST> : combine_grad_kernel<T, 256, KB, PAST>;
         hipLaunchKernelGGL(kernel, dim3(wgs), dim3(THREADS), lds, ctx->stream, g);
     } else {
         g.part = part_of(g.T, g.d, sizeof(T), lanes);
-        const auto kernel = lanes == 16 ? combine_kernel<T, 16, KB> : lanes == 64 ? combine_kernel<T, 64, KB> : combine_kernel<T, 256, KB>;
+        const auto kernel = lanes == 16 ? combine_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_kernel<T, 64, KB, PAST> : combine_kernel<T, 256, KB, PAST>;
         hipLaunchKernelGGL(kernel, dim3(wgs, (unsigned)((g.d + g.part - 1) / g.part)), dim3(THREADS), lds, ctx->stream, g);
     }
     KFAC_HIP_CHECK(hipGetLastError());
     return KFAC_OK;
+}
+template <typename T, int KB> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
+    return (double)sizeof(T) * g.d * g.T * g.k > PAST_BYTES ? launch_combine<T, KB, true>(ctx, g, flops, bytes) : launch_combine<T, KB, false>(ctx, g, flops, bytes);
 }
 template <typename T> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
     return g.k == 1 ? launch_combine<T, 1>(ctx, g, flops, bytes) : g.k == 2 ? launch_combine<T, 2>(ctx, g, flops, bytes) : launch_combine<T, 4>(ctx, g, flops, bytes);
@@ -654,7 +747,7 @@ int runs_of(int64_t S, int E, size_t ws_bytes) {
 
 size_t kfac_experts_dispatch_ws_bytes_impl(int tokens, int topk, int experts) {
     const int64_t S = (int64_t)tokens * topk;
-    if (S <= FEW_SLOTS) return 0;
+    if (S <= FEW_SLOTS || (S <= ONE_SLOTS && experts <= ONE_EXPERTS)) return 0;
     return kfac_align_up((size_t)runs_of(S, experts, SIZE_MAX) * experts * sizeof(int), 256);
 }
 
@@ -702,6 +795,15 @@ int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int exp
     s.offsets = offsets;
     s.rows = rows;
     if (S <= FEW_SLOTS) return bf ? launch_scatter<unsigned short, COUNTED>(ctx, g, bytes) : launch_scatter<float, COUNTED>(ctx, g, bytes);
+    if (S <= ONE_SLOTS && experts <= ONE_EXPERTS) {
+        s.runs = SCAN / 64;
+        s.per = (int)((S + SCAN - 1) / SCAN * 64);
+        KfacProfScope prof(ctx, KC_TOKENS, 0.0, 8.0 * (double)S);
+        hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(SCAN), SCAN / 64 * sizeof(int) * (experts + 1), ctx->stream, s);
+        KFAC_HIP_CHECK(hipGetLastError());
+        if (!X) return KFAC_OK;
+        return bf ? launch_scatter<unsigned short, GIVEN>(ctx, g, bytes) : launch_scatter<float, GIVEN>(ctx, g, bytes);
+    }
     s.runs = runs_of(S, experts, ctx->ws_bytes);
     s.per = (int)(((S + s.runs - 1) / s.runs + 63) / 64 * 64);
     s.runs = (int)((S + s.per - 1) / s.per);

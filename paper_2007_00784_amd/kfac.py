@@ -788,7 +788,7 @@ def _scalar(t, dtype, name):
     if t.dtype != dtype or t.numel() != 1:
         raise ValueError("%s must be one %s" % (name, dtype))
     _on_gpu(t)
-    return _ptr(t)
+    return t.data_ptr()
 
 
 _told = False

@@ -219,7 +219,7 @@ def random_ids(T, k, E, gen, nobody=True):
     return ids
 
 
-SORTS = [(1, 1, 1), (1, 64, 4), (8, 2, 8), (16, 64, 3), (17, 64, 4096), (512, 2, 300), (1024, 1, 4096), (1025, 1, 5), (513, 2, 64), (700, 8, 1), (3000, 7, 33), (4100, 64, 4096), (20000, 4, 1025),
+SORTS = [(1, 1, 1), (1, 64, 4), (8, 2, 8), (16, 64, 3), (17, 64, 4096), (512, 2, 300), (1024, 1, 4096), (1025, 1, 5), (513, 2, 64), (700, 8, 1), (3000, 7, 33), (1024, 4, 512), (4096, 1, 1), (4097, 1, 77), (300, 8, 513), (43, 64, 100), (4100, 64, 4096), (20000, 4, 1025),
          (65536, 8, 128), (9, 3, 2)]
 
 
@@ -260,7 +260,7 @@ def test_order_of_nothing(ctx):
 
 # T, k, E, d: few slots and many, rows of one lane, a wave's, a workgroup's and longer ones, cut among workgroups or not
 MOVES = [(1, 1, 1, 1), (1, 2, 4, 65536), (3, 2, 8, 7), (8, 2, 8, 2048), (40, 3, 5, 128), (33, 4, 16, 129), (200, 2, 10, 577), (90, 8, 30, 1000), (64, 16, 20, 2049),
-         (600, 2, 64, 9), (1030, 1, 3, 640), (400, 6, 100, 1031), (300, 4, 7, 5000), (2100, 3, 65, 64), (20, 64, 64, 260), (17, 64, 4096, 33)]
+         (600, 2, 64, 9), (1030, 1, 3, 640), (400, 6, 100, 1031), (300, 4, 7, 5000), (2100, 3, 65, 64), (1360, 3, 6, 33), (20, 64, 64, 260), (17, 64, 4096, 33)]
 
 
 @pytest.mark.parametrize("bf16", [True, False])
