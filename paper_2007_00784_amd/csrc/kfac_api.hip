@@ -519,7 +519,7 @@ size_t kfac_grad_norm_workspace_bytes(int n, const kfac_grad_item *items) {
 }
 
 int kfac_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef) {
-    if (!ctx || !valid_grads(n, items, true, false) || !(max_norm > 0.f) || !norm || norm == coef || norm == grad_scale) return KFAC_EINVAL;
+    if (!ctx || !valid_grads(n, items, true, false) || !(max_norm > 0.f) || !norm || norm == coef || norm == grad_scale || (coef && coef == grad_scale)) return KFAC_EINVAL;
     if (!aligned4(norm) || !aligned4(coef) || !aligned4(grad_scale)) return KFAC_EINVAL;
     const KfacDeviceScope dev(ctx->device);
     if (!dev.ok) return KFAC_EHIP;

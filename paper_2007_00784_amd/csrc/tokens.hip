@@ -21,6 +21,16 @@ using namespace kfac;
 namespace {
 
 constexpr int THREADS = 256;
+constexpr unsigned MOST_WGS = 1u << 23;      // of a launch, which has fewer than 2^32 threads: longer batches go in several
+
+// launch(first token, workgroups) for all tokens, `tok` to a workgroup.
+template <typename F> int each_launch(int64_t T, int tok, F launch) {
+    for (int64_t first = 0; first < T; first += (int64_t)MOST_WGS * tok) {
+        launch((int)first, (unsigned)std::min<int64_t>(MOST_WGS, (T - first + tok - 1) / tok));
+        KFAC_HIP_CHECK(hipGetLastError());
+    }
+    return KFAC_OK;
+}
 
 // ---------------------------------------------------------------- the router's choice
 // A group of L lanes takes a token, each lane V logits, so what has to cross lanes is one value a choice.  A lane's logits lie in vectors of N (16 bytes) that
@@ -514,6 +524,7 @@ __global__ __launch_bounds__(THREADS) void sort_rows_kernel(const SortArgs g) {
 // ---------------------------------------------------------------- rows of tokens to rows of experts
 struct MoveArgs {
     int T, k, R, d;          // tokens, slots of a token, rows of the experts' matrices, width
+    int first;               // the launch's first token
     const int *rows;         // [T][k]
     const float *w;          // [T][k] or NULL
     const void *x;           // the tokens' matrix, or the experts' (combine)
@@ -555,7 +566,7 @@ template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS)
     constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), U = 2;
     extern __shared__ int shared[];                       // rows of the workgroup's slots [TOK k]; COUNTED: experts of all slots [S], counts [E]
     __shared__ int waves[THREADS / 64];
-    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
     const int mine = (int)min((int64_t)TOK, max((int64_t)g.T - t0, (int64_t)0)) * g.k;
     if (MODE == COUNTED) {
         int *const expert = shared + TOK * g.k;
@@ -666,7 +677,7 @@ template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__
     constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), STEP = LANES * N, U = 2;
     extern __shared__ int shared[];
     float *const weights = (float *)(shared + TOK * g.k);
-    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
     slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
     const int64_t t = t0 + threadIdx.x / LANES;
     if (t >= g.T) return;
@@ -711,7 +722,7 @@ template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__
     extern __shared__ int shared[];
     __shared__ float partial[THREADS / 64][KB];
     float *const weights = (float *)(shared + TOK * g.k);
-    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
     slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
     const int64_t t = t0 + threadIdx.x / LANES;
     const bool there = t < g.T;
@@ -782,32 +793,34 @@ template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, do
     const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
     g.part = MODE == RANKED ? (1 << 30) : part_of(g.T, g.d, sizeof(T), lanes);   // (a second workgroup of a slot would find its rank replaced)
     const unsigned parts = MODE == RANKED ? 1 : std::max(1, (g.d + g.part - 1) / g.part);     // (no columns: the order of the slots alone)
-    const dim3 grid((unsigned)(((int64_t)g.T + tok - 1) / tok + (MODE == COUNTED ? 1 : 0)), parts);
     const size_t lds = 4 * ((size_t)tok * g.k + (MODE == COUNTED ? g.sort.S + g.sort.E : 0));
     KfacProfScope prof(ctx, KC_TOKENS, 0.0, bytes);
     const auto kernel = lanes == 16 ? scatter_kernel<T, 16, MODE> : lanes == 64 ? scatter_kernel<T, 64, MODE> : scatter_kernel<T, 256, MODE>;
-    hipLaunchKernelGGL(kernel, grid, dim3(THREADS), lds, ctx->stream, g);
-    KFAC_HIP_CHECK(hipGetLastError());
-    return KFAC_OK;
+    if (MODE == COUNTED) {                                // (one workgroup more, for the offsets)
+        hipLaunchKernelGGL(kernel, dim3((g.T + tok - 1) / tok + 1, parts), dim3(THREADS), lds, ctx->stream, g);
+        KFAC_HIP_CHECK(hipGetLastError());
+        return KFAC_OK;
+    }
+    return each_launch(g.T, tok, [&](int first, unsigned wgs) {
+        g.first = first;
+        hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(THREADS), lds, ctx->stream, g);
+    });
 }
 
 // The experts' rows are read past the caches where they are too long to be there still.
 constexpr double PAST_BYTES = 128e6;
 template <typename T, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
     const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
-    const unsigned wgs = (unsigned)(((int64_t)g.T + tok - 1) / tok);
     const size_t lds = 8 * (size_t)tok * g.k;
+    g.part = g.dw ? g.d : part_of(g.T, g.d, sizeof(T), lanes);
+    const unsigned parts = (g.d + g.part - 1) / g.part;
+    const auto kernel = g.dw ? (lanes == 16 ? combine_grad_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_grad_kernel<T, 64, KB, PAST> : combine_grad_kernel<T, 256, KB, PAST>)
+                             : (lanes == 16 ? combine_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_kernel<T, 64, KB, PAST> : combine_kernel<T, 256, KB, PAST>);
     KfacProfScope prof(ctx, KC_TOKENS, flops, bytes);
-    if (g.dw) {
-        const auto kernel = lanes == 16 ? combine_grad_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_grad_kernel<T, 64, KB, PAST> : combine_grad_kernel<T, 256, KB, PAST>;
-        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(THREADS), lds, ctx->stream, g);
-    } else {
-        g.part = part_of(g.T, g.d, sizeof(T), lanes);
-        const auto kernel = lanes == 16 ? combine_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_kernel<T, 64, KB, PAST> : combine_kernel<T, 256, KB, PAST>;
-        hipLaunchKernelGGL(kernel, dim3(wgs, (unsigned)((g.d + g.part - 1) / g.part)), dim3(THREADS), lds, ctx->stream, g);
-    }
-    KFAC_HIP_CHECK(hipGetLastError());
-    return KFAC_OK;
+    return each_launch(g.T, tok, [&](int first, unsigned wgs) {
+        g.first = first;
+        hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(THREADS), lds, ctx->stream, g);
+    });
 }
 template <typename T, int KB> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
     return (double)sizeof(T) * g.d * g.T * g.k > PAST_BYTES ? launch_combine<T, KB, true>(ctx, g, flops, bytes) : launch_combine<T, KB, false>(ctx, g, flops, bytes);
@@ -816,25 +829,39 @@ template <typename T> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, doubl
     return g.k == 1 ? launch_combine<T, 1>(ctx, g, flops, bytes) : g.k == 2 ? launch_combine<T, 2>(ctx, g, flops, bytes) : launch_combine<T, 4>(ctx, g, flops, bytes);
 }
 
-template <typename T, int L, int V> void launch_route(kfac_ctx *ctx, const RouteArgs &g) {
-    hipLaunchKernelGGL((g.k <= L ? route_kernel<T, L, V, true> : route_kernel<T, L, V, false>), dim3((g.T + THREADS / L - 1) / (THREADS / L)), dim3(THREADS), 0, ctx->stream, g);
+template <typename T, int L, int V> int launch_route(kfac_ctx *ctx, const RouteArgs &all) {
+    return each_launch(all.T, THREADS / L, [&](int first, unsigned wgs) {
+        RouteArgs g = all;
+        g.logits = (const T *)g.logits + first * g.ldl;
+        g.T -= first;
+        g.ids += (int64_t)first * g.k;
+        g.weights += (int64_t)first * g.k;
+        hipLaunchKernelGGL((g.k <= L ? route_kernel<T, L, V, true> : route_kernel<T, L, V, false>), dim3(wgs), dim3(THREADS), 0, ctx->stream, g);
+    });
 }
-template <typename T, int L, int V> void launch_route(kfac_ctx *ctx, const RouteGradArgs &g) {
-    hipLaunchKernelGGL((g.k <= L ? route_grad_kernel<T, L, V, true> : route_grad_kernel<T, L, V, false>), dim3((g.T + THREADS / L - 1) / (THREADS / L)), dim3(THREADS), 0, ctx->stream, g);
+template <typename T, int L, int V> int launch_route(kfac_ctx *ctx, const RouteGradArgs &all) {
+    return each_launch(all.T, THREADS / L, [&](int first, unsigned wgs) {
+        RouteGradArgs g = all;
+        g.logits = (const T *)g.logits + first * g.ldl;
+        g.T -= first;
+        g.ids += (int64_t)first * g.k;
+        g.dw += (int64_t)first * g.k;
+        g.out = (T *)g.out + first * g.ldo;
+        hipLaunchKernelGGL((g.k <= L ? route_grad_kernel<T, L, V, true> : route_grad_kernel<T, L, V, false>), dim3(wgs), dim3(THREADS), 0, ctx->stream, g);
+    });
 }
 // The smallest group of lanes that holds the logits of a token.  A choice among up to 128 experts for many tokens is bound by its operations, and groups of
 // eight lanes have fewer for each; for few tokens sixteen are sooner done (64 experts, 8 choices: 65536 tokens 8.2 us instead of 10.5, 16 tokens 3.5 instead of 3.0).
-template <typename T, typename Args> void launch_route(kfac_ctx *ctx, const Args &g) {
-    if (std::is_same_v<Args, RouteArgs> && g.E > 16 && g.E <= 128 && g.T >= 4096) {
-        if (g.E <= 64) launch_route<T, 8, 8>(ctx, g);
-        else launch_route<T, 8, 16>(ctx, g);
-    } else if (g.E <= 16) launch_route<T, 4, 4>(ctx, g);
-    else if (g.E <= 64) launch_route<T, 16, 4>(ctx, g);
-    else if (g.E <= 128) launch_route<T, 16, 8>(ctx, g);
-    else if (g.E <= 256) launch_route<T, 16, 16>(ctx, g);
-    else if (g.E <= 512) launch_route<T, 16, 32>(ctx, g);
-    else if (g.E <= 1024) launch_route<T, 64, 16>(ctx, g);
-    else launch_route<T, 64, 64>(ctx, g);
+template <typename T, typename Args> int launch_route(kfac_ctx *ctx, const Args &g) {
+    if constexpr (std::is_same_v<Args, RouteArgs>)
+        if (g.E > 16 && g.E <= 128 && g.T >= 4096) return g.E <= 64 ? launch_route<T, 8, 8>(ctx, g) : launch_route<T, 8, 16>(ctx, g);
+    if (g.E <= 16) return launch_route<T, 4, 4>(ctx, g);
+    if (g.E <= 64) return launch_route<T, 16, 4>(ctx, g);
+    if (g.E <= 128) return launch_route<T, 16, 8>(ctx, g);
+    if (g.E <= 256) return launch_route<T, 16, 16>(ctx, g);
+    if (g.E <= 512) return launch_route<T, 16, 32>(ctx, g);
+    if (g.E <= 1024) return launch_route<T, 64, 16>(ctx, g);
+    return launch_route<T, 64, 64>(ctx, g);
 }
 
 // Runs of a sort: short ones while their counts are few, as many as the workspace holds.  With a single one its counts become the
@@ -858,10 +885,7 @@ int kfac_launch_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, 
     const RouteArgs g{logits, ldl, tokens, experts, topk, normalize, ids, weights};
     const double n = (double)tokens * experts, es = dtype == KFAC_BF16 ? 2.0 : 4.0;
     KfacProfScope prof(ctx, KC_ROUTE, n * (4 + topk), n * es + 8.0 * tokens * topk);
-    if (dtype == KFAC_BF16) launch_route<unsigned short>(ctx, g);
-    else launch_route<float>(ctx, g);
-    KFAC_HIP_CHECK(hipGetLastError());
-    return KFAC_OK;
+    return dtype == KFAC_BF16 ? launch_route<unsigned short>(ctx, g) : launch_route<float>(ctx, g);
 }
 
 int kfac_launch_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, const int *ids, const float *dweights,
@@ -869,10 +893,7 @@ int kfac_launch_experts_route_grad(kfac_ctx *ctx, int tokens, int experts, int t
     const RouteGradArgs g{logits, ldl, tokens, experts, topk, normalize, ids, dweights, dlogits, ldd};
     const double n = (double)tokens * experts, s = (double)tokens * topk, es = dtype == KFAC_BF16 ? 2.0 : 4.0;
     KfacProfScope prof(ctx, KC_ROUTE, normalize ? 4.0 * s : 6.0 * n, es * (n + (normalize ? s : n)) + 8.0 * s);
-    if (dtype == KFAC_BF16) launch_route<unsigned short>(ctx, g);
-    else launch_route<float>(ctx, g);
-    KFAC_HIP_CHECK(hipGetLastError());
-    return KFAC_OK;
+    return dtype == KFAC_BF16 ? launch_route<unsigned short>(ctx, g) : launch_route<float>(ctx, g);
 }
 
 int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int experts, const int *ids, const void *X, int64_t ldx, int *offsets, int *rows, void *Xs,

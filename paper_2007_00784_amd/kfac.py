@@ -550,7 +550,7 @@ def _slots(t, name, shape=None, ints=True):
     if dtype not in _slot_types:
         import torch
         _slot_types.update({torch.int32: True, torch.float32: False})
-    if _slot_types.get(dtype) is not ints:
+    if _slot_types.get(dtype) is not ints:      # (None: neither)
         raise ValueError("%s must be %s" % (name, "int32" if ints else "float32"))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
@@ -594,7 +594,8 @@ def kfac_experts_route(ctx, logits, ids, weights, normalize=False):
     ip, shape = _slots(ids, "ids")
     wp, _ = _slots(weights, "weights", shape, False)
     lp, ldl, tokens, experts = _matrix(logits, "logits", logits.dtype, shape[0])
-    _on_gpu(logits, ids, weights)
+    if not (logits.is_cuda and ids.is_cuda and weights.is_cuda):
+        _on_gpu(logits, ids, weights)
     _check(lib().kfac_experts_route(ctx, _c_int(tokens), _c_int(experts), _c_int(shape[1]), lp, code, ldl, 1 if normalize else 0, ip, wp), "kfac_experts_route")
 
 
@@ -606,7 +607,8 @@ def kfac_experts_route_grad(ctx, logits, ids, dweights, dlogits, normalize=False
     wp, _ = _slots(dweights, "dweights", shape, False)
     lp, ldl, tokens, experts = _matrix(logits, "logits", dtype, shape[0])
     dp, ldd, _, _ = _matrix(dlogits, "dlogits", dtype, tokens, experts)
-    _on_gpu(logits, ids, dweights, dlogits)
+    if not (logits.is_cuda and ids.is_cuda and dweights.is_cuda and dlogits.is_cuda):
+        _on_gpu(logits, ids, dweights, dlogits)
     _check(lib().kfac_experts_route_grad(ctx, _c_int(tokens), _c_int(experts), _c_int(shape[1]), lp, code, ldl, ip, wp, 1 if normalize else 0, dp, ldd),
            "kfac_experts_route_grad")
 
@@ -640,7 +642,8 @@ def kfac_experts_dispatch(ctx, ids, X, offsets, rows, Xs):
         if R < tokens * topk:
             raise ValueError("Xs must have a row for each slot")
         d = _slot_desc(tokens, topk, R, width, code)
-    _on_gpu(ids, X, offsets, rows, Xs)
+    if not (ids.is_cuda and offsets.is_cuda and rows.is_cuda and (X is None or (X.is_cuda and Xs.is_cuda))):
+        _on_gpu(ids, X, offsets, rows, Xs)
     _check(lib().kfac_experts_dispatch(ctx, d, _c_int(experts), ip, xp, ldx, op, rp, sp, lds), "kfac_experts_dispatch")
 
 
@@ -664,7 +667,8 @@ def kfac_experts_combine(ctx, Ys, rows, weights, Y, add=None):
     yp, ldy, _, width = _matrix(Y, "Y", dtype, tokens)
     sp, lds, R, _ = _matrix(Ys, "Ys", dtype, None, width)
     ap, lda, _, _ = (None, 0, 0, 0) if add is None else _matrix(add, "add", dtype, tokens, width)
-    _on_gpu(Ys, rows, weights, Y, add)
+    if not (Ys.is_cuda and rows.is_cuda and Y.is_cuda and (weights is None or weights.is_cuda) and (add is None or add.is_cuda)):
+        _on_gpu(Ys, rows, weights, Y, add)
     _check(lib().kfac_experts_combine(ctx, _slot_desc(tokens, topk, R, width, code), rp, wp, sp, lds, ap, lda, yp, ldy), "kfac_experts_combine")
 
 
@@ -679,7 +683,8 @@ def kfac_experts_combine_grad(ctx, dY, Ys, rows, weights, dYs, dweights):
     yp, ldy, _, width = _matrix(dY, "dY", dtype, tokens)
     sp, lds, R, _ = _matrix(Ys, "Ys", dtype, None, width)
     op, ldo, _, _ = _matrix(dYs, "dYs", dtype, R, width)
-    _on_gpu(dY, Ys, rows, weights, dYs, dweights)
+    if not (dY.is_cuda and Ys.is_cuda and rows.is_cuda and weights.is_cuda and dYs.is_cuda and dweights.is_cuda):
+        _on_gpu(dY, Ys, rows, weights, dYs, dweights)
     _check(lib().kfac_experts_combine_grad(ctx, _slot_desc(tokens, topk, R, width, code), rp, wp, yp, ldy, sp, lds, op, ldo, gp), "kfac_experts_combine_grad")
 
 

@@ -515,3 +515,25 @@ def test_far_elements(ctx):
         results.append([ids, w, out.clone()])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_more_tokens_than_a_launch_has_workgroups(ctx):
+    """2^24 and some tokens of a workgroup each, of four to a workgroup, and as many routed: in two launches."""
+    T, d = (1 << 24) + 3, 1032
+    v = torch.randn(1, d, generator=torch.Generator().manual_seed(0)).bfloat16().to(DEV)
+    rows = torch.zeros(T, 1, dtype=torch.int32, device=DEV)
+    rows[-2:] = -1
+    Y = torch.zeros(T, d, dtype=torch.bfloat16, device=DEV)
+    K.kfac_experts_combine(ctx.h, v, rows, None, Y)
+    assert bool((Y[:5] == v).all()) and bool((Y[(1 << 23) - 3:(1 << 23) + 3] == v).all()) and bool((Y[-9:-2] == v).all()) and bool((Y[-2:] == 0).all())
+    assert bool((Y[:, 7] == v[0, 7])[:-2].all()) and bool((Y[:, -1] == v[0, -1])[:-2].all())
+    del Y
+    T, E = (1 << 25) + 5, 513
+    logits = torch.zeros(T, E, dtype=torch.bfloat16, device=DEV)
+    logits[:, 77] = 2.0
+    logits[-1, 500] = 3.0
+    ids, w = torch.full((T, 1), -7, dtype=torch.int32, device=DEV), torch.zeros(T, 1, device=DEV)
+    K.kfac_experts_route(ctx.h, logits, ids, w)
+    assert bool((ids[:-1] == 77).all()) and int(ids[-1]) == 500
+    want = math.exp(2.0) / (math.exp(2.0) + E - 1)
+    assert float((w[:-1].double() - want).abs().max()) <= (E + 30) * U * want

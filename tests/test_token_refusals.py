@@ -114,11 +114,11 @@ def grads(item=None, n=1, clip=True, ctx=CTX, max_norm=1.0, scale=None, norm=C, 
 def test_norm_and_clip():
     for clip in (False, True):
         for kw in (dict(item=dict(grad=None)), dict(item=dict(n=-1)), dict(item=dict(grad_dtype=2)), dict(n=-1), dict(ctx=None), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=NAN), dict(norm=None),
-                   dict(norm=D), dict(scale=C), dict(norm=C + 1), dict(coef=D + 2), dict(scale=E + 1)):
+                   dict(norm=D), dict(scale=C), dict(scale=D), dict(norm=C + 1), dict(coef=D + 2), dict(scale=E + 1)):
             assert grads(clip=clip, **kw) == BAD, kw
         f = K.lib().kfac_clip_grads_batched if clip else K.lib().kfac_grad_norm_batched
         assert f(CTX, 1, None, 1.0, None, C, D) == BAD
-    for kw in (dict(item=dict(out=None)), dict(item=dict(out=A)), dict(item=dict(out_dtype=2)), dict(coef=None), dict(scale=D)):
+    for kw in (dict(item=dict(out=None)), dict(item=dict(out=A)), dict(item=dict(out_dtype=2)), dict(coef=None)):
         assert grads(**kw) == BAD, kw
     f = K.lib().kfac_grad_norm_workspace_bytes
     assert f(-1, None) == 0 and f(1, None) == 0 and f(0, None) == 0
