@@ -42,7 +42,7 @@ template <typename T, int L, int V> __device__ constexpr int place(int v) {
     return v / N * (L * N) + v % N;
 }
 
-// The largest, the smallest, the sum over a group of 4, 8, 16 or 64 lanes, in all of them: inside a row of sixteen by the cross-lane moves.
+// The largest, the smallest, the sum over a group of 4 to 64 lanes, in all of them: inside a row of sixteen by the cross-lane moves.
 template <int L, typename F> __device__ inline unsigned group_fold(unsigned x, F fold) {
 #define KFAC_GROUP_STEP(ctrl) x = fold(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, true))
     KFAC_GROUP_STEP(0xB1);               // lanes 1 0 3 2
@@ -334,10 +334,11 @@ template <typename T, int L, int V, bool ONE> __global__ __launch_bounds__(THREA
 struct SortArgs {
     const int *ids;
     int S, E, k;             // slots, experts, slots of a token
-    int per, runs;           // slots of a run (a wave's, multiple of 64), runs
+    int per, runs;           // slots of a run (a workgroup's), runs
     int *offsets;            // [E + 1]
     int *rows;               // [S]
-    int *base;               // [runs][E]: slots of the expert in a run, then the row of the first of them
+    int *count;              // [runs][E]: slots of the expert in a run
+    int *base;               // [runs][E]: the row of the first of them.  (One run: both lie where the offsets do.)
 };
 
 __device__ inline int expert_of(int id, int E) { return (unsigned)id < (unsigned)E ? id : E; }
@@ -357,39 +358,6 @@ __device__ inline int rank_in_run(int e, int bits, int *seen) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     return had + before;
 }
-constexpr int AHEAD = 4;     // steps of a run whose experts are asked for together
-
-// Each wave counts its run's slots by expert and leaves at rows[s] how many of its own expert are in front of s in the run.
-__global__ __launch_bounds__(THREADS) void sort_count_kernel(const SortArgs g) {
-    extern __shared__ int shared[];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int run = blockIdx.x * (blockDim.x >> 6) + wave;
-    int *const seen = shared + wave * (g.E + 1);
-    for (int e = lane; e <= g.E; e += 64) seen[e] = 0;
-    __syncthreads();
-    const int64_t first = (int64_t)run * g.per;
-    if (run < g.runs) {
-        const int bits = 32 - __builtin_clz(g.E);         // of 0 .. E
-        const int last = (int)min(first + g.per, (int64_t)g.S);
-        for (int64_t s0 = first; s0 < last; s0 += 64 * AHEAD) {
-            int e[AHEAD];
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int64_t s = s0 + 64 * a + lane;
-                e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
-            }
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int64_t s = s0 + 64 * a + lane;
-                const int rank = rank_in_run(e[a], bits, seen);
-                if (s < last) g.rows[s] = e[a] < g.E ? rank : -1;
-            }
-        }
-    }
-    __syncthreads();
-    if (run < g.runs)
-        for (int e = lane; e < g.E; e += 64) g.base[(int64_t)run * g.E + e] = seen[e];
-}
 
 // Exclusive sums over the lanes of a workgroup of WAVES waves, and the total; `shared`: WAVES ints.
 template <int WAVES> __device__ inline int scan_workgroup(int x, int *shared, int &total) {
@@ -404,6 +372,7 @@ template <int WAVES> __device__ inline int scan_workgroup(int x, int *shared, in
     __syncthreads();
     int before = 0;
     total = 0;
+#pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         if (w < wave) before += shared[w];
         total += shared[w];
@@ -412,103 +381,136 @@ template <int WAVES> __device__ inline int scan_workgroup(int x, int *shared, in
     return before + incl - x;
 }
 
-// use(run, slots of e in it) for the runs r0 .. r1 - 1, eight counts asked for at a time.
-template <typename F> __device__ inline void each_run(const SortArgs &g, int e, int r0, int r1, F use) {
-    for (int r = r0; r < r1; r += 8) {
-        int c[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = g.base[(int64_t)min(r + i, r1 - 1) * g.E + e];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r + i < r1) use(r + i, c[i]);
-    }
-}
-
-// One workgroup: the counts of the runs become the rows at which each run's slots of an expert begin.
-constexpr int SCAN = 1024;
-__global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
-    __shared__ int part[SCAN], waves[SCAN / 64];
-    int at = 0;                                           // rows of the experts before e0
-    // W experts at a time, one for each of W threads, whose runs SCAN / W threads share
-    int W = 1;
-    while (W < g.E && W < SCAN) W <<= 1;
-    const int shares = SCAN / W, col = threadIdx.x % W, share = threadIdx.x / W;
-    const int each = (g.runs + shares - 1) / shares;
-    const int r0 = min(share * each, g.runs), r1 = min(r0 + each, g.runs);
-    for (int e0 = 0; e0 < g.E; e0 += W) {
-        const int e = e0 + col;
-        int sum = 0;
-        if (e < g.E) each_run(g, e, r0, r1, [&](int, int c) { sum += c; });
-        part[threadIdx.x] = sum;
-        __syncthreads();
-        int whole = 0, before = 0;                        // of the expert; of its shares before this one
-        for (int i = 0; i < shares; ++i) {
-            const int c = part[i * W + col];
-            whole += c;
-            before += i < share ? c : 0;
-        }
-        int total;
-        const int start = scan_workgroup<SCAN / 64>(share == 0 ? whole : 0, waves, total);
-        if (share == 0) {
-            part[col] = at + start;
-            if (e < g.E) g.offsets[e] = at + start;
-        }
-        __syncthreads();
-        int row = part[col] + before;
-        if (e < g.E)
-            each_run(g, e, r0, r1, [&](int r, int c) {
-                g.base[(int64_t)r * g.E + e] = row;
-                row += c;
-            });
-        at += total;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) g.offsets[g.E] = at;
-}
-
-// The whole order by one workgroup, whose waves take a run each: counts in LDS, then the rows at which each run's slots of an expert begin.
-constexpr int ONE_SLOTS = 4096, ONE_EXPERTS = 512, ONE_STEPS = ONE_SLOTS / SCAN;
-__global__ __launch_bounds__(SCAN) void sort_one_kernel(const SortArgs g) {
+constexpr int SCAN = 1024;        // threads of a workgroup that sorts, at most
+constexpr int STEPS = 4;          // of a wave over its slots that stay in registers
+// A run's slots, its waves' one after another: how many of its own expert are in front of each in the run (rows), and of each expert in all (count).
+// ALONE: a single run, E <= SCAN: the whole order, offsets and all.
+template <bool ALONE> __global__ __launch_bounds__(SCAN) void sort_count_kernel(const SortArgs g) {
     extern __shared__ int shared[];                       // [waves][E + 1]
-    __shared__ int waves[SCAN / 64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, pitch = g.E + 1;
+    __shared__ int sums[SCAN / 64];
+    const int n = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, pitch = g.E + 1;
     int *const seen = shared + wave * pitch;
-    int e[ONE_STEPS], rank[ONE_STEPS];
-    const int first = wave * g.per, last = min(first + g.per, g.S);
-#pragma unroll
-    for (int a = 0; a < ONE_STEPS; ++a) {
-        const int s = first + 64 * a + lane;
-        e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
-    }
-    for (int i = threadIdx.x; i < SCAN / 64 * pitch; i += SCAN) shared[i] = 0;
-    __syncthreads();
+    const int span = g.per / n;                           // of a wave, a multiple of 64
+    const int64_t first = (int64_t)blockIdx.x * g.per + (int64_t)wave * span;
+    const int64_t last = min(first + span, (int64_t)g.S);
     const int bits = 32 - __builtin_clz(g.E);             // of 0 .. E
+    int e[STEPS], rank[STEPS];
+    if (span <= 64 * STEPS)
 #pragma unroll
-    for (int a = 0; a < ONE_STEPS; ++a)
-        if (first + 64 * a < last) rank[a] = rank_in_run(e[a], bits, seen);
+        for (int a = 0; a < STEPS; ++a) {
+            const int64_t s = first + 64 * a + lane;
+            e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
+        }
+    for (int i = threadIdx.x; i < n * pitch; i += blockDim.x) shared[i] = 0;
     __syncthreads();
-    int count[SCAN / 64], whole = 0, total;               // of this thread's expert, by run
-    if ((int)threadIdx.x < g.E)
+    if (span <= 64 * STEPS) {
 #pragma unroll
-        for (int w = 0; w < SCAN / 64; ++w) {
-            count[w] = shared[w * pitch + threadIdx.x];
-            whole += count[w];
-        }
-    int row = scan_workgroup<SCAN / 64>(whole, waves, total);
-    if (threadIdx.x == 0) g.offsets[g.E] = total;
-    if ((int)threadIdx.x < g.E) {
-        g.offsets[threadIdx.x] = row;
+        for (int a = 0; a < STEPS; ++a)
+            if (first + 64 * a < last) rank[a] = rank_in_run(e[a], bits, seen);
+    } else
+        for (int64_t s0 = first; s0 < last; s0 += 64 * STEPS) {
 #pragma unroll
-        for (int w = 0; w < SCAN / 64; ++w) {
-            shared[w * pitch + threadIdx.x] = row;
-            row += count[w];
+            for (int a = 0; a < STEPS; ++a) {
+                const int64_t s = s0 + 64 * a + lane;
+                e[a] = s < last ? expert_of(g.ids[s], g.E) : g.E;
+            }
+#pragma unroll
+            for (int a = 0; a < STEPS; ++a) {
+                const int64_t s = s0 + 64 * a + lane;
+                const int r = rank_in_run(e[a], bits, seen);
+                if (s < last) g.rows[s] = e[a] < g.E ? r : -1;
+            }
         }
+    __syncthreads();
+    // what the waves in front of one have of an expert, in the place of what it has itself
+    int row = 0;
+    if (ALONE) {
+        int whole = 0, total;
+        if ((int)threadIdx.x < g.E)
+            for (int w = 0; w < n; ++w) whole += shared[w * pitch + threadIdx.x];
+        row = scan_workgroup<SCAN / 64>(whole, sums, total);
+        if (threadIdx.x == 0) g.offsets[g.E] = total;
+        if ((int)threadIdx.x < g.E) g.offsets[threadIdx.x] = row;
+    }
+    for (int c = threadIdx.x; c < g.E; c += blockDim.x) {
+        if (!ALONE) row = 0;
+        for (int w = 0; w < n; ++w) {
+            const int had = shared[w * pitch + c];
+            shared[w * pitch + c] = row;
+            row += had;
+        }
+        if (!ALONE) g.count[(int64_t)blockIdx.x * g.E + c] = row;
     }
     __syncthreads();
+    if (span <= 64 * STEPS) {
 #pragma unroll
-    for (int a = 0; a < ONE_STEPS; ++a) {
-        const int s = first + 64 * a + lane;
-        if (s < last) g.rows[s] = e[a] < g.E ? seen[e[a]] + rank[a] : -1;
+        for (int a = 0; a < STEPS; ++a) {
+            const int64_t s = first + 64 * a + lane;
+            if (s < last) g.rows[s] = e[a] < g.E ? seen[e[a]] + rank[a] : -1;
+        }
+    } else
+        for (int64_t s = first + lane; s < last; s += 64) {
+            const int r = g.rows[s];
+            if (r >= 0) g.rows[s] = r + seen[g.ids[s]];
+        }
+}
+
+// The counts of the runs become the rows at which each run's slots of an expert begin.  A workgroup takes SLICE experts, and adds up all counts of those before;
+// a single one takes slice after slice (which it has to where the counts lie in the place of the offsets).
+constexpr int SLICE = 64, SHARES = SCAN / SLICE;          // sixteen threads share an expert's runs
+constexpr int EACH = 8;                                   // counts that a thread asks for together
+__global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
+    __shared__ int part[SHARES][SLICE], sums[SCAN / 64], start[SLICE];
+    const int col = threadIdx.x % SLICE, share = threadIdx.x / SLICE;
+    const int each = (g.runs + SHARES - 1) / SHARES, r0 = min(share * each, g.runs), r1 = min(r0 + each, g.runs);
+    int below = 0;                                        // rows of the experts before the slice
+    for (int e0 = blockIdx.x * SLICE; e0 < g.E; e0 += gridDim.x * SLICE) {
+        const int e = e0 + col;
+        if (gridDim.x > 1) {
+            const int quads = e0 / 4;
+            int sum = 0;
+            for (int i = threadIdx.x; i < g.runs * quads; i += SCAN) {
+                const Vec<int, 4> c = load<int, 4>(g.count, (int64_t)(i / quads) * g.E + i % quads * 4);
+                sum += c.x[0] + c.x[1] + c.x[2] + c.x[3];
+            }
+            (void)scan_workgroup<SCAN / 64>(sum, sums, below);
+        }
+        int c[EACH], whole = 0;                           // this thread's runs of the expert, the first EACH of them
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) c[i] = e < g.E && r0 + i < r1 ? g.count[(int64_t)(r0 + i) * g.E + e] : 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) whole += c[i];
+        part[share][col] = whole;
+        __syncthreads();
+        if (threadIdx.x < SLICE) {                        // one wave: the shares in their order, then the experts
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < SHARES; ++i) {
+                const int had = part[i][col];
+                part[i][col] = at;
+                at += had;
+            }
+            int incl = at;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(incl, d);
+                if (col >= d) incl += o;
+            }
+            start[col] = below + incl - at;
+            if (e < g.E) g.offsets[e] = below + incl - at;
+            if (e == g.E - 1) g.offsets[g.E] = below + incl;
+            if (col == SLICE - 1) sums[0] = below + incl;
+        }
+        __syncthreads();
+        int row = start[col] + part[share][col];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (e < g.E && r0 + i < r1) {
+                g.base[(int64_t)(r0 + i) * g.E + e] = row;
+                row += c[i];
+            }
+        below = sums[0];
+        __syncthreads();
     }
 }
 
@@ -534,7 +536,7 @@ struct MoveArgs {
     void *out;
     int64_t ldo;
     float *dw;               // combine_grad
-    int part;                // columns of a workgroup (a launch's second dimension goes over them)
+    int part;                // vectors of a row that a workgroup takes (a launch's second dimension goes over them)
     SortArgs sort;           // dispatch
 };
 
@@ -561,13 +563,48 @@ __device__ inline void count_offsets(const SortArgs &g, const int *expert /* LDS
     if (threadIdx.x == 0) g.offsets[g.E] = total;
 }
 
-// Xs[rows[s]] = X[t]: every token is read once and stored k times.  LANES lanes take a token.
-template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS) void scatter_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), U = 2;
+// A row in vectors of N elements that begin anywhere.  What is left at its end, less than a vector, is the end of a vector that begins N in front of the
+// row's end, whose first elements are another's.  (Loads are whole vectors then.  With a path of its own for single elements, which a wave went through
+// besides the other, the sum of 20000 x 6 rows of 700 bf16 took 69 us instead of 46.)  A row shorter than a vector is one of single elements, N = 1.
+template <int N> struct Row {
+    int d, whole;
+    __device__ explicit Row(int width) : d(width), whole(width / N) {}
+    __device__ int vectors() const { return whole + (d % N != 0); }
+    __device__ int column(int q) const { return q < whole ? q * N : d - N; }
+    __device__ int others(int q) const { return q < whole ? 0 : N - d % N; }
+};
+template <typename T, int N, bool PAST> __device__ inline Vec<T, N> fetch(const void *p, int64_t i) {
+    if constexpr (PAST && N > 1) return load_past<T, N>(p, i);
+    else return load<T, N>(p, i);
+}
+template <typename T, int N> __device__ inline void put(void *p, int64_t i, const Vec<T, N> &r) {
+    if constexpr (N > 1) store_past(p, i, r);
+    else store(p, i, r);
+}
+template <typename T, int N> __device__ inline Vec<T, N> rounded(const float (&x)[N]) {
+    Vec<T, N> r;
+#pragma unroll
+    for (int n = 0; n < N; ++n) r.x[n] = element_of<T>(x[n]);
+    return r;
+}
+
+// Xs[rows[s]] = X[t]: every token is read once and stored k times, past the caches (105 us instead of 131 for 16384 x 4 rows of 4096 bf16).  LANES lanes take
+// a token, U vectors each at a time; the first are asked for before the rows are known.
+template <typename T, int N, int LANES, int MODE> __global__ __launch_bounds__(THREADS) void scatter_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, U = 2;
     extern __shared__ int shared[];                       // rows of the workgroup's slots [TOK k]; COUNTED: experts of all slots [S], counts [E]
     __shared__ int waves[THREADS / 64];
-    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK, t = t0 + threadIdx.x / LANES;
     const int mine = (int)min((int64_t)TOK, max((int64_t)g.T - t0, (int64_t)0)) * g.k;
+    const Row<N> row(g.d);
+    const int q0 = blockIdx.y * g.part + (int)(threadIdx.x % LANES), q1 = t < g.T ? min(row.vectors(), ((int)blockIdx.y + 1) * g.part) : 0;
+    const auto ask = [&](int q, Vec<T, N> (&r)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (q + u * LANES < q1) r[u] = load<T, N>(g.x, t * g.ldx + row.column(q + u * LANES));
+    };
+    Vec<T, N> r[U];
+    ask(q0, r);
     if (MODE == COUNTED) {
         int *const expert = shared + TOK * g.k;
         for (int s = threadIdx.x; s < g.sort.S; s += THREADS) expert[s] = expert_of(g.sort.ids[s], g.sort.E);
@@ -579,78 +616,38 @@ template <typename T, int LANES, int MODE> __global__ __launch_bounds__(THREADS)
         const int lane = threadIdx.x & 63;
         for (int i = threadIdx.x >> 6; i < mine; i += THREADS / 64) {
             const int s = (int)t0 * g.k + i, e = expert[s];
-            int row = 0;
+            int at = 0;
             for (int o = 0; o < g.sort.S; o += 64) {
                 const int f = o + lane < g.sort.S ? expert[o + lane] : g.sort.E;
-                row += __popcll(__ballot(f < e || (f == e && o + lane < s)));
+                at += __popcll(__ballot(f < e || (f == e && o + lane < s)));
             }
             if (lane == 0) {
-                shared[i] = row = e < g.sort.E ? row : -1;
-                if (blockIdx.y == 0) g.sort.rows[s] = row;
+                shared[i] = at = e < g.sort.E ? at : -1;
+                if (blockIdx.y == 0) g.sort.rows[s] = at;
             }
         }
     } else {
         for (int i = threadIdx.x; i < mine; i += THREADS) {
             const int64_t s = t0 * g.k + i;
-            const int row = MODE == RANKED ? ranked_row(g.sort, (unsigned)s) : g.rows[s];
-            if (MODE == RANKED) g.sort.rows[s] = row;
-            shared[i] = row;
+            const int at = MODE == RANKED ? ranked_row(g.sort, (unsigned)s) : g.rows[s];
+            if (MODE == RANKED) g.sort.rows[s] = at;
+            shared[i] = at;
         }
     }
     __syncthreads();
-    const int64_t t = t0 + threadIdx.x / LANES;
-    if (t >= g.T) return;
     const int *const rows = shared + threadIdx.x / LANES * g.k;
-    const int c0 = blockIdx.y * g.part, c1 = min(g.d, c0 + g.part);
-    for (int i = c0 + (int)(threadIdx.x % LANES) * N; i < c1; i += LANES * N * U) {
-        if (i + (U - 1) * LANES * N + N <= c1) {
-            Vec<T, N> r[U];
+    for (int q = q0; q < q1; q += LANES * U) {
+        Vec<T, N> now[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) r[u] = load<T, N>(g.x, t * g.ldx + i + u * LANES * N);
-            for (int j = 0; j < g.k; ++j) {
-                const int row = rows[j];
-                if ((unsigned)row >= (unsigned)g.R) continue;
+        for (int u = 0; u < U; ++u) now[u] = r[u];
+        ask(q + LANES * U, r);
+        for (int j = 0; j < g.k; ++j) {
+            const int at = rows[j];
+            if ((unsigned)at >= (unsigned)g.R) continue;
 #pragma unroll
-                for (int u = 0; u < U; ++u) store_past(g.out, row * g.ldo + i + u * LANES * N, r[u]);
-            }
-        } else {
-            for (int u = 0; u < U; ++u) {
-                const int b = i + u * LANES * N, in = min(N, c1 - b);
-                Vec<T, N> r{};
-                if (in == N) r = load<T, N>(g.x, t * g.ldx + b);
-                else
-                    for (int n = 0; n < in; ++n) r.x[n] = ((const T *)g.x)[t * g.ldx + b + n];
-                for (int j = 0; j < g.k; ++j) {
-                    const int row = rows[j];
-                    if ((unsigned)row >= (unsigned)g.R) continue;
-                    if (in == N) store_past(g.out, row * g.ldo + b, r);
-                    else
-                        for (int n = 0; n < in; ++n) ((T *)g.out)[row * g.ldo + b + n] = r.x[n];
-                }
-            }
+            for (int u = 0; u < U; ++u)
+                if (q + u * LANES < q1) put<T, N>(g.out, at * g.ldo + row.column(q + u * LANES), now[u]);
         }
-    }
-}
-
-// N elements from i on; `in` of them exist, the others are zero (FULL: all exist).  PAST: loaded past the caches.
-template <typename T, int N, bool FULL, bool PAST> __device__ inline Vec<T, N> fetch(const void *p, int64_t i, int in) {
-    if (FULL || in >= N) return PAST ? load_past<T, N>(p, i) : load<T, N>(p, i);
-    Vec<T, N> r{};
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-        if (n < in) r.x[n] = ((const T *)p)[i + n];
-    return r;
-}
-template <typename T, int N, bool FULL> __device__ inline void put(void *p, int64_t i, int in, const float (&x)[N]) {
-    if (FULL || in >= N) {
-        Vec<T, N> r;
-#pragma unroll
-        for (int n = 0; n < N; ++n) r.x[n] = element_of<T>(x[n]);
-        store_past(p, i, r);
-    } else {
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-            if (n < in) ((T *)p)[i + n] = element_of<T>(x[n]);
     }
 }
 
@@ -664,44 +661,39 @@ __device__ inline void slots_of(const MoveArgs &g, int64_t t0, int mine, int *ro
     __syncthreads();
 }
 
-// A step of a lane goes over U vectors, LANES vectors apart.  F(FULL, column) for the steps of this lane from c0 to c1.
-template <int STEP, int N, int U, typename F> __device__ inline void each_step(int c0, int c1, F f) {
-    for (int i = c0; i < c1; i += STEP * U) {
-        if (i + (U - 1) * STEP + N <= c1) f(std::true_type{}, i);
-        else f(std::false_type{}, i);
-    }
-}
-
-// Y[t] = add[t] + sum_j w[s] Ys[rows[s]]: sums in fp32 in the order of j, rounded once.  KB rows are asked for at a time, two vectors of each.
-template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), STEP = LANES * N, U = 2;
+// Y[t] = add[t] + sum_j w[s] Ys[rows[s]]: sums in fp32 in the order of j, rounded once.  KB rows are asked for at a time, U vectors of each.
+template <typename T, int N, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, U = 2;
     extern __shared__ int shared[];
     float *const weights = (float *)(shared + TOK * g.k);
-    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK, t = t0 + threadIdx.x / LANES;
+    const Row<N> row(g.d);
+    const int q0 = blockIdx.y * g.part + (int)(threadIdx.x % LANES), q1 = t < g.T ? min(row.vectors(), ((int)blockIdx.y + 1) * g.part) : 0;
     slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
-    const int64_t t = t0 + threadIdx.x / LANES;
-    if (t >= g.T) return;
     const int *const rows = shared + threadIdx.x / LANES * g.k;
     const float *const w = weights + threadIdx.x / LANES * g.k;
-    const int c0 = blockIdx.y * g.part, c1 = min(g.d, c0 + g.part);
-    each_step<STEP, N, U>(c0 + (int)(threadIdx.x % LANES) * N, c1, [&](auto full, int i) {
-        constexpr bool FULL = decltype(full)::value;
+    for (int q = q0; q < q1; q += LANES * U) {
+        Vec<T, N> a[U] = {};
+        if (g.y)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (q + u * LANES < q1) a[u] = fetch<T, N, PAST>(g.y, t * g.ldy + row.column(q + u * LANES));
         float sum[U][N];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const Vec<T, N> a = g.y ? fetch<T, N, FULL, PAST>(g.y, t * g.ldy + i + u * STEP, c1 - i - u * STEP) : Vec<T, N>{};
-#pragma unroll
-            for (int n = 0; n < N; ++n) sum[u][n] = value_of(a.x[n]);
-        }
         for (int j0 = 0; j0 < g.k; j0 += KB) {
             Vec<T, N> x[KB][U];
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
-                const int row = rows[min(j0 + j, g.k - 1)];
-                if (row >= 0)
+                const int at = rows[min(j0 + j, g.k - 1)];
+                if (at >= 0)
 #pragma unroll
-                    for (int u = 0; u < U; ++u) x[j][u] = fetch<T, N, FULL, PAST>(g.x, row * g.ldx + i + u * STEP, c1 - i - u * STEP);
+                    for (int u = 0; u < U; ++u)
+                        if (q + u * LANES < q1) x[j][u] = fetch<T, N, PAST>(g.x, at * g.ldx + row.column(q + u * LANES));
             }
+            if (j0 == 0)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sum[u][n] = value_of(a[u].x[n]);
 #pragma unroll
             for (int j = 0; j < KB; ++j)
                 if (j0 + j < g.k && rows[j0 + j] >= 0)
@@ -711,50 +703,66 @@ template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__
                         for (int n = 0; n < N; ++n) sum[u][n] = fmaf(w[j0 + j], value_of(x[j][u].x[n]), sum[u][n]);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) put<T, N, FULL>(g.out, t * g.ldo + i + u * STEP, c1 - i - u * STEP, sum[u]);
-    });
+        for (int u = 0; u < U; ++u) {
+            const int v = q + u * LANES;
+            if (v >= q1) continue;
+            const Vec<T, N> o = rounded<T>(sum[u]);
+            const int64_t at = t * g.ldo + row.column(v);
+            if (row.others(v) == 0) put<T, N>(g.out, at, o);
+            else                                          // (the others' elements may be what is added, not yet read)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    if (n >= row.others(v)) ((T *)g.out)[at + n] = o.x[n];
+        }
+    }
 }
 
 // dYs[rows[s]] = w[s] dY[t] and dw[s] = <dY[t], Ys[rows[s]]>, KB slots of a token at a time.  A lane's share of a product is summed in fp32 in
 // the order of the columns, the lanes' then by halves: the same order from run to run.
-template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, N = 16 / (int)sizeof(T), STEP = LANES * N;
+template <typename T, int N, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
+    constexpr int TOK = THREADS / LANES, WAVES = LANES / 64;
     extern __shared__ int shared[];
     __shared__ float partial[THREADS / 64][KB];
     float *const weights = (float *)(shared + TOK * g.k);
-    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK;
-    slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
-    const int64_t t = t0 + threadIdx.x / LANES;
+    const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK, t = t0 + threadIdx.x / LANES;
     const bool there = t < g.T;
-    const int lane = threadIdx.x % LANES;
+    const Row<N> row(g.d);
+    const int lane = threadIdx.x % LANES, q1 = there ? row.vectors() : 0;
+    Vec<T, N> first;                                      // of dY, asked for before the rows are known
+    if (lane < q1) first = fetch<T, N, PAST>(g.x, t * g.ldx + row.column(lane));
+    slots_of(g, t0, (int)min((int64_t)TOK, (int64_t)g.T - t0) * g.k, shared, weights);
     const int *const rows = shared + threadIdx.x / LANES * g.k;
     const float *const w = weights + threadIdx.x / LANES * g.k;
     for (int j0 = 0; j0 < g.k; j0 += KB) {
         float dot[KB];
 #pragma unroll
         for (int j = 0; j < KB; ++j) dot[j] = 0.f;
-        each_step<STEP, N, 1>(lane * N, there ? g.d : 0, [&](auto full, int i) {
-            constexpr bool FULL = decltype(full)::value;
-            const Vec<T, N> dy = fetch<T, N, FULL, PAST>(g.x, t * g.ldx + i, g.d - i);
+        for (int q = lane; q < q1; q += LANES) {
+            const int c = row.column(q);
+            const Vec<T, N> dy = q == lane ? first : fetch<T, N, PAST>(g.x, t * g.ldx + c);
             Vec<T, N> x[KB];
 #pragma unroll
             for (int j = 0; j < KB; ++j)
-                if (j0 + j < g.k && rows[j0 + j] >= 0) x[j] = fetch<T, N, FULL, PAST>(g.y, rows[j0 + j] * g.ldy + i, g.d - i);
+                if (j0 + j < g.k && rows[j0 + j] >= 0) x[j] = fetch<T, N, PAST>(g.y, rows[j0 + j] * g.ldy + c);
+            float v[N];                                   // what is another's has its place in the stored vector, not in the sum
+            const int others = row.others(q);
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] = n >= others ? value_of(dy.x[n]) : 0.f;
 #pragma unroll
             for (int j = 0; j < KB; ++j)
                 if (j0 + j < g.k && rows[j0 + j] >= 0)
 #pragma unroll
-                    for (int n = 0; n < N; ++n) dot[j] = fmaf(value_of(dy.x[n]), value_of(x[j].x[n]), dot[j]);
-            __builtin_amdgcn_sched_barrier(0);       // (stores between the loads: 229 us instead of 220 for 16384 x 4 rows of 4096 bf16)
+                    for (int n = 0; n < N; ++n) dot[j] = n >= others ? fmaf(v[n], value_of(x[j].x[n]), dot[j]) : dot[j];
+            __builtin_amdgcn_sched_barrier(0);            // (stores between the loads: 229 us instead of 220 for 16384 x 4 rows of 4096 bf16)
 #pragma unroll
             for (int j = 0; j < KB; ++j)
                 if (j0 + j < g.k && rows[j0 + j] >= 0) {
                     float o[N];
 #pragma unroll
                     for (int n = 0; n < N; ++n) o[n] = w[j0 + j] * value_of(dy.x[n]);
-                    put<T, N, FULL>(g.out, rows[j0 + j] * g.ldo + i, g.d - i, o);
+                    put<T, N>(g.out, rows[j0 + j] * g.ldo + c, rounded<T>(o));
                 }
-        });
+        }
 #pragma unroll
         for (int j = 0; j < KB; ++j) {
             dot[j] = group_sum<(LANES < 64 ? LANES : 64)>(dot[j]);
@@ -764,7 +772,7 @@ template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__
         if (there && lane < KB && j0 + lane < g.k) {
             float s = 0.f;
             if (LANES > 64) {
-                for (int v = 0; v < LANES / 64; ++v) s += partial[v][lane];
+                for (int v = 0; v < WAVES; ++v) s += partial[threadIdx.x / LANES * WAVES + v][lane];
             } else {
 #pragma unroll
                 for (int j = 0; j < KB; ++j) s = j == lane ? dot[j] : s;
@@ -775,27 +783,34 @@ template <typename T, int LANES, int KB, bool PAST> __global__ __launch_bounds__
     }
 }
 
-// Lanes for a token: sixteen where its row is sixteen vectors or less, a wave up to 128, else a workgroup.
-int lanes_of(int d, int es) {
-    const int vectors = (d * es + 15) / 16;
-    return vectors <= 16 ? 16 : vectors <= 128 ? 64 : 256;
+// Lanes for a token: a power of two from 8 to 256, for `each` vectors of its row a lane: two where rows are read (sums of 65536 x 2 rows of 256 bf16 19 us instead of
+// 29 with twice the lanes), one where they are stored (65536 x 8 rows of 100 fp32 74 us instead of 92: parts of cache lines go out alone).
+int lanes_of(int vectors, int each) {
+    int lanes = 8;
+    while (lanes < THREADS && lanes * each < vectors) lanes *= 2;
+    return lanes;
 }
-// Columns of a workgroup: a few long rows are cut until 512 workgroups share them, into parts of a vector for each lane at least.
-int part_of(int T, int d, int es, int lanes) {
-    const int step = lanes * (16 / es), tok = THREADS / lanes;
+// Vectors of a row that a workgroup takes: a few long rows are cut until 512 workgroups share them, into parts of a vector for each lane at least.
+int part_of(int T, int vectors, int lanes) {
+    const int tok = THREADS / lanes;
     const int64_t wgs = ((int64_t)T + tok - 1) / tok;
-    const int most = (d + step - 1) / step, want = (int)std::max<int64_t>(1, 512 / std::max<int64_t>(wgs, 1));
+    const int most = (vectors + lanes - 1) / lanes, want = (int)std::max<int64_t>(1, 512 / std::max<int64_t>(wgs, 1));
     const int parts = std::max(1, std::min(most, want)), steps = std::max(1, (most + parts - 1) / parts);
-    return steps * step;
+    return steps * lanes;
 }
 
-template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, double bytes) {
-    const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
-    g.part = MODE == RANKED ? (1 << 30) : part_of(g.T, g.d, sizeof(T), lanes);   // (a second workgroup of a slot would find its rank replaced)
-    const unsigned parts = MODE == RANKED ? 1 : std::max(1, (g.d + g.part - 1) / g.part);     // (no columns: the order of the slots alone)
+template <typename T, int N, int MODE> auto scatter_of(int lanes) {
+    if constexpr (N == 1) return scatter_kernel<T, 1, 8, MODE>;
+    else return lanes == 8 ? scatter_kernel<T, N, 8, MODE> : lanes == 16 ? scatter_kernel<T, N, 16, MODE> : lanes == 32 ? scatter_kernel<T, N, 32, MODE> : lanes == 64 ? scatter_kernel<T, N, 64, MODE>
+              : lanes == 128 ? scatter_kernel<T, N, 128, MODE> : scatter_kernel<T, N, 256, MODE>;
+}
+template <typename T, int N, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, double bytes) {
+    const int vectors = (g.d + N - 1) / N, lanes = lanes_of(vectors, 1), tok = THREADS / lanes;
+    g.part = MODE == RANKED ? 1 << 30 : part_of(g.T, vectors, lanes);     // (a second workgroup of a slot would find its rank replaced)
+    const unsigned parts = MODE == RANKED ? 1 : std::max(1, (vectors + g.part - 1) / g.part);     // (no columns: the order of the slots alone)
     const size_t lds = 4 * ((size_t)tok * g.k + (MODE == COUNTED ? g.sort.S + g.sort.E : 0));
+    const auto kernel = scatter_of<T, N, MODE>(lanes);
     KfacProfScope prof(ctx, KC_TOKENS, 0.0, bytes);
-    const auto kernel = lanes == 16 ? scatter_kernel<T, 16, MODE> : lanes == 64 ? scatter_kernel<T, 64, MODE> : scatter_kernel<T, 256, MODE>;
     if (MODE == COUNTED) {                                // (one workgroup more, for the offsets)
         hipLaunchKernelGGL(kernel, dim3((g.T + tok - 1) / tok + 1, parts), dim3(THREADS), lds, ctx->stream, g);
         KFAC_HIP_CHECK(hipGetLastError());
@@ -806,24 +821,37 @@ template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, do
         hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(THREADS), lds, ctx->stream, g);
     });
 }
+template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, const MoveArgs &g, double bytes) {
+    constexpr int N = 16 / (int)sizeof(T);
+    return g.d < N ? launch_scatter<T, 1, MODE>(ctx, g, bytes) : launch_scatter<T, N, MODE>(ctx, g, bytes);
+}
 
-// The experts' rows are read past the caches where they are too long to be there still.
-constexpr double PAST_BYTES = 128e6;
-template <typename T, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
-    const int lanes = lanes_of(g.d, sizeof(T)), tok = THREADS / lanes;
+template <typename T, int N, int KB, bool PAST> auto combine_of(int lanes, bool grad) {
+    if constexpr (N == 1) return grad ? combine_grad_kernel<T, 1, 8, KB, PAST> : combine_kernel<T, 1, 8, KB, PAST>;
+    else if (grad) return lanes == 8 ? combine_grad_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_grad_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_grad_kernel<T, N, 32, KB, PAST>
+                   : lanes == 64 ? combine_grad_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_grad_kernel<T, N, 128, KB, PAST> : combine_grad_kernel<T, N, 256, KB, PAST>;
+    else return lanes == 8 ? combine_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_kernel<T, N, 32, KB, PAST> : lanes == 64 ? combine_kernel<T, N, 64, KB, PAST>
+              : lanes == 128 ? combine_kernel<T, N, 128, KB, PAST> : combine_kernel<T, N, 256, KB, PAST>;
+}
+template <typename T, int N, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
+    const bool grad = g.dw != nullptr;
+    const int vectors = (g.d + N - 1) / N, lanes = lanes_of(vectors, grad ? 1 : 2), tok = THREADS / lanes;
     const size_t lds = 8 * (size_t)tok * g.k;
-    g.part = g.dw ? g.d : part_of(g.T, g.d, sizeof(T), lanes);
-    const unsigned parts = (g.d + g.part - 1) / g.part;
-    const auto kernel = g.dw ? (lanes == 16 ? combine_grad_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_grad_kernel<T, 64, KB, PAST> : combine_grad_kernel<T, 256, KB, PAST>)
-                             : (lanes == 16 ? combine_kernel<T, 16, KB, PAST> : lanes == 64 ? combine_kernel<T, 64, KB, PAST> : combine_kernel<T, 256, KB, PAST>);
+    g.part = grad ? vectors : part_of(g.T, vectors, lanes);
+    const unsigned parts = (vectors + g.part - 1) / g.part;
+    const auto kernel = combine_of<T, N, KB, PAST>(lanes, grad);
     KfacProfScope prof(ctx, KC_TOKENS, flops, bytes);
     return each_launch(g.T, tok, [&](int first, unsigned wgs) {
         g.first = first;
         hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(THREADS), lds, ctx->stream, g);
     });
 }
+// The experts' rows are read past the caches where they are too long to be there still.
+constexpr double PAST_BYTES = 128e6;
 template <typename T, int KB> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
-    return (double)sizeof(T) * g.d * g.T * g.k > PAST_BYTES ? launch_combine<T, KB, true>(ctx, g, flops, bytes) : launch_combine<T, KB, false>(ctx, g, flops, bytes);
+    constexpr int N = 16 / (int)sizeof(T);
+    if (g.d < N) return launch_combine<T, 1, KB, false>(ctx, g, flops, bytes);
+    return (double)sizeof(T) * g.d * g.T * g.k > PAST_BYTES ? launch_combine<T, N, KB, true>(ctx, g, flops, bytes) : launch_combine<T, N, KB, false>(ctx, g, flops, bytes);
 }
 template <typename T> int launch_combine(kfac_ctx *ctx, const MoveArgs &g, double flops, double bytes) {
     return g.k == 1 ? launch_combine<T, 1>(ctx, g, flops, bytes) : g.k == 2 ? launch_combine<T, 2>(ctx, g, flops, bytes) : launch_combine<T, 4>(ctx, g, flops, bytes);
@@ -864,13 +892,14 @@ template <typename T, typename Args> int launch_route(kfac_ctx *ctx, const Args 
     return launch_route<T, 64, 64>(ctx, g);
 }
 
-// Runs of a sort: short ones while their counts are few, as many as the workspace holds.  With a single one its counts become the
+// Waves of a workgroup that sorts, for its counts in LDS.
+int sort_waves(int E) { return E <= 512 ? 16 : E <= 1024 ? 8 : E <= 2048 ? 4 : 2; }
+constexpr int ONE_SLOTS = 64 * STEPS * SCAN / 64, ONE_EXPERTS = 512;     // what one workgroup sorts alone
+// Runs of a sort: as many as the workspace holds, up to as many as a workgroup of the scan has places for.  With a single one its counts become the
 // offsets themselves, where they are.
-constexpr int RUN = 256;
-constexpr int64_t COUNTS = 1 << 16;
 int runs_of(int64_t S, int E, size_t ws_bytes) {
-    const int64_t most = std::min<int64_t>((S + RUN - 1) / RUN, std::max<int64_t>(COUNTS / E, 64));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)(std::min<size_t>(ws_bytes, (size_t)1 << 40) / ((size_t)E * sizeof(int)))));
+    const int64_t step = 64 * sort_waves(E), most = std::min<int64_t>((S + step - 1) / step, SHARES * EACH);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)(std::min<size_t>(ws_bytes, (size_t)1 << 40) / (2 * (size_t)E * sizeof(int)))));
 }
 
 }  // namespace
@@ -878,7 +907,7 @@ int runs_of(int64_t S, int E, size_t ws_bytes) {
 size_t kfac_experts_dispatch_ws_bytes_impl(int tokens, int topk, int experts) {
     const int64_t S = (int64_t)tokens * topk;
     if (S <= FEW_SLOTS || (S <= ONE_SLOTS && experts <= ONE_EXPERTS)) return 0;
-    return kfac_align_up((size_t)runs_of(S, experts, SIZE_MAX) * experts * sizeof(int), 256);
+    return kfac_align_up(2 * (size_t)runs_of(S, experts, SIZE_MAX) * experts * sizeof(int), 256);
 }
 
 int kfac_launch_experts_route(kfac_ctx *ctx, int tokens, int experts, int topk, const void *logits, int dtype, int64_t ldl, int normalize, int *ids, float *weights) {
@@ -919,24 +948,23 @@ int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int exp
     s.offsets = offsets;
     s.rows = rows;
     if (S <= FEW_SLOTS) return bf ? launch_scatter<unsigned short, COUNTED>(ctx, g, bytes) : launch_scatter<float, COUNTED>(ctx, g, bytes);
-    if (S <= ONE_SLOTS && experts <= ONE_EXPERTS) {
-        s.runs = SCAN / 64;
-        s.per = (int)((S + SCAN - 1) / SCAN * 64);
+    const int waves = sort_waves(experts), step = 64 * waves;
+    const size_t counts = (size_t)waves * sizeof(int) * (experts + 1);
+    const bool alone = S <= ONE_SLOTS && experts <= ONE_EXPERTS;
+    s.runs = alone ? 1 : runs_of(S, experts, ctx->ws_bytes);
+    s.per = (int)(((S + s.runs - 1) / s.runs + step - 1) / step * step);
+    s.runs = (int)((S + s.per - 1) / s.per);
+    s.count = s.runs > 1 ? (int *)ctx->ws : offsets;
+    s.base = s.runs > 1 ? s.count + (int64_t)s.runs * experts : offsets;
+    {
         KfacProfScope prof(ctx, KC_TOKENS, 0.0, 8.0 * (double)S);
-        hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(SCAN), SCAN / 64 * sizeof(int) * (experts + 1), ctx->stream, s);
+        hipLaunchKernelGGL((alone ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(s.runs), dim3(64 * waves), counts, ctx->stream, s);
+        if (!alone) hipLaunchKernelGGL(sort_scan_kernel, dim3(s.runs > 1 ? (experts + SLICE - 1) / SLICE : 1), dim3(SCAN), 0, ctx->stream, s);
+    }
+    if (alone) {
         KFAC_HIP_CHECK(hipGetLastError());
         if (!X) return KFAC_OK;
         return bf ? launch_scatter<unsigned short, GIVEN>(ctx, g, bytes) : launch_scatter<float, GIVEN>(ctx, g, bytes);
-    }
-    s.runs = runs_of(S, experts, ctx->ws_bytes);
-    s.per = (int)(((S + s.runs - 1) / s.runs + 63) / 64 * 64);
-    s.runs = (int)((S + s.per - 1) / s.per);
-    s.base = s.runs > 1 ? (int *)ctx->ws : offsets;
-    {
-        KfacProfScope prof(ctx, KC_TOKENS, 0.0, 8.0 * (double)S);
-        const int waves = experts <= 1024 ? THREADS / 64 : 1;      // of a workgroup, for its counts in LDS
-        hipLaunchKernelGGL(sort_count_kernel, dim3((s.runs + waves - 1) / waves), dim3(64 * waves), waves * sizeof(int) * (experts + 1), ctx->stream, s);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(SCAN), 0, ctx->stream, s);
     }
     KFAC_HIP_CHECK(hipGetLastError());
     if (X) return bf ? launch_scatter<unsigned short, RANKED>(ctx, g, bytes) : launch_scatter<float, RANKED>(ctx, g, bytes);
