@@ -588,23 +588,19 @@ template <typename T, int N> __device__ inline Vec<T, N> rounded(const float (&x
     return r;
 }
 
-// Xs[rows[s]] = X[t]: every token is read once and stored k times, past the caches (105 us instead of 131 for 16384 x 4 rows of 4096 bf16).  LANES lanes take
-// a token, U vectors each at a time; the first are asked for before the rows are known.
+// Xs[rows[s]] = X[t]: every token is read once and stored k times, past the caches.  LANES lanes take a token, a vector each at a time; the first is asked for
+// before the rows are known.  16384 x 4 rows of 4096 bf16 that no cache holds: 121 us, 5.5 TB/s, as much as a copy with such stores; with two
+// vectors a lane 128, with plain stores 124 (and 132 instead of 104 where X is in the cache).
 template <typename T, int N, int LANES, int MODE> __global__ __launch_bounds__(THREADS) void scatter_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, U = 2;
+    constexpr int TOK = THREADS / LANES;
     extern __shared__ int shared[];                       // rows of the workgroup's slots [TOK k]; COUNTED: experts of all slots [S], counts [E]
     __shared__ int waves[THREADS / 64];
     const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK, t = t0 + threadIdx.x / LANES;
     const int mine = (int)min((int64_t)TOK, max((int64_t)g.T - t0, (int64_t)0)) * g.k;
     const Row<N> row(g.d);
     const int q0 = blockIdx.y * g.part + (int)(threadIdx.x % LANES), q1 = t < g.T ? min(row.vectors(), ((int)blockIdx.y + 1) * g.part) : 0;
-    const auto ask = [&](int q, Vec<T, N> (&r)[U]) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (q + u * LANES < q1) r[u] = load<T, N>(g.x, t * g.ldx + row.column(q + u * LANES));
-    };
-    Vec<T, N> r[U];
-    ask(q0, r);
+    Vec<T, N> r;
+    if (q0 < q1) r = load<T, N>(g.x, t * g.ldx + row.column(q0));
     if (MODE == COUNTED) {
         int *const expert = shared + TOK * g.k;
         for (int s = threadIdx.x; s < g.sort.S; s += THREADS) expert[s] = expert_of(g.sort.ids[s], g.sort.E);
@@ -636,17 +632,12 @@ template <typename T, int N, int LANES, int MODE> __global__ __launch_bounds__(T
     }
     __syncthreads();
     const int *const rows = shared + threadIdx.x / LANES * g.k;
-    for (int q = q0; q < q1; q += LANES * U) {
-        Vec<T, N> now[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) now[u] = r[u];
-        ask(q + LANES * U, r);
+    for (int q = q0; q < q1; q += LANES) {
+        const Vec<T, N> now = r;
+        if (q + LANES < q1) r = load<T, N>(g.x, t * g.ldx + row.column(q + LANES));
         for (int j = 0; j < g.k; ++j) {
             const int at = rows[j];
-            if ((unsigned)at >= (unsigned)g.R) continue;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (q + u * LANES < q1) put<T, N>(g.out, at * g.ldo + row.column(q + u * LANES), now[u]);
+            if ((unsigned)at < (unsigned)g.R) put<T, N>(g.out, at * g.ldo + row.column(q), now);
         }
     }
 }

@@ -96,7 +96,7 @@ def logits_for(T, E, kind, gen):
     return x
 
 
-ROUTES = [(1, 1, 1), (5, 2, 2), (33, 3, 1), (7, 15, 4), (70, 16, 16), (9, 17, 3), (130, 64, 8), (31, 65, 6), (257, 128, 8), (12, 129, 64), (6, 200, 2), (5, 256, 64), (3, 257, 8),
+ROUTES = [(1, 1, 1), (5, 2, 2), (33, 3, 1), (7, 15, 4), (70, 16, 16), (9, 17, 3), (130, 64, 8), (31, 65, 6), (257, 128, 8), (4100, 64, 8), (4096, 17, 17), (4200, 100, 20), (4097, 128, 64), (12, 129, 64), (6, 200, 2), (5, 256, 64), (3, 257, 8),
           (4, 512, 4), (3, 513, 10), (2, 1000, 64), (3, 1024, 1), (2, 1025, 8), (2, 4095, 64), (1, 4096, 2)]
 
 
