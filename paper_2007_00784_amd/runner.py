@@ -329,8 +329,11 @@ class RoutedExpertRunner(ExpertRunner):
         K.kfac_experts_combine(self.ctx, self.y, self.row, self.weights, self.out, add=add)
         return self.out
 
-    def backward(self, x, g, accumulate=False):
-        """The tokens' gradient (returned), every expert's (self.grad) and the router's (self.router_grad) from the output's.  (What was added passes g on.)"""
+    def backward(self, x, g, accumulate=False, gather=False):
+        """The tokens' gradient (returned), every expert's (self.grad) and the router's (self.router_grad) from the output's.  (What was added passes g on.)
+        gather: the sorted rows are made from x once more (where layers share self.xs, another's stand there by now)."""
+        if gather:
+            K.kfac_experts_gather(self.ctx, self.row, x, self.xs)
         K.kfac_experts_combine_grad(self.ctx, g, self.y, self.row, self.weights, self.gs, self.dweights)
         super().backward(self.xs, self.gs, self.offsets, accumulate=accumulate)
         K.kfac_experts_route_grad(self.ctx, self.logits, self.ids, self.dweights, self.dlogits, normalize=self.normalize)
