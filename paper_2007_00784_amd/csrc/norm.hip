@@ -4,7 +4,8 @@
 //
 // Squares and sums are in 64 bits: the square of an fp32 gradient need not have one in fp32 (above 2^64, below 2^-75), and of many small terms
 // behind a large sum fp32 would lose most.  A first launch leaves one sum for each workgroup; a second adds them in a fixed order, so that the
-// result is the same from run to run: one workgroup for the norm alone, every workgroup for itself where it goes on to clip.  Bound by memory.
+// result is the same from run to run: one workgroup for the norm alone, every workgroup for itself where it goes on to clip.  Bound by memory; a
+// short list by its launches.
 #include <algorithm>
 #include <cmath>
 #include "kfac_internal.h"
@@ -44,18 +45,18 @@ __device__ inline int item_of(const GradLaunch &a, unsigned chunk) {   // the la
 
 // What a thread has of a chunk: UNROLL vectors as they lie in memory, zeros behind the tensor's end.
 struct Raw { Vec<unsigned, 4> v[UNROLL]; };
-template <bool PAST> __device__ inline Raw raw_chunk(const void *p, int64_t first /* byte */, int64_t end, bool bf) {
+template <bool PAST> __device__ inline Raw raw_chunk(const void *p, int64_t first /* byte */, int64_t end, bool bf, int thread) {
     Raw r;
     if (first + CHUNK <= end) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const char *const at = (const char *)p + first + (u * THREADS + (int)threadIdx.x) * 16;
+            const char *const at = (const char *)p + first + (u * THREADS + thread) * 16;
             r.v[u] = PAST ? load_past<unsigned, 4>(at, 0) : load<unsigned, 4>(at, 0);
         }
     } else {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int64_t at = first + (u * THREADS + (int)threadIdx.x) * 16;
+            const int64_t at = first + (u * THREADS + thread) * 16;
             r.v[u] = Vec<unsigned, 4>{};
             if (at + 16 <= end) r.v[u] = load<unsigned, 4>((const char *)p + at, 0);
             else if (bf) {
@@ -85,25 +86,23 @@ template <int WAVES> __device__ inline double sum_workgroup(double x, double *sh
     return x;
 }
 
-// The next chunk is asked for before this one is summed.  PAST: a list that the cache cannot hold is read past it (537 MB: 79 us instead of 89, 6.8 TB/s);
-// of a shorter one the clipping, or the optimizer's step, finds what was read (102 MB: 33 us of clipping instead of 45).
-template <bool PAST> __global__ __launch_bounds__(THREADS) void norm_kernel(const GradLaunch a) {
-    __shared__ double shared[THREADS / 64];
-    unsigned c = blockIdx.x;
+// The squares of a thread's share of chunks c0, c0 + step, ..  The next chunk is asked for before this one is summed.
+template <bool PAST> __device__ inline double sum_chunks(const GradLaunch &a, unsigned c, unsigned step, int thread) {
+    double sum = 0.0;
+    if (c >= a.chunks) return sum;
     int id = item_of(a, c);
     const auto ask = [&](unsigned chunk, bool &bf) {
         while (id + 1 < a.n && a.item[id + 1].first <= chunk) ++id;
         const GradItem &it = a.item[id];
         bf = a.gbf[id] != 0;
-        return raw_chunk<PAST>(it.g, (int64_t)(chunk - it.first) * CHUNK, (int64_t)it.n * (bf ? 2 : 4), bf);
+        return raw_chunk<PAST>(it.g, (int64_t)(chunk - it.first) * CHUNK, (int64_t)it.n * (bf ? 2 : 4), bf, thread);
     };
-    double sum = 0.0;
     bool bf;
     Raw r = ask(c, bf);
-    for (; c < a.chunks; c += gridDim.x) {
+    for (; c < a.chunks; c += step) {
         const Raw now = r;
         const bool now_bf = bf;
-        if (c + gridDim.x < a.chunks) r = ask(c + gridDim.x, bf);
+        if (c + step < a.chunks) r = ask(c + step, bf);
         if (now_bf) {
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u)
@@ -123,7 +122,13 @@ template <bool PAST> __global__ __launch_bounds__(THREADS) void norm_kernel(cons
                 }
         }
     }
-    sum = sum_workgroup<THREADS / 64>(sum, shared);
+    return sum;
+}
+// PAST: a list that the cache cannot hold is read past it (537 MB: 79 us instead of 89, 6.8 TB/s); of a shorter one the clipping, or the
+// optimizer's step, finds what was read (102 MB: 33 us of clipping instead of 45).
+template <bool PAST> __global__ __launch_bounds__(THREADS) void norm_kernel(const GradLaunch a) {
+    __shared__ double shared[THREADS / 64];
+    const double sum = sum_workgroup<THREADS / 64>(sum_chunks<PAST>(a, blockIdx.x, gridDim.x, threadIdx.x), shared);
     if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
 }
 
@@ -135,7 +140,19 @@ struct NormArgs {
     float *norm, *coef;
 };
 constexpr int EACH = MOST / THREADS;     // sums that a thread asks for together
-// The coefficient; `writes`: this workgroup leaves both results.
+// The coefficient from the sum of all squares; `writes`: this thread leaves both results.
+__device__ inline float finish(const NormArgs &g, double scale, double sum, bool writes) {
+    const double norm = sqrt(sum) * fabs(scale);
+    // (a norm that is NaN makes the coefficient NaN, an infinite one makes it zero)
+    const double clip = norm > g.max_norm ? g.max_norm / norm : norm == norm ? 1.0 : norm;
+    const float coef = (float)(scale * clip);
+    if (writes) {
+        *g.norm = (float)norm;
+        if (g.coef) *g.coef = coef;
+    }
+    return coef;
+}
+// The same from the workgroups' sums.
 __device__ inline float join_sums(const NormArgs &g, bool writes, double *shared) {
     const double scale = g.scale ? (double)*g.scale : 1.0;
     double sum = 0.0;
@@ -149,19 +166,21 @@ __device__ inline float join_sums(const NormArgs &g, bool writes, double *shared
 #pragma unroll
         for (int k = 0; k < EACH; ++k) sum += x[k];
     }
-    const double norm = sqrt(sum_workgroup<THREADS / 64>(sum, shared)) * fabs(scale);
-    // (a norm that is NaN makes the coefficient NaN, an infinite one makes it zero)
-    const double clip = norm > g.max_norm ? g.max_norm / norm : norm == norm ? 1.0 : norm;
-    const float coef = (float)(scale * clip);
-    if (writes && threadIdx.x == 0) {
-        *g.norm = (float)norm;
-        if (g.coef) *g.coef = coef;
-    }
-    return coef;
+    return finish(g, scale, sum_workgroup<THREADS / 64>(sum, shared), writes && threadIdx.x == 0);
 }
 __global__ __launch_bounds__(THREADS) void norm_join_kernel(const NormArgs g) {
     __shared__ double shared[THREADS / 64];
     (void)join_sums(g, true, shared);
+}
+
+// A short list by one workgroup, whose sixteen waves take four chunks at a time: 128 KB 5.2 us a call instead of 8.4 by two launches, but 192 KB, waited for, no sooner.
+constexpr int ALONE = 1024;
+constexpr unsigned ALONE_CHUNKS = 8;
+__global__ __launch_bounds__(ALONE) void norm_alone_kernel(const GradLaunch a, const NormArgs g) {
+    __shared__ double shared[ALONE / 64];
+    const double scale = g.scale ? (double)*g.scale : 1.0;
+    const double sum = sum_workgroup<ALONE / 64>(sum_chunks<false>(a, threadIdx.x / THREADS, ALONE / THREADS, threadIdx.x % THREADS), shared);
+    (void)finish(g, scale, sum, threadIdx.x == 0);
 }
 
 // N results of a thread from element i on; `in` of them exist.
@@ -190,7 +209,7 @@ __global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a, const
         if (coef == 1.f && it.out == it.g) continue;
         const bool bf = a.gbf[id] != 0, obf = a.obf[id] != 0;
         const int64_t first = (int64_t)(c - it.first) * CHUNK;
-        const Raw r = raw_chunk<true>(it.g, first, (int64_t)it.n * (bf ? 2 : 4), bf);
+        const Raw r = raw_chunk<true>(it.g, first, (int64_t)it.n * (bf ? 2 : 4), bf, threadIdx.x);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int64_t at = first + (u * THREADS + (int)threadIdx.x) * 16;
@@ -262,9 +281,22 @@ size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items) {
 int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef, bool clip) {
     if (kfac_grad_norm_ws_bytes_impl(n, items) > ctx->ws_bytes) return KFAC_EWORKSPACE;
     double whole = 0.0;
-    for (int i = 0; i < n; ++i) whole += (double)items[i].n * (items[i].grad_dtype == KFAC_BF16 ? 2.0 : 4.0);
+    int64_t all = 0;                                      // chunks
+    for (int i = 0; i < n; ++i) {
+        const int64_t bytes = items[i].n * (items[i].grad_dtype == KFAC_BF16 ? 2 : 4);
+        whole += (double)bytes;
+        all += (bytes + CHUNK - 1) / CHUNK;
+    }
     NormArgs g{(double *)ctx->ws, 0, (double)max_norm, grad_scale, norm, coef};
+    bool alone = false;
     KFAC_CHECK(each_launch(n, items, [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t) -> int {
+        if (!clip && g.n == 0 && a.chunks <= ALONE_CHUNKS && a.chunks == all) {
+            alone = true;
+            KfacProfScope prof(ctx, KC_NORM, 2.0 * (double)elements, (double)bytes);
+            hipLaunchKernelGGL(norm_alone_kernel, dim3(1), dim3(ALONE), 0, ctx->stream, a, g);
+            KFAC_HIP_CHECK(hipGetLastError());
+            return KFAC_OK;
+        }
         const unsigned wgs = std::min<unsigned>(a.chunks, MOST);
         a.part = (double *)ctx->ws + g.n;
         g.n += (int)wgs;
@@ -273,6 +305,7 @@ int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *it
         KFAC_HIP_CHECK(hipGetLastError());
         return KFAC_OK;
     }));
+    if (alone) return KFAC_OK;
     if (!clip || g.n == 0) {
         KfacProfScope prof(ctx, KC_NORM, 0.0, 8.0 * g.n);
         hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(THREADS), 0, ctx->stream, g);

@@ -467,11 +467,16 @@ __global__ __launch_bounds__(SCAN) void sort_scan_kernel(const SortArgs g) {
     for (int e0 = blockIdx.x * SLICE; e0 < g.E; e0 += gridDim.x * SLICE) {
         const int e = e0 + col;
         if (gridDim.x > 1) {
-            const int quads = e0 / 4;
-            int sum = 0;
-            for (int i = threadIdx.x; i < g.runs * quads; i += SCAN) {
-                const Vec<int, 4> c = load<int, 4>(g.count, (int64_t)(i / quads) * g.E + i % quads * 4);
-                sum += c.x[0] + c.x[1] + c.x[2] + c.x[3];
+            int wide = 16, sum = 0;                       // threads for a run's counts, four each
+            while (wide * 4 < e0 && wide < SCAN) wide *= 2;
+            const int q = threadIdx.x % wide * 4, step = SCAN / wide;
+            for (int r = threadIdx.x / wide; r < g.runs && q < e0; r += EACH * step) {
+                Vec<int, 4> c[EACH] = {};
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (r + i * step < g.runs) c[i] = load<int, 4>(g.count, (int64_t)(r + i * step) * g.E + q);
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) sum += c[i].x[0] + c[i].x[1] + c[i].x[2] + c[i].x[3];
             }
             (void)scan_workgroup<SCAN / 64>(sum, sums, below);
         }
