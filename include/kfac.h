@@ -340,7 +340,8 @@ typedef struct {
  * rows[t][j] the row of slot (t, j) or -1, and Xs[rows[t][j]] = X[t].  offsets and Xs are what the products for layers of experts take.
  *   ids [tokens][topk];  offsets [experts + 1], rows [tokens][topk]: written;  X [tokens][d] with pitch ldx, Xs [rows][d] with pitch lds
  *   X = Xs = NULL: the order alone (d and the pitches are not looked at).  Rows of Xs from offsets[experts] on are left as they were.
- * More than 1024 slots make use of kfac_experts_dispatch_workspace_bytes() of the context's workspace; with less of it the sort takes longer.  */
+ * Many slots (or experts) make use of kfac_experts_dispatch_workspace_bytes() of the context's workspace (4 MB at most); with less of it the sort takes
+ * longer.  (So graphs captured from one context must not run at the same time.)  */
 int kfac_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *desc, int experts, const int *ids /* device */, const void *X, int64_t ldx, int *offsets, int *rows,
                           void *Xs, int64_t lds);
 size_t kfac_experts_dispatch_workspace_bytes(int tokens, int topk, int experts);

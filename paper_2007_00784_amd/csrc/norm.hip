@@ -18,7 +18,7 @@ namespace {
 constexpr int ITEMS = 100;           // tensors of a launch: the table and the rest of the arguments stay below 4 KB
 constexpr int THREADS = 256;
 constexpr int UNROLL = 4;            // vectors of 16 bytes of a thread and chunk
-constexpr int64_t CHUNK = 16 * THREADS * UNROLL;      // bytes
+template <int TH> constexpr int64_t chunk_bytes() { return 16 * TH * UNROLL; }     // of a chunk that TH threads take
 constexpr int MOST = 1024;           // workgroups of a launch that sums
 
 struct GradItem {
@@ -45,18 +45,18 @@ __device__ inline int item_of(const GradLaunch &a, unsigned chunk) {   // the la
 
 // What a thread has of a chunk: UNROLL vectors as they lie in memory, zeros behind the tensor's end.
 struct Raw { Vec<unsigned, 4> v[UNROLL]; };
-template <bool PAST> __device__ inline Raw raw_chunk(const void *p, int64_t first /* byte */, int64_t end, bool bf, int thread) {
+template <int TH, bool PAST> __device__ inline Raw raw_chunk(const void *p, int64_t first /* byte */, int64_t end, bool bf, int thread) {
     Raw r;
-    if (first + CHUNK <= end) {
+    if (first + chunk_bytes<TH>() <= end) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const char *const at = (const char *)p + first + (u * THREADS + thread) * 16;
+            const char *const at = (const char *)p + first + (u * TH + thread) * 16;
             r.v[u] = PAST ? load_past<unsigned, 4>(at, 0) : load<unsigned, 4>(at, 0);
         }
     } else {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int64_t at = first + (u * THREADS + thread) * 16;
+            const int64_t at = first + (u * TH + thread) * 16;
             r.v[u] = Vec<unsigned, 4>{};
             if (at + 16 <= end) r.v[u] = load<unsigned, 4>((const char *)p + at, 0);
             else if (bf) {
@@ -87,7 +87,7 @@ template <int WAVES> __device__ inline double sum_workgroup(double x, double *sh
 }
 
 // The squares of a thread's share of chunks c0, c0 + step, ..  The next chunk is asked for before this one is summed.
-template <bool PAST> __device__ inline double sum_chunks(const GradLaunch &a, unsigned c, unsigned step, int thread) {
+template <int TH, bool PAST> __device__ inline double sum_chunks(const GradLaunch &a, unsigned c, unsigned step, int thread) {
     double sum = 0.0;
     if (c >= a.chunks) return sum;
     int id = item_of(a, c);
@@ -95,7 +95,7 @@ template <bool PAST> __device__ inline double sum_chunks(const GradLaunch &a, un
         while (id + 1 < a.n && a.item[id + 1].first <= chunk) ++id;
         const GradItem &it = a.item[id];
         bf = a.gbf[id] != 0;
-        return raw_chunk<PAST>(it.g, (int64_t)(chunk - it.first) * CHUNK, (int64_t)it.n * (bf ? 2 : 4), bf, thread);
+        return raw_chunk<TH, PAST>(it.g, (chunk - it.first) * chunk_bytes<TH>(), (int64_t)it.n * (bf ? 2 : 4), bf, thread);
     };
     bool bf;
     Raw r = ask(c, bf);
@@ -128,7 +128,7 @@ template <bool PAST> __device__ inline double sum_chunks(const GradLaunch &a, un
 // optimizer's step, finds what was read (102 MB: 33 us of clipping instead of 45).
 template <bool PAST> __global__ __launch_bounds__(THREADS) void norm_kernel(const GradLaunch a) {
     __shared__ double shared[THREADS / 64];
-    const double sum = sum_workgroup<THREADS / 64>(sum_chunks<PAST>(a, blockIdx.x, gridDim.x, threadIdx.x), shared);
+    const double sum = sum_workgroup<THREADS / 64>(sum_chunks<THREADS, PAST>(a, blockIdx.x, gridDim.x, threadIdx.x), shared);
     if (threadIdx.x == 0) a.part[blockIdx.x] = sum;
 }
 
@@ -173,16 +173,6 @@ __global__ __launch_bounds__(THREADS) void norm_join_kernel(const NormArgs g) {
     (void)join_sums(g, true, shared);
 }
 
-// A short list by one workgroup, whose sixteen waves take four chunks at a time: 128 KB 5.2 us a call instead of 8.4 by two launches, but 192 KB, waited for, no sooner.
-constexpr int ALONE = 1024;
-constexpr unsigned ALONE_CHUNKS = 8;
-__global__ __launch_bounds__(ALONE) void norm_alone_kernel(const GradLaunch a, const NormArgs g) {
-    __shared__ double shared[ALONE / 64];
-    const double scale = g.scale ? (double)*g.scale : 1.0;
-    const double sum = sum_workgroup<ALONE / 64>(sum_chunks<false>(a, threadIdx.x / THREADS, ALONE / THREADS, threadIdx.x % THREADS), shared);
-    (void)finish(g, scale, sum, threadIdx.x == 0);
-}
-
 // N results of a thread from element i on; `in` of them exist.
 template <typename O, int N> __device__ inline void put(void *p, int64_t i, int64_t in, const float (&x)[N]) {
     Vec<O, N> o;
@@ -197,6 +187,34 @@ template <typename O, int N> __device__ inline void put(void *p, int64_t i, int6
             if (k < in) ((O *)p)[i + k] = o.x[k];
 }
 
+// A thread's share of chunk c of tensor id, times coef.
+template <int TH> __device__ inline void clip_chunk(const GradLaunch &a, int id, unsigned c, float coef, int thread) {
+    const GradItem &it = a.item[id];
+    const bool bf = a.gbf[id] != 0, obf = a.obf[id] != 0;
+    const int64_t first = (c - it.first) * chunk_bytes<TH>();
+    const Raw r = raw_chunk<TH, true>(it.g, first, (int64_t)it.n * (bf ? 2 : 4), bf, thread);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int64_t at = first + (u * TH + thread) * 16;
+        if (bf) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[2 * k] = low_bf16(r.v[u].x[k]) * coef;
+                x[2 * k + 1] = high_bf16(r.v[u].x[k]) * coef;
+            }
+            if (obf) put<unsigned short, 8>(it.out, at / 2, it.n - at / 2, x);
+            else put<float, 8>(it.out, at / 2, it.n - at / 2, x);
+        } else {
+            float x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(r.v[u].x[k]) * coef;
+            if (obf) put<unsigned short, 4>(it.out, at / 4, it.n - at / 4, x);
+            else put<float, 4>(it.out, at / 4, it.n - at / 4, x);
+        }
+    }
+}
+
 // The last chunks first: what was read last may still be in the cache.  Nothing is read a third time, so loads and stores go past it.
 __global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a, const NormArgs g, bool writes) {
     __shared__ double shared[THREADS / 64];
@@ -205,32 +223,26 @@ __global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a, const
     for (unsigned q = blockIdx.x; q < a.chunks; q += gridDim.x) {
         const unsigned c = a.chunks - 1 - q;
         while (a.item[id].first > c) --id;
-        const GradItem &it = a.item[id];
-        if (coef == 1.f && it.out == it.g) continue;
-        const bool bf = a.gbf[id] != 0, obf = a.obf[id] != 0;
-        const int64_t first = (int64_t)(c - it.first) * CHUNK;
-        const Raw r = raw_chunk<true>(it.g, first, (int64_t)it.n * (bf ? 2 : 4), bf, threadIdx.x);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int64_t at = first + (u * THREADS + (int)threadIdx.x) * 16;
-            if (bf) {
-                float x[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    x[2 * k] = low_bf16(r.v[u].x[k]) * coef;
-                    x[2 * k + 1] = high_bf16(r.v[u].x[k]) * coef;
-                }
-                if (obf) put<unsigned short, 8>(it.out, at / 2, it.n - at / 2, x);
-                else put<float, 8>(it.out, at / 2, it.n - at / 2, x);
-            } else {
-                float x[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(r.v[u].x[k]) * coef;
-                if (obf) put<unsigned short, 4>(it.out, at / 4, it.n - at / 4, x);
-                else put<float, 4>(it.out, at / 4, it.n - at / 4, x);
-            }
-        }
+        if (coef == 1.f && a.item[id].out == a.item[id].g) continue;
+        clip_chunk<THREADS>(a, id, c, coef, threadIdx.x);
     }
+}
+
+// A short list by one workgroup, whose sixteen waves take chunks of 4 KB: two rounds of them for the norm (8 tensors of 16 KB 5.1 us a call instead of 8.4 by two
+// launches; a third takes as long, waited for), one where it goes on to clip (4 of them 5.7 instead of 8.9; two rounds 8.3 for 9.0, and no sooner).
+constexpr int ALONE = 1024;
+constexpr int64_t alone_chunks(bool clip) { return (clip ? 1 : 2) * ALONE / 64; }
+template <bool CLIP> __global__ __launch_bounds__(ALONE) void norm_alone_kernel(const GradLaunch a, const NormArgs g) {
+    __shared__ double shared[ALONE / 64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const double scale = g.scale ? (double)*g.scale : 1.0;
+    const double sum = sum_workgroup<ALONE / 64>(sum_chunks<64, false>(a, wave, ALONE / 64, lane), shared);
+    const float coef = finish(g, scale, sum, threadIdx.x == 0);
+    if (CLIP)
+        for (unsigned c = wave; c < a.chunks; c += ALONE / 64) {
+            const int id = item_of(a, c);
+            if (coef != 1.f || a.item[id].out != a.item[id].g) clip_chunk<64>(a, id, c, coef, lane);
+        }
 }
 
 // The launches of a list: up to ITEMS tensors each, tensors longer than 32-bit counts reach in pieces.
@@ -238,7 +250,7 @@ constexpr int64_t PIECE = (int64_t)1 << 31;
 constexpr unsigned MOST_CHUNKS = 1u << 23;
 constexpr double CACHE_BYTES = 256e6;       // of the cache in front of the memory
 constexpr unsigned CLIP_WGS = 4096;         // (1024 to 8192 differ by 1 us for 25.6M gradients)
-template <typename F> int each_launch(int n, const kfac_grad_item *items, F launch) {
+template <typename F> int each_launch(int n, const kfac_grad_item *items, int64_t chunk, F launch) {
     GradLaunch a{};
     int64_t elements = 0, bytes = 0, written = 0;
     auto go = [&]() -> int {
@@ -252,7 +264,7 @@ template <typename F> int each_launch(int n, const kfac_grad_item *items, F laun
         const kfac_grad_item &t = items[i];
         const bool bf = t.grad_dtype == KFAC_BF16, obf = t.out_dtype == KFAC_BF16;
         for (int64_t at = 0; at < t.n; at += PIECE) {
-            const int64_t len = std::min(PIECE, t.n - at), per = CHUNK / (bf ? 2 : 4);
+            const int64_t len = std::min(PIECE, t.n - at), per = chunk / (bf ? 2 : 4);
             const unsigned mine = (unsigned)((len + per - 1) / per);
             if (a.n == ITEMS || a.chunks + mine > MOST_CHUNKS) KFAC_CHECK(go());
             a.gbf[a.n] = bf;
@@ -271,7 +283,7 @@ template <typename F> int each_launch(int n, const kfac_grad_item *items, F laun
 
 size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items) {
     size_t parts = 0;
-    (void)each_launch(n, items, [&](const GradLaunch &a, int64_t, int64_t, int64_t) -> int {
+    (void)each_launch(n, items, chunk_bytes<THREADS>(), [&](const GradLaunch &a, int64_t, int64_t, int64_t) -> int {
         parts += std::min<size_t>(a.chunks, MOST);
         return KFAC_OK;
     });
@@ -280,23 +292,24 @@ size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items) {
 
 int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef, bool clip) {
     if (kfac_grad_norm_ws_bytes_impl(n, items) > ctx->ws_bytes) return KFAC_EWORKSPACE;
+    NormArgs g{(double *)ctx->ws, 0, (double)max_norm, grad_scale, norm, coef};
     double whole = 0.0;
-    int64_t all = 0;                                      // chunks
+    int64_t shorts = 0;                                   // chunks of a wave
+    int tensors = 0;
     for (int i = 0; i < n; ++i) {
         const int64_t bytes = items[i].n * (items[i].grad_dtype == KFAC_BF16 ? 2 : 4);
         whole += (double)bytes;
-        all += (bytes + CHUNK - 1) / CHUNK;
+        shorts += (bytes + chunk_bytes<64>() - 1) / chunk_bytes<64>();
+        tensors += bytes > 0;
     }
-    NormArgs g{(double *)ctx->ws, 0, (double)max_norm, grad_scale, norm, coef};
-    bool alone = false;
-    KFAC_CHECK(each_launch(n, items, [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t) -> int {
-        if (!clip && g.n == 0 && a.chunks <= ALONE_CHUNKS && a.chunks == all) {
-            alone = true;
-            KfacProfScope prof(ctx, KC_NORM, 2.0 * (double)elements, (double)bytes);
-            hipLaunchKernelGGL(norm_alone_kernel, dim3(1), dim3(ALONE), 0, ctx->stream, a, g);
+    if (tensors > 0 && tensors <= ITEMS && shorts <= alone_chunks(clip))
+        return each_launch(n, items, chunk_bytes<64>(), [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t written) -> int {
+            KfacProfScope prof(ctx, KC_NORM, (clip ? 3.0 : 2.0) * (double)elements, (double)(bytes + (clip ? written : 0)));
+            hipLaunchKernelGGL((clip ? norm_alone_kernel<true> : norm_alone_kernel<false>), dim3(1), dim3(ALONE), 0, ctx->stream, a, g);
             KFAC_HIP_CHECK(hipGetLastError());
             return KFAC_OK;
-        }
+        });
+    KFAC_CHECK(each_launch(n, items, chunk_bytes<THREADS>(), [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t) -> int {
         const unsigned wgs = std::min<unsigned>(a.chunks, MOST);
         a.part = (double *)ctx->ws + g.n;
         g.n += (int)wgs;
@@ -305,7 +318,6 @@ int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *it
         KFAC_HIP_CHECK(hipGetLastError());
         return KFAC_OK;
     }));
-    if (alone) return KFAC_OK;
     if (!clip || g.n == 0) {
         KfacProfScope prof(ctx, KC_NORM, 0.0, 8.0 * g.n);
         hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(THREADS), 0, ctx->stream, g);
@@ -313,7 +325,7 @@ int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *it
         return KFAC_OK;
     }
     bool first = true;
-    return each_launch(n, items, [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t written) -> int {
+    return each_launch(n, items, chunk_bytes<THREADS>(), [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t written) -> int {
         KfacProfScope prof(ctx, KC_NORM, (double)elements, (double)(bytes + written));
         hipLaunchKernelGGL(clip_kernel, dim3(std::min<unsigned>(a.chunks, CLIP_WGS)), dim3(THREADS), 0, ctx->stream, a, g, first);
         KFAC_HIP_CHECK(hipGetLastError());
