@@ -797,8 +797,8 @@ int part_of(int T, int vectors, int lanes) {
 
 template <typename T, int N, int MODE> auto scatter_of(int lanes) {
     if constexpr (N == 1) return scatter_kernel<T, 1, 8, MODE>;
-    else return lanes == 8 ? scatter_kernel<T, N, 8, MODE> : lanes == 16 ? scatter_kernel<T, N, 16, MODE> : lanes == 32 ? scatter_kernel<T, N, 32, MODE> : lanes == 64 ? scatter_kernel<T, N, 64, MODE>
-              : lanes == 128 ? scatter_kernel<T, N, 128, MODE> : scatter_kernel<T, N, 256, MODE>;
+    else return lanes == 8 ? scatter_kernel<T, N, 8, MODE> : lanes == 16 ? scatter_kernel<T, N, 16, MODE> : lanes == 32 ? scatter_kernel<T, N, 32, MODE>
+              : lanes == 64 ? scatter_kernel<T, N, 64, MODE> : lanes == 128 ? scatter_kernel<T, N, 128, MODE> : scatter_kernel<T, N, 256, MODE>;
 }
 template <typename T, int N, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, double bytes) {
     const int vectors = (g.d + N - 1) / N, lanes = lanes_of(vectors, 1), tok = THREADS / lanes;
@@ -826,8 +826,8 @@ template <typename T, int N, int KB, bool PAST> auto combine_of(int lanes, bool 
     if constexpr (N == 1) return grad ? combine_grad_kernel<T, 1, 8, KB, PAST> : combine_kernel<T, 1, 8, KB, PAST>;
     else if (grad) return lanes == 8 ? combine_grad_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_grad_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_grad_kernel<T, N, 32, KB, PAST>
                    : lanes == 64 ? combine_grad_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_grad_kernel<T, N, 128, KB, PAST> : combine_grad_kernel<T, N, 256, KB, PAST>;
-    else return lanes == 8 ? combine_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_kernel<T, N, 32, KB, PAST> : lanes == 64 ? combine_kernel<T, N, 64, KB, PAST>
-              : lanes == 128 ? combine_kernel<T, N, 128, KB, PAST> : combine_kernel<T, N, 256, KB, PAST>;
+    else return lanes == 8 ? combine_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_kernel<T, N, 32, KB, PAST>
+              : lanes == 64 ? combine_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_kernel<T, N, 128, KB, PAST> : combine_kernel<T, N, 256, KB, PAST>;
 }
 template <typename T, int N, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
     const bool grad = g.dw != nullptr;

@@ -194,6 +194,7 @@ class ExpertRunner:
 
     The rows of x and g are sorted by expert, offsets (int32 [experts + 1], on the GPU) say where each one's begin.  Parameters are kept in fp32 with their
     bias as last column; bf16 layers multiply with a bf16 copy of them that the optimizer step writes.  seed: of the rounding of an 8-bit state.
+    more_workspace: bytes that the context's workspace has at least, for calls besides this layer's.
     """
     # At step t a gradient as large as the average moves sqrt(v) by 1 / (2 t) (beta2 near 1), which up to the eighth is half the distance of two
     # codes at least: until then an 8-bit state is rounded to nearest, which is off by less; from then on by the seed, or it would stand still.
@@ -320,9 +321,12 @@ class RoutedExpertRunner(ExpertRunner):
         if self.router_weight is not self.router:
             self.router_weight.copy_(self.router)
 
-    def forward(self, x, add=None):
-        """[tokens, d_out]: add (or zero) plus the weighted results of each token's experts."""
+    def forward(self, x, add=None, masked=None):
+        """[tokens, d_out]: add (or zero) plus the weighted results of each token's experts.  masked: truth values [tokens, 1] (padding) or [tokens or 1, experts]
+        (experts out of use) of what is not to be chosen; a token without a choice gets no result, and no gradient but what was added passes on."""
         K.kfac_experts_forward(self.ctx, x, self.router_weight, self.all, self.logits)
+        if masked is not None:
+            self.logits.masked_fill_(masked, float("-inf"))
         K.kfac_experts_route(self.ctx, self.logits, self.ids, self.weights, normalize=self.normalize)
         K.kfac_experts_dispatch(self.ctx, self.ids, x, self.offsets, self.row, self.xs)
         super().forward(self.xs, self.offsets)

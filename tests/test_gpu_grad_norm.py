@@ -46,7 +46,7 @@ def norm_of(grads, scale=1.0):
 
 F32, BF16 = torch.float32, torch.bfloat16
 LISTS = [([1], [F32]), ([7], [BF16]), ([4096], [F32]), ([4097, 8191], [BF16]), ([0, 5, 0, 1], [F32]), ([8192, 8193, 3], [F32, BF16]), ([100000, 17, 300001], [F32, BF16]),
-         ([33] * 250, [F32, BF16, BF16]), ([1024] * 16, [F32]), ([1025] * 8 + [7], [F32]), ([2048] * 16 + [1, 0] * 8, [BF16, F32]), ([100] * 32, [F32, BF16]), ([1 << 22, 12345], [BF16]), ([20 << 20], [F32])]
+         ([33] * 250, [F32, BF16, BF16]), ([1024] * 16, [F32]), ([1025] * 8 + [7], [F32]), ([2048] * 16 + [1, 0] * 8, [BF16, F32]), ([100] * 32, [F32, BF16]), ([50000] * 150, [F32]), ([1 << 22, 12345], [BF16]), ([20 << 20], [F32])]
 
 
 @pytest.mark.parametrize("start", [0, 1])

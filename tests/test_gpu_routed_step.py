@@ -99,6 +99,32 @@ def test_accumulated_batches():
     run.close()
 
 
+def test_padding_and_experts_out_of_use():
+    """Padded tokens get what is added and no gradients; an expert out of use no rows; the others are those of a batch without either."""
+    T, E, live = 60, 5, 41
+    gen = torch.Generator().manual_seed(3)
+    W, Wr = torch.randn(E, 16, 25, generator=gen) * 0.2, torch.randn(1, E, 24, generator=gen) * 0.2
+    x, g, add = torch.randn(T, 24, generator=gen), torch.randn(T, 16, generator=gen), torch.randn(T, 16, generator=gen)
+    masked = torch.zeros(T, E, dtype=torch.bool)
+    masked[live:] = True
+    masked[:, 2] = True
+    results = []
+    for n in (T, live):
+        run = RoutedExpertRunner(E, n, 2, 24, 16, bf16=False)
+        run.load(W, Wr)
+        dev = lambda t: t[:n].to(run.dev)  # noqa: E731
+        y = run.forward(dev(x), dev(add), masked=dev(masked))
+        if n == T:
+            assert torch.equal(y[live:], dev(add)[live:]) and (run.ids[live:] == -1).all() and (run.row[live:] == -1).all()
+        assert int(run.offsets[2]) == int(run.offsets[3]) and int(run.offsets[-1]) == 2 * live
+        dx = run.backward(dev(x), dev(g))
+        assert (dx[live:] == 0).all() and not run.grad[2].any() and not run.router_grad[0, 2].any()
+        results.append([t.clone() for t in (y[:live], dx[:live], run.grad, run.router_grad)])
+        run.close()
+    for a, b in zip(*results):                               # (sums over more rows may go in other parts)
+        assert relfro(a.double().cpu(), b.double().cpu()) <= 1e-6
+
+
 def test_clip_of_other_runners():
     """The gradients of a network in place, and the coefficient of a layer of experts."""
     run = KfacRunner(S.workload("resnet32_cifar"), n_updates=1, batch=2, layers=[0, 3, 33])
