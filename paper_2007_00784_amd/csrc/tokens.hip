@@ -548,7 +548,7 @@ struct MoveArgs {
 // Where a workgroup gets the rows of its slots from: they are given; or the runs' counts and first rows are; or there are so few slots that
 // every workgroup counts those in front of its own, and a launch needs no other before it.
 enum { GIVEN = 0, RANKED = 1, COUNTED = 2 };
-constexpr int FEW_SLOTS = 1024;
+constexpr int FEW_SLOTS = 2048;      // (512 x 4 tokens of 4096 bf16 8.2 us in one launch, 9.7 to 10.3 in two; 4096 slots: as long in one)
 
 // The offsets from the counts of all slots, by the launch's last workgroup.
 __device__ inline void count_offsets(const SortArgs &g, const int *expert /* LDS */, int *count /* LDS, [E] */, int *waves) {
@@ -796,12 +796,14 @@ int part_of(int T, int vectors, int lanes) {
 }
 
 template <typename T, int N, int MODE> auto scatter_of(int lanes) {
-    if constexpr (N == 1) return scatter_kernel<T, 1, 8, MODE>;
+    if constexpr (MODE == COUNTED) return scatter_kernel<T, N, THREADS, MODE>;
+    else if constexpr (N == 1) return scatter_kernel<T, 1, 8, MODE>;
     else return lanes == 8 ? scatter_kernel<T, N, 8, MODE> : lanes == 16 ? scatter_kernel<T, N, 16, MODE> : lanes == 32 ? scatter_kernel<T, N, 32, MODE>
               : lanes == 64 ? scatter_kernel<T, N, 64, MODE> : lanes == 128 ? scatter_kernel<T, N, 128, MODE> : scatter_kernel<T, N, 256, MODE>;
 }
 template <typename T, int N, int MODE> int launch_scatter(kfac_ctx *ctx, MoveArgs g, double bytes) {
-    const int vectors = (g.d + N - 1) / N, lanes = lanes_of(vectors, 1), tok = THREADS / lanes;
+    // (counting takes longer than copying, so a workgroup has the slots of one token: 256 x 4 of 512 bf16 4.7 us, with four tokens 8.6)
+    const int vectors = (g.d + N - 1) / N, lanes = MODE == COUNTED ? THREADS : lanes_of(vectors, 1), tok = THREADS / lanes;
     g.part = MODE == RANKED ? 1 << 30 : part_of(g.T, vectors, lanes);     // (a second workgroup of a slot would find its rank replaced)
     const unsigned parts = MODE == RANKED ? 1 : std::max(1, (vectors + g.part - 1) / g.part);     // (no columns: the order of the slots alone)
     const size_t lds = 4 * ((size_t)tok * g.k + (MODE == COUNTED ? g.sort.S + g.sort.E : 0));

@@ -219,7 +219,7 @@ def random_ids(T, k, E, gen, nobody=True):
     return ids
 
 
-SORTS = [(1, 1, 1), (1, 64, 4), (8, 2, 8), (16, 64, 3), (17, 64, 4096), (512, 2, 300), (1024, 1, 4096), (1025, 1, 5), (513, 2, 64), (700, 8, 1), (3000, 7, 33), (1024, 4, 512), (4096, 1, 1), (4097, 1, 77), (300, 8, 513), (43, 64, 100), (4100, 64, 4096), (20000, 4, 1025), (9000, 64, 512), (70000, 8, 513), (5000, 8, 2049), (66000, 1, 130),
+SORTS = [(1, 1, 1), (1, 64, 4), (8, 2, 8), (16, 64, 3), (17, 64, 4096), (512, 2, 300), (1024, 1, 4096), (1025, 1, 5), (1024, 2, 300), (2048, 1, 4096), (2049, 1, 4096), (683, 3, 40), (2047, 1, 3), (513, 2, 64), (700, 8, 1), (3000, 7, 33), (1024, 4, 512), (4096, 1, 1), (4097, 1, 77), (300, 8, 513), (43, 64, 100), (4100, 64, 4096), (20000, 4, 1025), (9000, 64, 512), (70000, 8, 513), (5000, 8, 2049), (66000, 1, 130),
          (65536, 8, 128), (9, 3, 2)]
 
 

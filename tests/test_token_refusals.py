@@ -99,7 +99,7 @@ def test_workspace_of_an_order():
     f = K.kfac_experts_dispatch_workspace_bytes
     assert f(-1, 2, 4) == f(8, 0, 4) == f(8, 65, 4) == f(8, 2, 0) == f(8, 2, 4097) == f(1 << 27, 2, 4) == f((1 << 32) + 8, 2, 4) == 0
     assert f(512, 2, 64) == f(2048, 2, 512) == 0                                              # few slots need none
-    for T, k, e in ((4097, 1, 64), (600, 2, 513), (16384, 4, 64), (65536, 8, 128), (65536, 8, 4096), ((1 << 25) - 1, 8, 4096), ((1 << 28) - 1, 1, 1)):
+    for T, k, e in ((4097, 1, 64), (1100, 2, 513), (16384, 4, 64), (65536, 8, 128), (65536, 8, 4096), ((1 << 25) - 1, 8, 4096), ((1 << 28) - 1, 1, 1)):
         assert 0 < f(T, k, e) <= 4 << 20 and f(T, k, e) % 256 == 0
 
 
