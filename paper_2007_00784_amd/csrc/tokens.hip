@@ -649,7 +649,7 @@ template <typename T, int N, int LANES, int MODE> __global__ __launch_bounds__(T
 
 // Rows and weights of a workgroup's slots in LDS: a row outside the matrix is -1.
 __device__ inline void slots_of(const MoveArgs &g, int64_t t0, int mine, int *rows, float *w) {
-    for (int i = threadIdx.x; i < mine; i += THREADS) {
+    for (int i = threadIdx.x; i < mine; i += blockDim.x) {
         const int row = g.rows[t0 * g.k + i];
         rows[i] = (unsigned)row < (unsigned)g.R ? row : -1;
         w[i] = g.w ? g.w[t0 * g.k + i] : 1.f;
@@ -715,10 +715,10 @@ template <typename T, int N, int LANES, int KB, bool PAST> __global__ __launch_b
 
 // dYs[rows[s]] = w[s] dY[t] and dw[s] = <dY[t], Ys[rows[s]]>, KB slots of a token at a time.  A lane's share of a product is summed in fp32 in
 // the order of the columns, the lanes' then by halves: the same order from run to run.
-template <typename T, int N, int LANES, int KB, bool PAST> __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const MoveArgs g) {
-    constexpr int TOK = THREADS / LANES, WAVES = LANES / 64;
+template <typename T, int N, int LANES, int KB, bool PAST> __global__ __launch_bounds__(std::max(THREADS, LANES)) void combine_grad_kernel(const MoveArgs g) {
+    constexpr int BLOCK = std::max(THREADS, LANES), TOK = BLOCK / LANES, WAVES = LANES / 64;
     extern __shared__ int shared[];
-    __shared__ float partial[THREADS / 64][KB];
+    __shared__ float partial[BLOCK / 64][KB];
     float *const weights = (float *)(shared + TOK * g.k);
     const int64_t t0 = g.first + (int64_t)blockIdx.x * TOK, t = t0 + threadIdx.x / LANES;
     const bool there = t < g.T;
@@ -824,16 +824,24 @@ template <typename T, int MODE> int launch_scatter(kfac_ctx *ctx, const MoveArgs
     return g.d < N ? launch_scatter<T, 1, MODE>(ctx, g, bytes) : launch_scatter<T, N, MODE>(ctx, g, bytes);
 }
 
+// A token's products are one workgroup's, so the gradient of a few tokens of long rows leaves most of the card idle: there a row is shared by more lanes.
+// bf16, 1024 lanes against 256: 2 x 2 rows of 65536 11.4 us and 27.6, 14 x 8 of 3272 fp32 6.6 and 11.5, 1 x 8 of 4096 7.0 and 9.7, 256 x 8 of 4096 10 and 13.7;
+// 512 x 8 of 4096 17.2 and 16.3, 2048 x 4 of 4096 35 and 24.
+constexpr int FEW_TOKENS = 256, FEW_LANES = 1024;
 template <typename T, int N, int KB, bool PAST> auto combine_of(int lanes, bool grad) {
     if constexpr (N == 1) return grad ? combine_grad_kernel<T, 1, 8, KB, PAST> : combine_kernel<T, 1, 8, KB, PAST>;
     else if (grad) return lanes == 8 ? combine_grad_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_grad_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_grad_kernel<T, N, 32, KB, PAST>
-                   : lanes == 64 ? combine_grad_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_grad_kernel<T, N, 128, KB, PAST> : combine_grad_kernel<T, N, 256, KB, PAST>;
+                   : lanes == 64 ? combine_grad_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_grad_kernel<T, N, 128, KB, PAST>
+                   : lanes == 256 ? combine_grad_kernel<T, N, 256, KB, PAST> : combine_grad_kernel<T, N, FEW_LANES, KB, PAST>;
     else return lanes == 8 ? combine_kernel<T, N, 8, KB, PAST> : lanes == 16 ? combine_kernel<T, N, 16, KB, PAST> : lanes == 32 ? combine_kernel<T, N, 32, KB, PAST>
               : lanes == 64 ? combine_kernel<T, N, 64, KB, PAST> : lanes == 128 ? combine_kernel<T, N, 128, KB, PAST> : combine_kernel<T, N, 256, KB, PAST>;
 }
 template <typename T, int N, int KB, bool PAST> int launch_combine(kfac_ctx *ctx, MoveArgs g, double flops, double bytes) {
     const bool grad = g.dw != nullptr;
-    const int vectors = (g.d + N - 1) / N, lanes = lanes_of(vectors, grad ? 1 : 2), tok = THREADS / lanes;
+    const int vectors = (g.d + N - 1) / N;
+    int lanes = lanes_of(vectors, grad ? 1 : 2);
+    if (grad && g.T <= FEW_TOKENS && vectors > THREADS) lanes = FEW_LANES;
+    const int threads = std::max(lanes, THREADS), tok = threads / lanes;
     const size_t lds = 8 * (size_t)tok * g.k;
     g.part = grad ? vectors : part_of(g.T, vectors, lanes);
     const unsigned parts = (vectors + g.part - 1) / g.part;
@@ -841,7 +849,7 @@ template <typename T, int N, int KB, bool PAST> int launch_combine(kfac_ctx *ctx
     KfacProfScope prof(ctx, KC_TOKENS, flops, bytes);
     return each_launch(g.T, tok, [&](int first, unsigned wgs) {
         g.first = first;
-        hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(THREADS), lds, ctx->stream, g);
+        hipLaunchKernelGGL(kernel, dim3(wgs, parts), dim3(threads), lds, ctx->stream, g);
     });
 }
 // The experts' rows are read past the caches where they are too long to be there still.

@@ -260,7 +260,8 @@ def test_order_of_nothing(ctx):
 
 # T, k, E, d: few slots and many, rows of one lane, a wave's, a workgroup's and longer ones, cut among workgroups or not
 MOVES = [(1, 1, 1, 1), (1, 2, 4, 65536), (3, 2, 8, 7), (8, 2, 8, 2048), (40, 3, 5, 128), (33, 4, 16, 129), (200, 2, 10, 577), (90, 8, 30, 1000), (64, 16, 20, 2049),
-         (600, 2, 64, 9), (1030, 1, 3, 640), (400, 6, 100, 1031), (300, 4, 7, 5000), (2100, 3, 65, 64), (1360, 3, 6, 33), (20, 64, 64, 260), (17, 64, 4096, 33)]
+         (600, 2, 64, 9), (1030, 1, 3, 640), (400, 6, 100, 1031), (300, 4, 7, 5000), (2100, 3, 65, 64), (1360, 3, 6, 33), (20, 64, 64, 260), (17, 64, 4096, 33),
+         (3, 7, 5, 16391), (256, 5, 9, 4099), (257, 2, 4, 4099)]
 
 
 @pytest.mark.parametrize("bf16", [True, False])
