@@ -314,6 +314,7 @@ class RoutedExpertRunner(ExpertRunner):
         self._adamw = K.adamw_items([self._item(self.param, self.grad, self.state, self.weight),
                                      self._item(self.router, self.router_grad, self.router_state, self.router_weight)])
         self._grads = K.grad_items([self.grad, self.router_grad])
+        self._masked = False                                 # whether the last forward() was given a mask
 
     def load(self, param, router):
         super().load(param)
@@ -323,9 +324,11 @@ class RoutedExpertRunner(ExpertRunner):
 
     def forward(self, x, add=None, masked=None):
         """[tokens, d_out]: add (or zero) plus the weighted results of each token's experts.  masked: truth values [tokens, 1] (padding) or [tokens or 1, experts]
-        (experts out of use) of what is not to be chosen; a token without a choice gets no result, and no gradient but what was added passes on."""
+        (experts out of use) of what is not to be chosen; a token without a choice gets no result, and no gradient but what was added passes on, and whatever stands in
+        a masked one's x and g (NaN among it) reaches nothing."""
         K.kfac_experts_forward(self.ctx, x, self.router_weight, self.all, self.logits)
-        if masked is not None:
+        self._masked = masked is not None
+        if self._masked:
             self.logits.masked_fill_(masked, float("-inf"))
         K.kfac_experts_route(self.ctx, self.logits, self.ids, self.weights, normalize=self.normalize)
         K.kfac_experts_dispatch(self.ctx, self.ids, x, self.offsets, self.row, self.xs)
@@ -342,6 +345,8 @@ class RoutedExpertRunner(ExpertRunner):
         super().backward(self.xs, self.gs, self.offsets, accumulate=accumulate)
         K.kfac_experts_route_grad(self.ctx, self.logits, self.ids, self.dweights, self.dlogits, normalize=self.normalize)
         K.kfac_experts_input_grad(self.ctx, self.dlogits, self.router_weight, self.all, self.dtokens)
+        if self._masked:                                     # (the logits of a padded token have no gradient, but zero times the NaN that may stand there is NaN)
+            x = x.masked_fill(self.ids[:, :1] < 0, 0.0)
         K.kfac_experts_weight_grad(self.ctx, self.dlogits, x, self.all, self.router_grad, accumulate=accumulate)
         K.kfac_experts_combine(self.ctx, self.dx, self.row, None, self.dtokens, add=self.dtokens)
         return self.dtokens

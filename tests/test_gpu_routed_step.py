@@ -125,6 +125,41 @@ def test_padding_and_experts_out_of_use():
         assert relfro(a.double().cpu(), b.double().cpu()) <= 1e-6
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("whole", [True, False])
+def test_padding_that_holds_anything(whole, bf16):
+    """What stands in padded tokens, NaN and infinities among it, and in their outputs' gradients reaches nothing: the same bits as with zeros there."""
+    T, E, k, live = 70, 5, 2, 53
+    gen = torch.Generator().manual_seed(11)
+    W, Wr = torch.randn(E, 16, 25, generator=gen) * 0.2, torch.randn(1, E, 24, generator=gen) * 0.2
+    batches = [(torch.randn(T, 24, generator=gen), torch.randn(T, 16, generator=gen)) for _ in range(2)]
+    masked = torch.zeros(T, 1 if whole else E, dtype=torch.bool)
+    masked[live:] = True
+    masked[7] = True
+    pad = masked[:, 0].clone()
+    if not whole:
+        masked[:, 3] = True
+    results = []
+    for odd in (torch.tensor([0.0]), torch.tensor([math.nan, math.inf, -math.inf, 1e30])):
+        run = RoutedExpertRunner(E, T, k, 24, 16, bf16=bf16)
+        run.load(W, Wr)
+        out = []
+        for i, batch in enumerate(batches):
+            x, g = (t.clone() for t in batch)
+            for t in (x, g):
+                t[pad] = odd[torch.arange(int(pad.sum()) * t.shape[1]) % odd.numel()].view(-1, t.shape[1])
+            x, g = x.to(run.dt).to(run.dev), g.to(run.dt).to(run.dev)
+            kept = x.clone()
+            out.append(run.forward(x, masked=masked.to(run.dev)).clone())
+            out.append(run.backward(x, g, accumulate=i > 0, gather=i > 0).clone())
+            assert torch.equal(x.view(torch.int16), kept.view(torch.int16))
+        run.update_factors(0.5)
+        results.append(out + [t.clone() for t in (run.grad, run.router_grad, run.A, run.G)])
+        run.close()
+    for a, b in zip(*results):
+        assert a.isfinite().all() and torch.equal(a, b)
+
+
 def test_clip_of_other_runners():
     """The gradients of a network in place, and the coefficient of a layer of experts."""
     run = KfacRunner(S.workload("resnet32_cifar"), n_updates=1, batch=2, layers=[0, 3, 33])
