@@ -2,12 +2,33 @@
 
 Holds device buffers and call order only: every arithmetic step is a library call.  Used by the
 benchmark and by the full-size parity tests.
+
+Everything a runner does goes to the stream that was the current one when it was made; inputs from another stream and
+results used on one are the caller's to order.
 """
+import contextlib
+
 import numpy as np
 import torch
 
 from . import kfac as K
 from . import synthetic as S
+
+
+@contextlib.contextmanager
+def own_stream(run, *inputs):
+    """torch's operations between the library's calls of a runner go where those do, whatever the caller's stream is, and behind what that stream holds by now
+    (a mask that was just made, say)."""
+    now = torch.cuda.current_stream(run.dev)
+    if now == run.stream:
+        yield
+        return
+    run.stream.wait_stream(now)
+    for t in inputs:
+        if t.is_cuda:
+            t.record_stream(run.stream)
+    with torch.cuda.stream(run.stream):
+        yield
 
 
 class KfacRunner:
@@ -61,6 +82,7 @@ class KfacRunner:
         self.ws = torch.empty(need + 4096, dtype=torch.uint8, device=self.dev)
         self.stream = torch.cuda.current_stream(self.dev)
         self.ctx = K.kfac_create(self.dev.index or 0, self.stream.cuda_stream, self.ws)
+        self.norm, self.coef = torch.zeros(1, **f32), torch.zeros(1, **f32)
         self.eig_info = None
         self._marshalled = {}    # item arrays of the batched calls, marshalled once per distinct argument set
 
@@ -121,7 +143,8 @@ class KfacRunner:
     def restore_gradients(self):
         """Fresh gradients for the next in-place preconditioning (one device copy of the flat master buffer): what
         the backward pass of a training iteration delivers."""
-        self.grad_flat.copy_(self.gradw_master_flat)
+        with own_stream(self):
+            self.grad_flat.copy_(self.gradw_master_flat)
 
     def precondition(self, damping=None, kappa=None, lr=None, split_f16=None, restore=True):
         """In-place preconditioning of the gradients (restored from their masters first unless restore=False); with
@@ -138,7 +161,8 @@ class KfacRunner:
         if kappa is None:
             K.kfac_precondition_batched(self.ctx, items=self._marshalled[key])
         else:
-            self.nu = torch.zeros(1, dtype=torch.float32, device=self.dev)
+            with own_stream(self):
+                self.nu = torch.zeros(1, dtype=torch.float32, device=self.dev)
             K.kfac_precondition_batched_scaled(self.ctx, kappa=kappa, lr=lr, nu=self.nu, items=self._marshalled[key])
 
     def clip(self, max_norm):
@@ -146,7 +170,6 @@ class KfacRunner:
         and self.coef."""
         if "clip" not in self._marshalled:
             self._marshalled["clip"] = K.grad_items(self.grad, self.grad)
-            self.norm, self.coef = (torch.zeros(1, dtype=torch.float32, device=self.dev) for _ in range(2))
         K.kfac_clip_grads_batched(self.ctx, self._marshalled["clip"], max_norm, self.norm, self.coef)
 
     # ---- the explicit-inverse method (Sec. II-C, Eq. (kfac-damped)): the paper's other way to the same step ----
@@ -154,8 +177,9 @@ class KfacRunner:
         """(A + gamma I)^-1 and (G + gamma I)^-1 of every layer by blocked Cholesky (buffers allocated on first use)."""
         gamma = self.wl.damping if damping is None else damping
         if not hasattr(self, "Ainv"):
-            self.Ainv = [torch.empty_like(a) for a in self.A]
-            self.Ginv = [torch.empty_like(g) for g in self.G]
+            with own_stream(self):
+                self.Ainv = [torch.empty_like(a) for a in self.A]
+                self.Ginv = [torch.empty_like(g) for g in self.G]
         K.kfac_invert_factors(self.ctx, self.A + self.G, gamma, self.Ainv + self.Ginv)
 
     def precondition_inverse(self, restore=True):
@@ -250,9 +274,10 @@ class ExpertRunner:
 
     def load(self, param):
         """The parameters [experts, d_out, d_in + bias], and the weights that the products read."""
-        self.param.copy_(param)
-        if self.weight is not self.param:
-            self.weight.copy_(self.param)
+        with own_stream(self, param):
+            self.param.copy_(param)
+            if self.weight is not self.param:
+                self.weight.copy_(self.param)
 
     def forward(self, x, offsets):
         K.kfac_experts_forward(self.ctx, x, self.weight, offsets, self.y, append_ones=self.bias)
@@ -318,9 +343,10 @@ class RoutedExpertRunner(ExpertRunner):
 
     def load(self, param, router):
         super().load(param)
-        self.router.copy_(router)
-        if self.router_weight is not self.router:
-            self.router_weight.copy_(self.router)
+        with own_stream(self, router):
+            self.router.copy_(router)
+            if self.router_weight is not self.router:
+                self.router_weight.copy_(self.router)
 
     def forward(self, x, add=None, masked=None):
         """[tokens, d_out]: add (or zero) plus the weighted results of each token's experts.  masked: truth values [tokens, 1] (padding) or [tokens or 1, experts]
@@ -329,7 +355,8 @@ class RoutedExpertRunner(ExpertRunner):
         K.kfac_experts_forward(self.ctx, x, self.router_weight, self.all, self.logits)
         self._masked = masked is not None
         if self._masked:
-            self.logits.masked_fill_(masked, float("-inf"))
+            with own_stream(self, masked):
+                self.logits.masked_fill_(masked, float("-inf"))
         K.kfac_experts_route(self.ctx, self.logits, self.ids, self.weights, normalize=self.normalize)
         K.kfac_experts_dispatch(self.ctx, self.ids, x, self.offsets, self.row, self.xs)
         super().forward(self.xs, self.offsets)
@@ -346,7 +373,8 @@ class RoutedExpertRunner(ExpertRunner):
         K.kfac_experts_route_grad(self.ctx, self.logits, self.ids, self.dweights, self.dlogits, normalize=self.normalize)
         K.kfac_experts_input_grad(self.ctx, self.dlogits, self.router_weight, self.all, self.dtokens)
         if self._masked:                                     # (the logits of a padded token have no gradient, but zero times the NaN that may stand there is NaN)
-            x = x.masked_fill(self.ids[:, :1] < 0, 0.0)
+            with own_stream(self, x):
+                x = x.masked_fill(self.ids[:, :1] < 0, 0.0)
         K.kfac_experts_weight_grad(self.ctx, self.dlogits, x, self.all, self.router_grad, accumulate=accumulate)
         K.kfac_experts_combine(self.ctx, self.dx, self.row, None, self.dtokens, add=self.dtokens)
         return self.dtokens

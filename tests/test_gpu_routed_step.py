@@ -178,3 +178,66 @@ def test_clip_of_other_runners():
     n = math.sqrt(run.grad.numel() * 4.0)
     assert abs(float(run.clip(n / 4, grad_scale=torch.full((1,), 0.5, device=run.dev))) - 0.25) <= 1e-6 and abs(float(run.norm) - n / 2) <= 1e-6 * n
     run.close()
+
+
+def busy(n=12):
+    """Some milliseconds of work for the current stream."""
+    a = torch.zeros(8192, 8192, dtype=torch.bfloat16, device="cuda:0")
+    for _ in range(n):
+        a = a @ a
+
+
+@pytest.mark.parametrize("before", ["runner", "caller", "neither"])
+@pytest.mark.parametrize("same", [True, False])
+def test_on_its_own_stream(same, before):
+    """A runner made on a side stream and called from it, or from another one, either of them busy: parameters, masks and padding take effect in the order of the calls."""
+    T, E, k = 300, 6, 2
+    gen = torch.Generator().manual_seed(5)
+    params = [(torch.randn(E, 16, 25, generator=gen) * 0.2, torch.randn(1, E, 24, generator=gen) * 0.2) for _ in range(2)]
+    x, g = torch.randn(T, 24, generator=gen).cuda(), torch.randn(T, 16, generator=gen).cuda()
+    x[250:] = math.nan
+    lengths = torch.tensor([250], device="cuda:0")
+    out = torch.tensor([[False, True, False, False, False, False]], device="cuda:0")
+    torch.cuda.synchronize()
+    results = []
+    for side in (None, torch.cuda.Stream()):
+        with torch.cuda.stream(side or torch.cuda.current_stream()):
+            run = RoutedExpertRunner(E, T, k, 24, 16, bf16=True)
+        xs, gs = x.to(run.dt), g.to(run.dt)
+        device = [[t.cuda() for t in p] for p in params]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side if side is not None and same else torch.cuda.current_stream()):
+            for p in device:
+                if side is not None and before != "neither":
+                    with torch.cuda.stream(side if before == "runner" else torch.cuda.current_stream()):
+                        busy()
+                run.load(*p)
+                masked = (torch.arange(T, device="cuda:0") >= lengths)[:, None] | out
+                run.forward(xs, masked=masked)
+                del masked
+                torch.ones(T, E, dtype=torch.bool, device="cuda:0")       # (takes the memory of the mask)
+                run.backward(xs, gs)
+        torch.cuda.synchronize()
+        assert (run.ids[250:] == -1).all() and not (run.ids == 1).any() and int(run.offsets[-1]) == 250 * k
+        results.append([t.clone() for t in (run.out, run.dtokens, run.grad, run.router_grad)])
+        run.close()
+    for a, b in zip(*results):
+        assert a.isfinite().all() and torch.equal(a, b)
+
+
+def test_clip_from_a_busy_stream():
+    """Gradients are restored and clipped for the first time from a busy stream that is not the runner's: none of it comes behind what it has to precede."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        run = KfacRunner(S.workload("resnet32_cifar"), n_updates=1, batch=2, layers=[0, 3, 33])
+    torch.cuda.synchronize()
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in run.gradw_master))
+    torch.cuda.synchronize()
+    busy()
+    run.restore_gradients()
+    run.clip(want / 2)
+    torch.cuda.synchronize()
+    assert abs(float(run.norm) - want) <= 1e-6 * want and abs(float(run.coef) - 0.5) <= 1e-6
+    for g, r in zip(run.grad, run.gradw_master):
+        assert relfro(g.double().cpu(), r.double().cpu() / 2) <= 1e-6
+    run.close()
