@@ -373,7 +373,8 @@ typedef struct {
     int64_t n;               /* may be 0                                                                   */
 } kfac_grad_item;
 /*   max_norm : > 0; infinite: coef is s.   norm, coef : DEVICE pointers to one float each, written; coef may be NULL
- * Workspace: kfac_grad_norm_workspace_bytes() (8 KB for each 100 tensors at most).  */
+ * Workspace: kfac_grad_norm_workspace_bytes() (8 KB for each 100 tensors at most).  Up to 100 tensors with together 32 runs of 4 KB (16 to clip; each tensor's
+ * last one may be shorter) are one workgroup's and need none.  */
 int kfac_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items /* host */, float max_norm, const float *grad_scale /* device */, float *norm, float *coef);
 size_t kfac_grad_norm_workspace_bytes(int n, const kfac_grad_item *items /* host; no pointer is looked at */);
 

@@ -291,7 +291,6 @@ size_t kfac_grad_norm_ws_bytes_impl(int n, const kfac_grad_item *items) {
 }
 
 int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *items, float max_norm, const float *grad_scale, float *norm, float *coef, bool clip) {
-    if (kfac_grad_norm_ws_bytes_impl(n, items) > ctx->ws_bytes) return KFAC_EWORKSPACE;
     NormArgs g{(double *)ctx->ws, 0, (double)max_norm, grad_scale, norm, coef};
     double whole = 0.0;
     int64_t shorts = 0;                                   // chunks of a wave
@@ -309,6 +308,7 @@ int kfac_launch_grad_norm_batched(kfac_ctx *ctx, int n, const kfac_grad_item *it
             KFAC_HIP_CHECK(hipGetLastError());
             return KFAC_OK;
         });
+    if (kfac_grad_norm_ws_bytes_impl(n, items) > ctx->ws_bytes) return KFAC_EWORKSPACE;
     KFAC_CHECK(each_launch(n, items, chunk_bytes<THREADS>(), [&](GradLaunch &a, int64_t elements, int64_t bytes, int64_t) -> int {
         const unsigned wgs = std::min<unsigned>(a.chunks, MOST);
         a.part = (double *)ctx->ws + g.n;

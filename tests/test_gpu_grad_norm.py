@@ -146,6 +146,33 @@ def test_workspace(ctx):
             small.close()
 
 
+def test_short_lists_without_workspace():
+    """One workgroup does a short list and touches no workspace: a context without any suffices, for up to 128 KB of gradients, and 64 KB to clip."""
+    c = Ctx(256)
+    K.kfac_destroy(c.h)
+    c.h = K.kfac_create(0, c.stream.cuda_stream, None)
+    try:
+        norm, coef = one(), one()
+        for sizes, dts in (([5], [F32]), ([0, 3, 0], [BF16]), ([1024] * 32, [F32]), ([2048] * 32, [BF16]), ([300] * 20, [F32, BF16])):
+            grads = tensors(sizes, dts, len(sizes))
+            want = norm_of(grads)
+            K.kfac_grad_norm_batched(c.h, grads, norm, max_norm=want / 2, coef=coef)
+            assert abs(float(norm) - want) <= 2 * U * want and abs(float(coef) - 0.5) <= 2 * U
+        for sizes, dts in (([5], [F32]), ([1024] * 16, [F32]), ([2048] * 16, [BF16])):
+            grads = tensors(sizes, dts, len(sizes))
+            want = [g.double() * 0.5 for g in grads]
+            K.kfac_clip_grads_batched(c.h, grads, norm_of(grads) / 2, norm, coef)
+            for g, w in zip(grads, want):
+                assert ((g.double() - w).abs() <= (3 * U + torch.finfo(g.dtype).eps / 2) * w.abs() + LEAST[g.dtype]).all()
+        for sizes, clip in (([1024] * 33, False), ([1024] * 17, True)):
+            grads = tensors(sizes, [F32], 1)
+            with pytest.raises(K.KfacError) as e:
+                K.kfac_clip_grads_batched(c.h, grads, 1.0, norm, coef) if clip else K.kfac_grad_norm_batched(c.h, grads, norm)
+            assert e.value.code == K.KFAC_EWORKSPACE
+    finally:
+        c.close()
+
+
 def test_same_bits_and_captured(ctx):
     """Repeated calls give the same bits; a captured clip takes each replay's gradients and scale; the optimizer reads the coefficient."""
     sizes = [70001, 13, 5000]
