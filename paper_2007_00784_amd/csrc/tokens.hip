@@ -974,6 +974,7 @@ int kfac_launch_experts_dispatch(kfac_ctx *ctx, const kfac_slot_desc *d, int exp
     }
     KFAC_HIP_CHECK(hipGetLastError());
     if (X) return bf ? launch_scatter<unsigned short, RANKED>(ctx, g, bytes) : launch_scatter<float, RANKED>(ctx, g, bytes);
+    KfacProfScope prof(ctx, KC_TOKENS, 0.0, 12.0 * (double)S);
     hipLaunchKernelGGL(sort_rows_kernel, dim3((unsigned)((S + THREADS - 1) / THREADS)), dim3(THREADS), 0, ctx->stream, s);
     KFAC_HIP_CHECK(hipGetLastError());
     return KFAC_OK;

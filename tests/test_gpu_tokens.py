@@ -385,6 +385,17 @@ def test_combine_gradient_by_differences(ctx):
         assert abs(float(loss(Ys + step, w) - loss(Ys, w) - dYs[r, c])) <= 64 * U * size
 
 
+def test_every_launch_is_counted(ctx):
+    """The order alone of many slots is three launches: their counts, the experts' first rows, and both together; the profile has the time of all of them."""
+    ids = random_ids(70000, 2, 40, torch.Generator().manual_seed(3)).to(DEV)
+    offsets, rows = torch.zeros(41, dtype=torch.int32, device=DEV), torch.zeros(70000, 2, dtype=torch.int32, device=DEV)
+    K.kfac_profile_begin(ctx.h)
+    K.kfac_experts_dispatch(ctx.h, ids, None, offsets, rows, None)
+    stat = K.kfac_profile_end(ctx.h)["experts_tokens"]
+    # ids read and rows written by the launch that counts; both, as they are by then, read and the rows written by the last
+    assert stat["launches"] == 2 and stat["bytes"] == (8.0 + 12.0) * 140000
+
+
 # ---------------------------------------------------------------- as they are used
 class Chain:
     """Route, sort, product, back, and the way back again, over buffers of one batch."""
