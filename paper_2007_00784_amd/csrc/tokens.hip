@@ -73,9 +73,17 @@ __device__ inline unsigned ordered(float x) {
 }
 __device__ inline float logit_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// exp(d) for d <= 0.  The product is off by 2^-24 of itself and its constant by less, as much as the difference d is already: no more than a sum of
-// probabilities is (results below 2^-126 are 0; infinity less infinity is NaN).
+// exp(d) for d <= 0.  With U = 2^-24 of the result: the product's rounding moves it by |d| U at most, the constant's by 0.23 |d| U, the instruction by 2 U (results
+// below 2^-126 are 0; infinity less infinity is NaN).  Of a softmax's sum that is little: the average of |d| over the softmax itself is at most ln E (its entropy
+// is that average plus the logarithm of the sum, and at most ln E), so a sum over 128 experts is off by 8 U, of 4096 by 12, as rounding its additions may.
 __device__ inline float exp_below(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504f); }
+// The same within 3 U however far d is, for what is a result by itself: what the product and its constant leave out is made good behind the instruction.  (A chosen logit
+// 80 below the largest had a weight that was off by 100 U.  Infinity, and infinity less infinity, give 0.)
+__device__ inline float exp_far(float d) {
+    d = fmaxf(d, -150.f);                                 // (infinity has no such rest)
+    const float p = d * 1.44269504f, rest = fmaf(d, 1.92596303e-8f, fmaf(d, 1.44269504f, -p)), r = __builtin_amdgcn_exp2f(p);
+    return fmaf(r, rest * 0.693147181f, r);
+}
 
 // A lane's logits of a token (base: lane N), -inf behind the last.
 template <typename T, int L, int V> __device__ inline void logits_of(const void *p, int64_t row, int base, int E, bool in, float (&x)[V]) {
@@ -195,9 +203,11 @@ template <typename T, int L, int V, bool ONE> __global__ __launch_bounds__(THREA
         }
     }
     float total = 0.f;
-    if (g.normalize) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) total += exp_below(w[c] - top);
+    for (int c = 0; c < C; ++c) w[c] = exp_far(w[c] - top);
+    if (g.normalize) {                                    // (top infinite: nothing but zeros, and zero over zero is NaN)
+#pragma unroll
+        for (int c = 0; c < C; ++c) total += w[c];
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) total += exp_below(x[v] - top);
@@ -208,7 +218,7 @@ template <typename T, int L, int V, bool ONE> __global__ __launch_bounds__(THREA
         const int j = c * L + lane;
         if (in && j < g.k) {
             g.ids[t * g.k + j] = id[c];
-            g.weights[t * g.k + j] = id[c] >= 0 ? exp_below(w[c] - top) / total : 0.f;
+            g.weights[t * g.k + j] = id[c] >= 0 ? w[c] / total : 0.f;
         }
     }
 }
@@ -247,7 +257,7 @@ template <typename T, int L, int V, bool ONE> __global__ __launch_bounds__(THREA
         top = some ? logit_of(most) : 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            x[v] = exp_below(x[v] - top);
+            x[v] = exp_far(x[v] - top);
             sum += x[v];
         }
         sum = group_sum<L>(sum);
@@ -280,7 +290,7 @@ template <typename T, int L, int V, bool ONE> __global__ __launch_bounds__(THREA
         top = some ? logit_of(most) : 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            p[c] = exp_below(p[c] - top);
+            p[c] = exp_far(p[c] - top);
             sum += p[c];
             inner = fmaf(p[c], id[c] >= 0 ? y[c] : 0.f, inner);
         }

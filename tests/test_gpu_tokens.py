@@ -198,6 +198,31 @@ def test_route_gradient_by_differences(ctx):
             assert ((diff - out[:, e].double()).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+def test_weights_of_far_logits(ctx, bf16):
+    """Two experts, the better one's logit 0, so that the difference of the logits is exact, however far the other one is.
+
+    In units of 2^-24 of the result: the exponential 2 (a last place) and the correction of its argument 1; the sum of both terms 1 for itself and less than 2
+    for the smaller term (its share is at most a half, and 1.22 d of it at most 0.35); the quotient 1.  The gradient has two such weights or sums, and three products.
+    """
+    gen = torch.Generator().manual_seed(9)
+    T, dt = 20000, torch.bfloat16 if bf16 else torch.float32
+    x = torch.zeros(T, 2)
+    x[:, 1] = -torch.rand(T, generator=gen) * 86.0                       # (e^-86 is a normal number)
+    logits = x.to(dt)
+    far = logits[:, 1].double()
+    want = torch.stack([1 / (1 + torch.exp(far)), torch.exp(far) / (1 + torch.exp(far))], 1)
+    for normalize in (False, True):
+        ids, w = torch.zeros(T, 2, dtype=torch.int32, device=DEV), torch.zeros(T, 2, device=DEV)
+        K.kfac_experts_route(ctx.h, logits.to(DEV), ids, w, normalize=normalize)
+        assert torch.equal(ids.cpu(), torch.tensor([[0, 1]], dtype=torch.int32).expand(T, 2))
+        near(w, want, 8 * U * want)
+        out = torch.zeros(T, 2, dtype=dt, device=DEV)
+        K.kfac_experts_route_grad(ctx.h, logits.to(DEV), ids, torch.tensor([[1.0, 0.0]], device=DEV).expand(T, 2).contiguous(), out, normalize=normalize)
+        grad = want[:, 0] * want[:, 1]
+        near(out[:, 1], -grad, 16 * U * grad + half_step(dt) * grad)
+
+
 # ---------------------------------------------------------------- the order of the slots
 def order_of(ids, E):
     """(offsets, rows) in plain Python's order."""
