@@ -173,6 +173,36 @@ def test_short_lists_without_workspace():
         c.close()
 
 
+@pytest.mark.parametrize("start", [0, 1])
+@pytest.mark.parametrize("dts", [[F32], [BF16], [F32, BF16]], ids=str)
+def test_more_than_the_cache_holds(ctx, dts, start):
+    """Over 256 MB of gradients, their last chunks in part, read past the cache; clipped in place and into buffers of the other type."""
+    sizes = [(75 << 20) + 12345, 4097, 3, 70000001] if F32 in dts else [(130 << 20) + 12345, 4097, 3]
+    grads = []
+    for i, n in enumerate(sizes):
+        buf = torch.full((n + start + 9,), math.nan, dtype=dts[i % len(dts)], device=DEV)
+        buf[start:start + n] = torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(i), device=DEV)
+        grads.append(buf[start:start + n])
+    assert sum(g.numel() * g.element_size() for g in grads) > 256e6
+    # (3 x 2^27 terms: of the sum 64 bits lose 2^-53 for each of a thread's, far below 2^-29)
+    want, norm, coef = norm_of(grads), one(), one()
+    K.kfac_grad_norm_batched(ctx.h, grads, norm, max_norm=want / 4, coef=coef)
+    assert abs(float(norm) - want) <= (U + 2.0 ** -29) * want and abs(float(coef) - 0.25) <= 2 * U
+    out = [torch.full_like(g, math.nan, dtype=BF16 if g.dtype == F32 else F32) for g in grads]
+    K.kfac_clip_grads_batched(ctx.h, K.grad_items(grads, out), want / 4, norm, coef)
+    fresh = [g.clone() for g in grads]
+    K.kfac_clip_grads_batched(ctx.h, fresh, want / 4, norm, coef)
+    for g, o, f in zip(grads, out, fresh):
+        w = g.double() * float(coef)
+        for r in (o, f):
+            assert ((r.double() - w).abs() <= (U + torch.finfo(r.dtype).eps / 2) * w.abs() + LEAST[r.dtype]).all()
+    K.kfac_clip_grads_batched(ctx.h, grads, want / 4, norm, coef)
+    for g, f in zip(grads, fresh):
+        assert torch.equal(g, f)
+        whole = g.as_strided((g.numel() + start + 9,), (1,), 0)
+        assert whole[:start].isnan().all() and whole[start + g.numel():].isnan().all()
+
+
 def test_same_bits_and_captured(ctx):
     """Repeated calls give the same bits; a captured clip takes each replay's gradients and scale; the optimizer reads the coefficient."""
     sizes = [70001, 13, 5000]
