@@ -173,14 +173,15 @@ __global__ __launch_bounds__(THREADS) void norm_join_kernel(const NormArgs g) {
     (void)join_sums(g, true, shared);
 }
 
-// N results of a thread from element i on; `in` of them exist.  Stored through the caches: what comes next reads them.  (Past them 25M gradients in fp32 took as long to
-// clip into other buffers, in place 58 us instead of 56, and 105M 212 instead of 195; read again at once, 63M took 184 with the clipping instead of 179.)
+// N results of a thread from element i on; `in` of them exist.
 template <typename O, int N> __device__ inline void put(void *p, int64_t i, int64_t in, const float (&x)[N]) {
     Vec<O, N> o;
 #pragma unroll
     for (int k = 0; k < N; ++k) o.x[k] = element_of<O>(x[k]);
-    if (in >= N) store(p, i, o);
-    else
+    if (in >= N) {
+        if constexpr (sizeof(o) == 16) store_past(p, i, o);
+        else store(p, i, o);
+    } else
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (k < in) ((O *)p)[i + k] = o.x[k];
@@ -214,7 +215,7 @@ template <int TH> __device__ inline void clip_chunk(const GradLaunch &a, int id,
     }
 }
 
-// The last chunks first: what was read last may still be in the cache.  No gradient is read a third time, so the loads go past it.
+// The last chunks first: what was read last may still be in the cache.  Nothing is read a third time, so loads and stores go past it.
 __global__ __launch_bounds__(THREADS) void clip_kernel(const GradLaunch a, const NormArgs g, bool writes) {
     __shared__ double shared[THREADS / 64];
     const float coef = join_sums(g, writes && blockIdx.x == 0, shared);
