@@ -315,7 +315,8 @@ class RoutedExpertRunner(ExpertRunner):
     weights, tokens sorted by expert, the products, and the weighted sum of each token's results; and the way back.
 
     x is [tokens, d_in]; the sorted rows of a step stay in self.xs, the gradients of their results in self.gs, where update_factors() takes them.
-    The router's parameters (fp32 [1, experts, d_in], no bias) take the optimizer step together with the experts'.
+    The router's parameters (fp32 [1, experts, d_in], no bias) take the optimizer step together with the experts'.  The logits are of the layer's type: in bf16
+    two experts' often tie, and the lower one is chosen.
     """
 
     def __init__(self, experts, tokens, topk, d_in, d_out, normalize=True, bias=True, bf16=True, **kw):
